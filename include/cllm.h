@@ -396,6 +396,110 @@ cllm_status cllm_seq_state(const cllm_ctx *ctx, int32_t seq, int32_t *committed_
 cllm_status cllm_timing_enable(cllm_ctx *ctx, int32_t kernel_class, int32_t max_rows, int32_t every);
 cllm_status cllm_timing_read(cllm_ctx *ctx, int64_t *launches, double *total_ms);
 
+/* Paged KV cache: a pool of pages that the requests of a server share, and the operators of a step on
+ * it, for decoders whose products the caller runs (any number of query heads per key head). The
+ * pool's books (free pages, block table, the step's rows) live on the device and are changed by
+ * kernels only, so the lengths of a step may come straight from the device (the accepted lengths of
+ * Jacobi blocks) and a step can be captured into a HIP graph: no call but create, free and status
+ * waits for the device or allocates.
+ *
+ * A slot (0 .. max_seqs - 1) holds a request. A layer's keys and values are two caller-owned device
+ * arrays k_pages, v_pages [n_pages][n_kv_heads][page_size][head_dim]; every layer uses the same block
+ * table. Token t of slot s is in page block_table[s][t / page_size] at offset t % page_size.
+ *
+ * head_dim: 32, 64, 128, or 256 (bf16) or 16 (fp32); n_heads a multiple of n_kv_heads, at most 1024;
+ * page_size 16, 32, 64, 128 or 256; n_pages * page_size below 2^31; max_seqs 1..1024; max_ctx (tokens
+ * of a request) and max_rows (new tokens of a plan, over all requests) 1..2^20. rope_base > 0: append
+ * turns queries and keys (rotate-half, angle t * rope_base^(-2j / head_dim) in double, rounded once to
+ * fp32); 0: it does not. dtype: of rows and pages. workspace: as in cllm_runtime_opts, of at least
+ * cllm_paged_workspace_bytes() bytes (books, rotary factors, attention partials); it need not be zero.
+ *
+ * Work is queued on the stream given at creation; calls on one cache share its books and partials, so
+ * whatever runs them (this thread, replayed graphs) is ordered by that stream. Calls may be made
+ * with any device current. Each array is memory that the cache's GPU can access (checked, else
+ * ERR_ARG); rows and pools are 16-byte aligned with row strides (in elements) of whole 16-byte
+ * vectors, the heads of a row contiguous. Sizes are not checked: an array of rows holds the plan's
+ * `rows` bound (with a bound of 0 append and attention do nothing and check no array). Rows behind the plan's last one, and pages of nobody, are left as they were. */
+typedef struct cllm_paged_config {
+    int32_t n_heads, n_kv_heads, head_dim, dtype;
+    int32_t page_size, n_pages;
+    int32_t max_seqs, max_ctx, max_rows;
+    float rope_base;
+    int32_t device;
+    void *stream;
+    void *workspace;
+    size_t workspace_bytes;
+} cllm_paged_config;
+typedef struct cllm_paged cllm_paged;
+
+/* Device arrays of a cache, for reading in the order of its stream. */
+typedef struct cllm_paged_views {
+    const int32_t *block_table; /* [max_seqs][max_pages] page ids, -1 where a slot has none */
+    const int32_t *seq_pages;   /* [max_seqs] pages of each slot */
+    const int32_t *free_list;   /* [n_pages]: the first (free pages) entries, the next page to take last */
+    const int32_t *row_start;   /* [n + 1] of the last plan: request b's rows are [row_start[b], row_start[b+1]) */
+    const int32_t *row_slot;    /* [rows]: page * page_size + offset */
+    const int32_t *row_pos;     /* [rows]: position */
+    int32_t max_pages;
+} cllm_paged_views;
+
+/* No device call. Errors: ERR_ARG (as cllm_paged_create's checks), ERR_OOM. */
+cllm_status cllm_paged_workspace_bytes(const cllm_paged_config *cfg, size_t *bytes);
+/* An empty cache. Synchronous. Errors: ERR_ARG (shape, workspace), ERR_CAPACITY (workspace too small),
+ * ERR_OOM, ERR_DEVICE. */
+cllm_status cllm_paged_create(const cllm_paged_config *cfg, cllm_paged **out);
+/* The caller has waited for the cache's stream before it frees the cache or a workspace of its own. */
+void cllm_paged_free(cllm_paged *c);
+/* Errors: ERR_ARG. */
+cllm_status cllm_paged_views_get(cllm_paged *c, cllm_paged_views *views);
+
+/* Block tables and slot maps of a step. Entry b of n is slot seq_ids[b] with ctx_lens[b] tokens
+ * already written and new_lens[b] to come (device arrays; 0 is a length): afterwards the slot owns
+ * exactly the pages of ctx_lens[b] + new_lens[b] tokens. Surplus pages go back first, the last entry's
+ * last page first, then missing ones are taken entry after entry, token after token; so a later plan
+ * that undoes this one restores the free list, and a request ends with both lengths 0. Slots that are
+ * not listed keep their pages. The rows of the step are the new tokens, entry after entry: row r of
+ * entry b is position ctx_lens[b] + r - row_start[b].
+ * rows, max_new, max_len: the host's bounds of the step's rows, of new_lens[b] (0: rows) and of
+ * ctx_lens[b] + new_lens[b] (0: max_ctx). Append and attention are launched for them; tighter bounds
+ * are faster.
+ * The lengths are on the device, so a plan that cannot be is known there only: a slot out of range or
+ * twice, a length negative or above its bound, more rows than `rows` or too few free pages refuse the
+ * whole plan. The books stay as they were, the plan has no rows (append and attention then do nothing)
+ * and cllm_paged_status says why.
+ * Errors: ERR_ARG (n outside [1, max_seqs], NULL or inaccessible arrays, bounds), ERR_CAPACITY (rows
+ * above max_rows, max_len above max_ctx), ERR_DEVICE. */
+cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, const int32_t *ctx_lens,
+                            const int32_t *new_lens, int32_t rows, int32_t max_new, int32_t max_len);
+
+/* The rows of the last plan into the pages of one layer: k and v rows ([n_kv_heads][head_dim]) to
+ * their slots, keys and queries (q rows [n_heads][head_dim] to q_out, which may be q) turned by their
+ * positions where rope_base > 0, in fp32 and rounded once. q and q_out NULL: keys and values only.
+ * A step may be appended again (another layer, or the same with other values).
+ * Errors: ERR_ARG, ERR_STATE (no plan yet), ERR_DEVICE. */
+cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                              int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages);
+
+/* Attention of the last plan's rows over the pages of one layer: out row r (of entry b, head h) =
+ * softmax over the positions t <= row_pos[r] of slot seq_ids[b] of scale q[r][h] . k[t][h / group]
+ * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim). lse (or NULL): fp32
+ * [rows][n_heads], the natural log of the sum of exponentials of the scaled scores. out may be q with
+ * q's stride. Statistics, products and sums in fp32 (bf16: the products of bf16 values, probabilities
+ * as two bf16 planes), the output rounded once. A row's bits depend on its queries, its position and
+ * the keys and values up to it alone, not on the chunk, the other requests, the pages or the bounds: a
+ * block of one token and a block of 64 give the same row. What a page holds past a row's position
+ * (another request's remains, rejected tokens, NaN) does not reach it.
+ * Errors: ERR_ARG, ERR_STATE (no plan yet), ERR_DEVICE. */
+cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                            float scale, void *out, int64_t out_stride, float *lse);
+
+/* Waits for the stream and says how the last plan went: its rows and the free pages (either may be
+ * NULL). Errors: ERR_ARG or ERR_CAPACITY (the plan was refused), ERR_STATE (append or attention of a
+ * replayed graph ran behind a plan with other bounds than its own and did nothing; or the stream is
+ * being captured), ERR_DEVICE. */
+cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages);
+const char *cllm_paged_last_error(const cllm_paged *c);
+
 /* Bytes of weights streamed by one forward pass (all matrices except the embedding), after
  * padding to the kernels' tiles. */
 int64_t cllm_streamed_weight_bytes(const cllm_ctx *ctx);

@@ -52,12 +52,25 @@ class cllm_trace_stats(ctypes.Structure):
                 ("stationary_per_window", _dbl)]
 
 
+class cllm_paged_config(ctypes.Structure):
+    _fields_ = [("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("dtype", _i32), ("page_size", _i32),
+                ("n_pages", _i32), ("max_seqs", _i32), ("max_ctx", _i32), ("max_rows", _i32), ("rope_base", _f32),
+                ("device", _i32), ("stream", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class cllm_paged_views(ctypes.Structure):
+    _fields_ = [("block_table", _vp), ("seq_pages", _vp), ("free_list", _vp), ("row_start", _vp), ("row_slot", _vp),
+                ("row_pos", _vp), ("max_pages", _i32)]
+
+
 TRACE_STRIDE = 5 + 2 * 64  # CLLM_TRACE_STRIDE
 
 EXPORTS = ["cllm_model_create", "cllm_model_set_weights", "cllm_model_init_random", "cllm_model_load", "cllm_model_free", "cllm_prefill",
            "cllm_jacobi_step", "cllm_jacobi_decode", "cllm_ar_decode", "cllm_jacobi_step_batch",
            "cllm_jacobi_decode_batch", "cllm_reset", "cllm_debug_logits", "cllm_trace_enable", "cllm_trace_read",
            "cllm_trace_count", "cllm_collect_states", "cllm_loss_head", "cllm_loss_head_device", "cllm_hidden_rows", "cllm_hidden_rows_noalloc", "cllm_seq_state", "cllm_timing_enable", "cllm_timing_read",
+           "cllm_paged_workspace_bytes", "cllm_paged_create", "cllm_paged_free", "cllm_paged_views_get", "cllm_paged_plan",
+           "cllm_paged_append", "cllm_paged_attn", "cllm_paged_status", "cllm_paged_last_error",
            "cllm_streamed_weight_bytes", "cllm_workspace_bytes", "cllm_status_string", "cllm_last_error"]
 
 _lib = None
@@ -112,8 +125,19 @@ def lib():
         L.cllm_status_string.restype = ctypes.c_char_p
         L.cllm_last_error.argtypes = [_vp]
         L.cllm_last_error.restype = ctypes.c_char_p
+        L.cllm_paged_workspace_bytes.argtypes = [P(cllm_paged_config), P(ctypes.c_size_t)]
+        L.cllm_paged_create.argtypes = [P(cllm_paged_config), P(_vp)]
+        L.cllm_paged_free.argtypes = [_vp]
+        L.cllm_paged_free.restype = None
+        L.cllm_paged_views_get.argtypes = [_vp, P(cllm_paged_views)]
+        L.cllm_paged_plan.argtypes = [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32]
+        L.cllm_paged_append.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+        L.cllm_paged_attn.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]
+        L.cllm_paged_status.argtypes = [_vp, P(_i32), P(_i32)]
+        L.cllm_paged_last_error.argtypes = [_vp]
+        L.cllm_paged_last_error.restype = ctypes.c_char_p
         for name in EXPORTS:
-            if name not in ("cllm_model_free", "cllm_streamed_weight_bytes", "cllm_status_string",
+            if name not in ("cllm_paged_free", "cllm_paged_last_error", "cllm_model_free", "cllm_streamed_weight_bytes", "cllm_status_string",
                             "cllm_last_error"):
                 getattr(L, name).restype = _i32
         _lib = L
@@ -382,6 +406,151 @@ def _dev_ptr(x, count, dtype):
         raise ValueError(f"device array: need a contiguous {dtype} tensor of >= {count} elements, got "
                          f"{x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
+
+
+class PagedCache:
+    """A paged KV cache (cllm_paged_*): the books of a page pool that the requests of a server share,
+    and the operators of a step on it, on PyTorch tensors of the cache's GPU:
+
+        cache.plan(seq_ids, ctx_lens, new_lens, rows)      # pages and rows of the step
+        per layer: cache.append(q, k, v, q, k_pages, v_pages); cache.attn(q, k_pages, v_pages, out)
+
+    Work is queued on the stream given at creation (None: PyTorch's current one), which has to be
+    PyTorch's current stream in every call. block_table, seq_pages, free_list, row_start, row_slot and
+    row_pos are int32 tensors over the cache's own books, to be read in that stream's order."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, max_ctx, max_rows, dtype="bf16",
+                 rope_base=0.0, device=0, stream=None):
+        import torch
+        if dtype not in ("bf16", "f32"):
+            raise ValueError("dtype must be 'bf16' or 'f32'")
+        self.L = lib()
+        self.h = None
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
+        self.max_rows, self.rows = max_rows, 0
+        self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.pool_shape = (n_pages, n_kv_heads, page_size, head_dim)
+        cfg = cllm_paged_config(n_heads, n_kv_heads, head_dim, 1 if dtype == "bf16" else 0, page_size, n_pages, max_seqs,
+                                max_ctx, max_rows, rope_base, device, None, None, 0)
+        n = ctypes.c_size_t(0)
+        st = self.L.cllm_paged_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n))
+        if st != CLLM_OK:
+            raise CllmError(st, "cllm_paged_workspace_bytes failed")
+        self.device = torch.device("cuda", device)
+        self._current = torch.cuda.current_stream
+        cur = self._current(self.device)
+        self.stream = cur.cuda_stream if stream is None else stream
+        self._ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        if self.stream != cur.cuda_stream:
+            cur.synchronize()  # the memory's last user in the allocator's order
+        cfg.stream, cfg.workspace, cfg.workspace_bytes = self.stream, self._ws.data_ptr(), n.value
+        h = _vp()
+        st = self.L.cllm_paged_create(ctypes.byref(cfg), ctypes.byref(h))
+        if st != CLLM_OK:
+            raise CllmError(st, "cllm_paged_create failed")
+        self.h = h
+        v = cllm_paged_views()
+        self._check(self.L.cllm_paged_views_get(h, ctypes.byref(v)))
+
+        def view(ptr, *shape):
+            o, count = ptr - self._ws.data_ptr(), 1
+            for x in shape:
+                count *= x
+            return self._ws[o:o + 4 * count].view(torch.int32).view(*shape)
+
+        self.block_table = view(v.block_table, max_seqs, v.max_pages)
+        self.seq_pages, self.free_list = view(v.seq_pages, max_seqs), view(v.free_list, n_pages)
+        self.row_start, self.row_slot = view(v.row_start, max_seqs + 1), view(v.row_slot, max_rows)
+        self.row_pos = view(v.row_pos, max_rows)
+
+    def close(self):
+        if getattr(self, "h", None):
+            import torch
+            torch.cuda.synchronize(self.device)  # work in flight still reads the books
+            self.L.cllm_paged_free(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st):
+        if st != CLLM_OK:
+            msg = self.L.cllm_paged_last_error(self.h)
+            raise CllmError(st, msg.decode() if msg else "")
+
+    def _on_stream(self):
+        if not self.h:
+            raise ValueError("the cache is closed")
+        if self._current(self.device).cuda_stream != self.stream:
+            raise ValueError("PyTorch's current stream is not the cache's")
+
+    def _lens(self, x, n):
+        import torch
+        if x.dtype != torch.int32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"lengths: contiguous int32 tensors of one size on {self.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
+
+    def _rows(self, x, heads, name):
+        """Address and row stride of rows [>= the plan's rows][heads][head_dim] (or [..][heads * head_dim])."""
+        s, t = x.shape, x.stride()
+        whole = (len(s) == 3 and s[1] == heads and s[2] == self.head_dim and t[2] == 1 and (heads == 1 or t[1] == self.head_dim)
+                 ) or (len(s) == 2 and s[1] == heads * self.head_dim and t[1] == 1)
+        if not whole or s[0] < self.rows or x.dtype != self.dtype or x.device != self.device:
+            raise ValueError(f"{name}: at least {self.rows} rows of {heads} x {self.head_dim} {self.dtype} with contiguous "
+                             f"heads on {self.device}, got {x.dtype} {tuple(s)} strides {tuple(t)} on {x.device}")
+        return x.data_ptr(), (t[0] if s[0] > 1 else heads * self.head_dim)
+
+    def _pool(self, x, name):
+        if tuple(x.shape) != self.pool_shape or x.dtype != self.dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {self.dtype} tensor {self.pool_shape} on {self.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
+
+    def plan(self, seq_ids, ctx_lens, new_lens, rows, max_new=0, max_len=0):
+        """cllm_paged_plan: int32 tensors of one size; rows, max_new, max_len: the host's bounds."""
+        self._on_stream()
+        n = seq_ids.numel()
+        self._check(self.L.cllm_paged_plan(self.h, n, self._lens(seq_ids, n), self._lens(ctx_lens, n),
+                                           self._lens(new_lens, n), rows, max_new, max_len))
+        self.rows = rows
+
+    def append(self, q, k, v, q_out, k_pages, v_pages):
+        """cllm_paged_append: rows q [.., n_heads, head_dim] (or None, with q_out), k and v
+        [.., n_kv_heads, head_dim], of any row stride, into pools of pool_shape."""
+        self._on_stream()
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        none = (None, 0)
+        qa = none if q is None else self._rows(q, self.n_heads, "q")
+        qo = none if q_out is None else self._rows(q_out, self.n_heads, "q_out")
+        self._check(self.L.cllm_paged_append(self.h, *qa, *self._rows(k, self.n_kv_heads, "k"),
+                                             *self._rows(v, self.n_kv_heads, "v"), *qo, self._pool(k_pages, "k_pages"),
+                                             self._pool(v_pages, "v_pages")))
+
+    def attn(self, q, k_pages, v_pages, out, scale=None, lse=None):
+        """cllm_paged_attn: rows q [.., n_heads, head_dim] over the pools into out (of q's shape); lse: a
+        contiguous float32 [.., n_heads]. scale None: 1 / sqrt(head_dim)."""
+        self._on_stream()
+        if scale is not None and not scale:
+            raise ValueError("scale must not be 0")
+        if lse is not None:
+            import torch
+            if lse.dtype != torch.float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
+                    not lse.is_contiguous() or lse.device != self.device:
+                raise ValueError(f"lse: a contiguous float32 tensor of at least {self.rows} x {self.n_heads} on {self.device}")
+        self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
+                                           self._pool(v_pages, "v_pages"), scale or 0.0, *self._rows(out, self.n_heads, "out"),
+                                           None if lse is None else lse.data_ptr()))
+
+    def status(self):
+        """cllm_paged_status: (rows of the last plan, free pages); raises when it was refused."""
+        rows, free = _i32(0), _i32(0)
+        self._check(self.L.cllm_paged_status(self.h, ctypes.byref(rows), ctypes.byref(free)))
+        return int(rows.value), int(free.value)
 
 
 def records_to_dicts(raw):

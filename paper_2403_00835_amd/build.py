@@ -17,7 +17,7 @@ ARCH = "gfx950"
 # float code.
 HIP_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I" + INCLUDE]
-SOURCES = ["gemm.hip", "kernels.hip", "loss.hip", "capi.cpp"]
+SOURCES = ["gemm.hip", "kernels.hip", "loss.hip", "capi.cpp", "paged.hip", "paged_attn.hip", "paged_capi.cpp"]
 
 
 def _run(cmd, verbose):
