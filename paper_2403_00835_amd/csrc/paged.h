@@ -6,9 +6,17 @@
 namespace cllm {
 
 constexpr int kPagedMaxSeqs = 1024;   // one plan thread per request
-constexpr int kPagedBlockRows = 64;   // query rows (row x head of a group) of one attention unit
-constexpr int kPagedSpanKeys = 512;   // keys of a span, at absolute positions: what a split unit takes
-constexpr int kPagedSplitBelow = 512; // workgroups below which long contexts are split into spans
+// Rows of a request's attention: new tokens x heads of a group. Requests of few rows (a token, a Jacobi
+// block), and fp32, take units of paged_block_rows() rows and spans of keys; longer bf16 chunks take tiles
+// of kPagedTileRows rows and a range of keys.
+constexpr int kPagedFewRows = 64;
+constexpr int kPagedTileRows = 128;
+constexpr int kPagedItemRows = 32;    // rows that are joined together
+// A wave holds a chunk of keys in registers beside its rows: of 512-byte keys, half the rows.
+constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >= 512 ? 16 : 32; }
+constexpr int kPagedSpanKeys = 512;   // keys of a span, at absolute positions
+constexpr int kPagedSplitBelow = 2048;  // workgroups below which row blocks are split into their spans
+constexpr int kPagedTileGroups = 512;   // workgroups that tiles of few requests are split into, about
 
 // Words of the status block, written by the plan.
 enum PagedStatus {
@@ -16,13 +24,29 @@ enum PagedStatus {
     PS_ENTRIES = 1,  // requests of the plan
     PS_FLAGS = 2,    // PF_* of the plan
     PS_FREE = 3,     // free pages
-    PS_UNITS = 4,    // attention units
-    PS_ITEMS = 5,    // split row blocks, whose spans are joined
+    PS_UNITS = 4,    // attention units of row blocks
+    PS_TILES = 5,    // attention units of tiles
     PS_BOUND_ROWS = 6, PS_BOUND_NEW = 7, PS_BOUND_LEN = 8,  // the plan's bounds
-    PS_LATE = 9,     // a call made for other bounds than the plan's ran (and did nothing)
+    PS_ITEMS = 9,    // row blocks whose partial states are joined
+    PS_LATE = 10,    // a call made for other bounds than the plan's ran (and did nothing)
     PS_WORDS = 16
 };
 enum PagedFlags { PF_ARG = 1, PF_ROWS = 2, PF_PAGES = 4 };
+
+// What one workgroup takes (per key head), and a row block whose partial states are joined.
+struct alignas(16) PagedUnit {
+    int slot, ctx, m, r0;  // the request: slot, context, new tokens, first row of the plan
+    int row;               // first row of the block or tile
+    int k0, k1;            // row blocks: the span and -, or -1: every span; tiles: chunks [k0, k1)
+    int part;              // partial row of the first row, or -1: none, the output is written
+};
+struct alignas(16) PagedItem {
+    int ctx, m, r0, row;
+    int part;    // partial row of the first row in the first span or range
+    int stride;  // partial rows from one span or range to the next
+    int count;   // ranges; 0: the spans up to the row's position
+    int pad;
+};
 
 // Device memory of a cache: the books of its pool and the last plan.
 struct PagedBooks {
@@ -33,9 +57,9 @@ struct PagedBooks {
     int32_t *row_start;  // [max_seqs + 1]
     int32_t *row_slot;   // [max_rows]: page * page_size + offset
     int32_t *row_pos;    // [max_rows]
-    int4 *ent;           // per request: slot, context, new tokens, first row
-    int4 *units;         // request, row block, span (-1: all of them), partial row (-1: none)
-    int4 *items;         // request, row block, first partial row, spans
+    PagedUnit *units, *tiles;
+    PagedItem *items;
+    int cap_units, cap_tiles, cap_items;  // entries of the three
     int max_seqs, max_pages, n_pages, page_shift;
 };
 
@@ -44,7 +68,9 @@ struct PagedPlanParams {
     const int32_t *seq, *ctx, *neu;
     int n, rows, max_new, max_len;  // the call's bounds
     int group, n_kv;                // query heads per key head, key heads
-    int cap_units, cap_items, cap_part;
+    bool tiled;                     // long chunks take tiles
+    int block_rows;                 // of the others
+    int cap_part;                   // partial rows
 };
 
 struct PagedAppendParams {
@@ -84,7 +110,7 @@ hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int
                              double rope_base, hipStream_t s);
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s);
 hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_t s);
-// units: upper bound of the launch's attention units; split: some row block may be in several spans.
-hipError_t launch_paged_attn(bool bf16, int64_t units, bool split, const PagedAttnParams &p, hipStream_t s);
+// Upper bounds of the plan's units and tiles; join: some may be split.
+hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s);
 
 }  // namespace cllm

@@ -16,27 +16,36 @@ namespace {
 constexpr int kPlanThreads = kPagedMaxSeqs;
 static_assert(kPlanThreads == 1024, "one thread per request");
 
-// Exclusive prefix sum over the workgroup; total: the sum. s_wave: 16 words of LDS.
-__device__ __forceinline__ int block_scan(int v, int *s_wave, int &total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    int x = v;
+// Exclusive prefix sums of N values over the workgroup, in place; total: the sums. s_wave: LDS.
+template <int N>
+__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (&s_wave)[N][kPlanThreads / kWave]) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int x[N];
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        if (lane >= off) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) s_wave[w] = x;
-    __syncthreads();
-    int before = 0, all = 0;
+    for (int k = 0; k < N; ++k) x[k] = v[k];
 #pragma unroll
-    for (int i = 0; i < kPlanThreads / kWave; ++i) {
-        const int t = s_wave[i];
-        before += i < w ? t : 0;
-        all += t;
+    for (int off = 1; off < kWave; off <<= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int y = __shfl_up(x[k], off);
+            if (lane >= off) x[k] += y;
+        }
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < N; ++k) s_wave[k][w] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        int t = s_wave[k][lane & (kPlanThreads / kWave - 1)];
+#pragma unroll
+        for (int off = 1; off < kPlanThreads / kWave; off <<= 1) {
+            const int y = __shfl_up(t, off);
+            if (lane >= off) t += y;
+        }
+        total[k] = __builtin_amdgcn_readlane(t, kPlanThreads / kWave - 1);
+        const int before = w > 0 ? __builtin_amdgcn_readlane(t, w - 1) : 0;
+        v[k] = before + x[k] - v[k];
     }
-    total = all;
-    return before + x - v;
 }
 
 // The entry e with start[e] <= i < start[e + 1] (start: n + 1 ascending words of LDS).
@@ -76,13 +85,13 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // (bad slot or length, more rows than the bound, too few pages) leaves the books as they were and has
 // no rows.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
-    __shared__ int s_wave[kPlanThreads / kWave];
+    __shared__ int s_wave[5][kPlanThreads / kWave], s_wave2[4][kPlanThreads / kWave];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
-    __shared__ int s_seq[kPlanThreads], s_ctx[kPlanThreads], s_own[kPlanThreads];
+    __shared__ int s_unit[kPlanThreads + 1], s_tile[kPlanThreads + 1], s_item[kPlanThreads + 1], s_part[kPlanThreads];
+    __shared__ int s_seq[kPlanThreads], s_ctx[kPlanThreads], s_m[kPlanThreads], s_own[kPlanThreads];
     __shared__ uint32_t s_seen[kPagedMaxSeqs / 32];
     const PagedBooks bk = p.bk;
     const int b = threadIdx.x, n = p.n, P = 1 << bk.page_shift;
-    if (b < kPagedMaxSeqs / 32) s_seen[b] = 0;
     const int free0 = bk.status[PS_FREE];
     int seq = 0, ctx = 0, m = 0;
     if (b < n) {
@@ -90,44 +99,72 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         ctx = p.ctx[b];
         m = p.neu[b];
     }
+    if (b < kPagedMaxSeqs / 32) s_seen[b] = 0;
     __syncthreads();
     bool bad = false;
     int own = 0, need = 0;
     if (b < n) {
         bad = seq < 0 || seq >= bk.max_seqs || ctx < 0 || m < 0 || m > p.max_new || ctx > p.max_len - m;
         if (!bad) {
-            bad = (atomicOr(&s_seen[seq >> 5], 1u << (seq & 31)) >> (seq & 31)) & 1;  // the slot appears twice
             own = bk.seq_pages[seq];
             need = (ctx + m + P - 1) >> bk.page_shift;
-        } else {
-            m = 0;
+            bad = (atomicOr(&s_seen[seq >> 5], 1u << (seq & 31)) >> (seq & 31)) & 1;  // the slot appears twice
         }
+        if (bad) m = 0;
     }
     int flags = __syncthreads_or(bad) ? PF_ARG : 0;
     // 1024 requests of at most 2^20 new tokens: the sums fit 31 bits
-    int R, G, T;
-    const int give = max(own - need, 0), take = max(need - own, 0);
-    const int r0 = block_scan(m, s_wave, R), g0 = block_scan(give, s_wave, G), t0 = block_scan(take, s_wave, T);
+    const int T0 = m * p.group;  // rows of the request's attention
+    const bool tiled = p.tiled && T0 > kPagedFewRows;
+    const int nrb = tiled ? 0 : (T0 + p.block_rows - 1) / p.block_rows;
+    const int ntile = tiled ? (T0 + kPagedTileRows - 1) / kPagedTileRows : 0;
+    int v[5] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile}, total[5];
+    block_scan(v, total, s_wave);
+    const int R = total[0], G = total[1], T = total[2];
     if (R > p.rows) flags |= PF_ROWS;
     if (T > free0 + G) flags |= PF_PAGES;
     if (flags) {  // uniform
         if (b == 0) {
-            bk.status[PS_ROWS] = bk.status[PS_ENTRIES] = bk.status[PS_UNITS] = bk.status[PS_ITEMS] = 0;
+            bk.status[PS_ROWS] = bk.status[PS_ENTRIES] = bk.status[PS_UNITS] = bk.status[PS_TILES] = bk.status[PS_ITEMS] = 0;
             bk.status[PS_FLAGS] = flags;
             bk.status[PS_LATE] = 0;
         }
         return;
     }
+    // Attention units. Row blocks: all the keys that the rows see, or, where that leaves workgroups idle,
+    // a unit per span (of the request's last token: units of spans that a block does not see do nothing).
+    // Tiles: ranges of keys, as many as make kPagedTileGroups workgroups of the plan's tiles, none under
+    // a span's keys. What the partial states' memory does not hold is not split.
+    int U = total[3], UT = total[4], I = 0, u0 = v[3], t0 = v[4], i0 = 0, p0 = 0, nspan = 1, nrange = 1;
+    {
+        const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
+        const int ranges = UT > 0 ? (kPagedTileGroups + UT * p.n_kv - 1) / (UT * p.n_kv) : 1;
+        const int ns = nrb && U * p.n_kv < kPagedSplitBelow ? spans : 1, nr = ntile ? min(ranges, spans) : 1;
+        const bool parts = ns > 1 || nr > 1;
+        int x[4] = {nrb * ns, ntile * nr, parts ? (T0 + kPagedItemRows - 1) / kPagedItemRows : 0, parts ? max(ns, nr) * T0 : 0};
+        int y[4];
+        block_scan(x, y, s_wave2);
+        if (y[0] <= bk.cap_units && y[1] <= bk.cap_tiles && y[2] <= bk.cap_items && y[3] <= p.cap_part)
+            U = y[0], UT = y[1], I = y[2], u0 = x[0], t0 = x[1], i0 = x[2], p0 = x[3], nspan = ns, nrange = nr;
+    }
     s_seq[b] = seq;
     s_ctx[b] = ctx;
+    s_m[b] = m;
     s_own[b] = own;
-    s_rows[b] = r0;
-    s_give[b] = g0;
-    s_take[b] = t0;
+    s_rows[b] = v[0];
+    s_give[b] = v[1];
+    s_take[b] = v[2];
+    s_unit[b] = u0;
+    s_tile[b] = t0;
+    s_item[b] = i0;
+    s_part[b] = nspan > 1 || nrange > 1 ? p0 : -1;
     if (b == 0) {
         s_rows[kPlanThreads] = R;
         s_give[kPlanThreads] = G;
         s_take[kPlanThreads] = T;
+        s_unit[kPlanThreads] = U;
+        s_tile[kPlanThreads] = UT;
+        s_item[kPlanThreads] = I;
     }
     __syncthreads();
     for (int i = b; i < G; i += kPlanThreads) {
@@ -136,57 +173,37 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         bk.free_list[free0 + G - s_give[e + 1] + k] = *at;
         *at = -1;
     }
-    __syncthreads();
+    if (G > 0) __syncthreads();  // uniform
     for (int i = b; i < T; i += kPlanThreads) {
         const int e = entry_of(s_take, n, i);
         bk.table[(size_t)s_seq[e] * bk.max_pages + s_own[e] + i - s_take[e]] = bk.free_list[free0 + G - 1 - i];
     }
     if (b < n) {
         bk.seq_pages[seq] = need;
-        bk.ent[b] = int4{seq, ctx, m, r0};
-        bk.row_start[b] = r0;
+        bk.row_start[b] = v[0];
     }
     if (b == 0) bk.row_start[n] = R;
-    __syncthreads();
-    for (int i = b; i < R; i += kPlanThreads) {
-        const int e = entry_of(s_rows, n, i), pos = s_ctx[e] + i - s_rows[e];
-        const int page = bk.table[(size_t)s_seq[e] * bk.max_pages + (pos >> bk.page_shift)];
-        bk.row_slot[i] = (page << bk.page_shift) + (pos & (P - 1));
-        bk.row_pos[i] = pos;
+    for (int i = b; i < U; i += kPlanThreads) {
+        const int e = entry_of(s_unit, n, i), k = i - s_unit[e], rows = s_m[e] * p.group;
+        const int blocks = (rows + p.block_rows - 1) / p.block_rows, part = s_part[e];
+        // the blocks of a span next to each other: they read the same keys
+        const int row = k % blocks * p.block_rows, span = k / blocks;
+        bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, part < 0 ? -1 : span, 0,
+                                part < 0 ? -1 : part + span * rows + row};
     }
-    // Attention units: row blocks of a request, each with all the keys that its rows see, or, where
-    // they are too few to fill the card, one unit per span of keys (if the partials hold them).
-    const int T0 = m * p.group, nrb = (T0 + kPagedBlockRows - 1) / kPagedBlockRows;
-    int U, u0 = block_scan(nrb, s_wave, U), I = 0, i0 = 0, p0 = 0;
-    bool split = U * p.n_kv < kPagedSplitBelow;
-    auto spans_of = [&](int rb) {
-        return (ctx + min(m - 1, (rb * kPagedBlockRows + kPagedBlockRows - 1) / p.group)) / kPagedSpanKeys + 1;
-    };
-    auto rows_of = [&](int rb) { return min(kPagedBlockRows, T0 - rb * kPagedBlockRows); };
-    if (split) {
-        int nu = 0, ni = 0, np = 0;
-        for (int rb = 0; rb < nrb; ++rb) {
-            const int sp = spans_of(rb);
-            nu += sp;
-            ni += sp > 1;
-            np += sp > 1 ? sp * rows_of(rb) : 0;
-        }
-        int U1, I1, P1;
-        const int u1 = block_scan(nu, s_wave, U1), i1 = block_scan(ni, s_wave, I1), p1 = block_scan(np, s_wave, P1);
-        split = U1 <= p.cap_units && I1 <= p.cap_items && P1 <= p.cap_part;
-        if (split) U = U1, u0 = u1, I = I1, i0 = i1, p0 = p1;
+    for (int i = b; i < UT; i += kPlanThreads) {
+        const int e = entry_of(s_tile, n, i), k = i - s_tile[e], rows = s_m[e] * p.group;
+        const int tiles = (rows + kPagedTileRows - 1) / kPagedTileRows, part = s_part[e];
+        const int ranges = (s_tile[e + 1] - s_tile[e]) / tiles, j = k / tiles;
+        const int row = (tiles - 1 - k % tiles) * kPagedTileRows;  // the tiles that see most keys first
+        const int chunks = (s_ctx[e] + s_m[e] + kAttnChunk - 1) / kAttnChunk, per = (chunks + ranges - 1) / ranges;
+        bk.tiles[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, j * per, min(chunks, (j + 1) * per),
+                                part < 0 ? -1 : part + j * rows + row};
     }
-    for (int rb = 0; rb < nrb; ++rb) {
-        const int sp = split ? spans_of(rb) : 1;
-        if (sp == 1) {
-            bk.units[u0++] = int4{b, rb, -1, -1};
-            continue;
-        }
-        bk.items[i0++] = int4{b, rb, p0, sp};
-        for (int s = 0; s < sp; ++s) {
-            bk.units[u0++] = int4{b, rb, s, p0};
-            p0 += rows_of(rb);
-        }
+    for (int i = b; i < I; i += kPlanThreads) {
+        const int e = entry_of(s_item, n, i), row = (i - s_item[e]) * kPagedItemRows, rows = s_m[e] * p.group;
+        const int tiles = (rows + kPagedTileRows - 1) / kPagedTileRows;
+        bk.items[i] = PagedItem{s_ctx[e], s_m[e], s_rows[e], row, s_part[e] + row, rows, (s_tile[e + 1] - s_tile[e]) / tiles, 0};
     }
     if (b == 0) {
         bk.status[PS_ROWS] = R;
@@ -194,11 +211,19 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         bk.status[PS_FLAGS] = 0;
         bk.status[PS_FREE] = free0 + G - T;
         bk.status[PS_UNITS] = U;
+        bk.status[PS_TILES] = UT;
         bk.status[PS_ITEMS] = I;
         bk.status[PS_BOUND_ROWS] = p.rows;
         bk.status[PS_BOUND_NEW] = p.max_new;
         bk.status[PS_BOUND_LEN] = p.max_len;
         bk.status[PS_LATE] = 0;
+    }
+    if (R > 0) __syncthreads();  // the tables
+    for (int i = b; i < R; i += kPlanThreads) {
+        const int e = entry_of(s_rows, n, i), pos = s_ctx[e] + i - s_rows[e];
+        const int page = bk.table[(size_t)s_seq[e] * bk.max_pages + (pos >> bk.page_shift)];
+        bk.row_slot[i] = (page << bk.page_shift) + (pos & (P - 1));
+        bk.row_pos[i] = pos;
     }
 }
 

@@ -1,15 +1,21 @@
 // Attention of chunks of new tokens over a paged KV cache on gfx950.
 //
-// Row (b, i, h) of a plan, token i of request b's chunk at position ctx_b + i, head h of the group of
-// key head h / group: softmax over the request's tokens t <= ctx_b + i of scale q . k_t, times v_t. The
-// keys of a request are walked in chunks of 64 at absolute positions. A chunk's state per row is its
-// maximum, its sum and its unnormalised output; states are merged in position order, the chunks of a
-// span of 512 keys first, then the spans. The order depends on positions alone: a row's bits are the
-// same whichever rows, requests, pages and launches it is computed with.
+// Row (i, h) of a request, token i of its chunk at position ctx + i, head h of the group of a key head:
+// softmax over the request's tokens t <= ctx + i of scale q . k_t, times v_t. Rows of a request and key
+// head are numbered i x group + h.
 //
-// Values: scores and softmax statistics in fp32; bf16 probabilities as hi + lo planes (~2^-17), so the
-// only rounding to bf16 is that of the output. Keys past a row's position contribute nothing, whatever
-// their values (NaN, infinities): scores are selected away, and values by the rules at chunk_output.
+// Few rows (paged_span_kernel): the keys are walked in chunks of 64 at absolute positions. A chunk's
+// state per row is its maximum, its sum and its unnormalised output; the states of the chunks that hold
+// a key the row sees are merged in position order into that of a span of 512 keys, and the spans' into
+// the row's. The order depends on positions alone: a row's bits are the same whichever rows, requests,
+// pages and launches it is computed with.
+// Long chunks (paged_tile_kernel): tiles of 128 rows walk their keys with a running maximum; ranges of
+// keys are joined where there are few tiles.
+//
+// Values: scores and softmax statistics in fp32; the probabilities of few rows as hi + lo bf16 planes
+// (~2^-17), so the only rounding to bf16 is that of the output. Keys past a row's position contribute
+// nothing, whatever their values (NaN, infinities): scores are selected away, values by the rules in
+// paged_span_kernel.
 #include <algorithm>
 
 #include "device.h"
@@ -21,29 +27,22 @@ namespace {
 
 constexpr int kKeys = kAttnChunk;  // keys of a chunk
 constexpr int kSpanChunks = kPagedSpanKeys / kKeys;
+constexpr float kLn2 = 0.6931471805599453f;
 
-// LDS image of a chunk's K or V: [64 keys][head_dim], 16-byte pieces permuted within a row so that the
-// reads below hit different banks: K is read 16 keys at one column (lanes of a group), bf16 V 16 keys
-// x 32 bytes (transposing reads), fp32 V 4 keys (4 apart) x 64 bytes.
-template <Prec P, int HD>
+// LDS image of 64 keys of a bf16 K or V: [64][head_dim], 16-byte pieces permuted within a row so that the
+// reads below hit different banks: K is read 16 or 32 keys at one column, V 4 or 8 keys x 32 bytes.
+template <int HD>
 struct Tile {
-    using T = typename PrecT<P>::T;
-    static constexpr int VEC = PrecT<P>::VEC;
-    static constexpr int ROWB = HD * (int)sizeof(T);  // bytes of a key
-    static constexpr int NC = ROWB / 16;              // 16-byte pieces of a key
+    static constexpr int ROWB = HD * 2;       // bytes of a key
+    static constexpr int NC = ROWB / 16;      // 16-byte pieces of a key
     static constexpr int BYTES = kKeys * ROWB;
-    static constexpr int KIB = BYTES / 1024;          // wave loads of a tile
-    static constexpr int RPK = 1024 / ROWB;           // keys per wave load (1..16)
+    static constexpr int KIB = BYTES / 1024;  // wave loads of a tile
+    static constexpr int RPK = 1024 / ROWB;   // keys per wave load (2..16)
     static_assert(RPK >= 1 && RPK <= 16 && NC >= 4, "a wave load stays within 16 keys");
     __device__ static int kswz(int key) { return NC >= 16 ? key & 15 : (key / (16 / NC)) & (NC - 1); }
     __device__ static int vswz(int key) {
-        if constexpr (P == Prec::BF16) {
-            constexpr int NP = HD / 16;  // 32-byte pairs
-            return 2 * (NP >= 8 ? key & 7 : (key / (8 / NP)) & (NP - 1));
-        } else {
-            constexpr int NB = HD / 16;  // 64-byte blocks
-            return NB >= 4 ? 4 * ((key >> 2) & 3) : 4 * ((key >> 2) & (NB - 1));
-        }
+        constexpr int NP = HD / 16;  // 32-byte pairs
+        return 2 * (NP >= 8 ? key & 7 : (key / (8 / NP)) & (NP - 1));
     }
 };
 
@@ -69,23 +68,6 @@ __device__ __forceinline__ void merge_weights(float &M, float Ms, float &w, floa
     M = Mn;
 }
 __device__ __forceinline__ float merge_value(float x, float xs, float w, float ws) { return __builtin_fmaf(xs, ws, x * w); }
-
-// Scores of a chunk for 16 rows: st[kt][v] = S^T[key 16 kt + 4 g + v][row r16], from K in LDS.
-template <Prec P, int HD>
-__device__ __forceinline__ void chunk_scores(const uint8_t *K, const u32x4 (&q)[HD / PrecT<P>::KSTEP], int lane, f32x4 (&st)[4]) {
-    using TL = Tile<P, HD>;
-    constexpr int NKK = HD / PrecT<P>::KSTEP;
-    const int g = lane >> 4, r16 = lane & 15;
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
-        const int key = 16 * kt + r16;
-        st[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < NKK; ++kk)
-            st[kt] = mfma_kstep<P>(*reinterpret_cast<const u32x4 *>(K + key * TL::ROWB + ((4 * kk + g) ^ TL::kswz(key)) * 16),
-                                   q[kk], st[kt]);
-    }
-}
 
 // Scores to probabilities: keys past qpos (relative to the chunk's first key) are out. mx: the row's
 // maximum (-inf: it sees no key), l: its sum.
@@ -115,31 +97,40 @@ __device__ __forceinline__ void chunk_softmax(f32x4 (&st)[4], int qpos, float sc
     l += __shfl_xor(l, 32);
 }
 
-// The V operand of 16 columns: vb[x] holds the keys of the probabilities' registers. bf16: x = 0, 1,
-// keys 32 x + 4 g + (0..3) and 32 x + 16 + 4 g + (0..3); fp32: x = 0..3, keys 16 x + 4 g + (0..3).
+// Columns of the output tile: MFMA row r of tile dt is column vcol(dt, r). bf16: 16 dt + r. fp32 values
+// come straight from memory, a lane's load holding W consecutive columns, one for each of W tiles.
 template <Prec P, int HD>
-__device__ __forceinline__ void v_operand(const uint8_t *V, int dt, int lane, u32x4 (&vb)[P == Prec::BF16 ? 2 : 4]) {
-    using TL = Tile<P, HD>;
+struct Cols {
+    static constexpr int W = P == Prec::BF16 ? 1 : (HD >= 64 ? 4 : HD / 16);
+    __device__ static int vcol(int dt, int r) { return dt / W * 16 * W + r * W + dt % W; }
+};
+
+// W consecutive words.
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&x)[W], const float *src) {
+    if constexpr (W == 4)
+        *reinterpret_cast<u32x4 *>(x) = *reinterpret_cast<const u32x4 *>(src);
+    else if constexpr (W == 2)
+        *reinterpret_cast<u32x2 *>(x) = *reinterpret_cast<const u32x2 *>(src);
+    else
+        x[0] = *reinterpret_cast<const uint32_t *>(src);
+}
+
+// The V operand of one output tile: vb[x] holds the keys of the probabilities' registers (bf16: x = 0, 1, keys
+// 32 x + 4 g + (0..3) and 32 x + 16 + 4 g + (0..3)), from LDS.
+template <int HD>
+__device__ __forceinline__ void v_operand(const uint8_t *V, int dt, int lane, u32x4 (&vb)[2]) {
+    using TL = Tile<HD>;
     const int g = lane >> 4, r16 = lane & 15;
-    if constexpr (P == Prec::BF16) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            u32x2 h[2];
+    for (int x = 0; x < 2; ++x) {
+        u32x2 h[2];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const int key = 32 * x + 16 * y + 4 * g + (r16 >> 2), c = 2 * dt + ((r16 & 3) >> 1);
-                h[y] = read_tr(V + key * TL::ROWB + (c ^ TL::vswz(key)) * 16 + (r16 & 1) * 8);
-            }
-            vb[x] = u32x4{h[0][0], h[0][1], h[1][0], h[1][1]};
+        for (int y = 0; y < 2; ++y) {
+            const int key = 4 * g + (r16 >> 2), c = 2 * dt + ((r16 & 3) >> 1);  // of 16 keys, whose permutations repeat
+            h[y] = read_tr(V + key * TL::ROWB + (c ^ TL::vswz(key)) * 16 + (r16 & 1) * 8 + (32 * x + 16 * y) * TL::ROWB);
         }
-    } else {
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const int key = 16 * x + 4 * g + y, c = 4 * dt + (r16 >> 2);
-                vb[x][y] = *reinterpret_cast<const uint32_t *>(V + key * TL::ROWB + (c ^ TL::vswz(key)) * 16 + (r16 & 3) * 4);
-            }
+        vb[x] = u32x4{h[0][0], h[0][1], h[1][0], h[1][1]};
     }
 }
 
@@ -182,267 +173,349 @@ __device__ __forceinline__ void weight_operand(const f32x4 (&st)[4], u32x4 (&pb)
     }
 }
 
-// Operand elements that are NaN or infinite, as (nan, +inf, -inf) indicators (1.0 / 0.0) and the
-// operand without them.
-template <Prec P, int N>
-__device__ __forceinline__ void split_nonfinite(u32x4 (&vb)[N], u32x4 (&ind)[3][N]) {
-    constexpr bool B = P == Prec::BF16;
-    constexpr uint32_t ONE = B ? 0x3f80u : 0x3f800000u, INF = B ? 0x7f80u : 0x7f800000u, SIGN = B ? 0x8000u : 0x80000000u;
+// Position of a unit's row.
+__device__ __forceinline__ int position_of(const PagedUnit &u, int row, int group) { return u.ctx + row / group; }
+
+// Four columns of a row's output, and with the first its log sum of exponentials.
+template <Prec P>
+__device__ __forceinline__ void store_row(const PagedAttnParams &p, int r0, int row, int h, int col, f32x4 o, float M, float l) {
+    using T = typename PrecT<P>::T;
+    const int token = row / p.group, head = h * p.group + row % p.group;
+    T *out = reinterpret_cast<T *>(p.out) + (size_t)(r0 + token) * p.out_stride + head * p.hd + col;
+    alignas(16) T x[4];
 #pragma unroll
-    for (int x = 0; x < N; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t out[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int half = 0; half < (B ? 2 : 1); ++half) {
-                const uint32_t e = B ? (vb[x][i] >> (16 * half)) & 0xffffu : vb[x][i], mag = e & ~SIGN;
-                const int sh = 16 * half;
-                out[0] |= (mag > INF ? ONE : 0u) << sh;
-                out[1] |= (e == INF ? ONE : 0u) << sh;
-                out[2] |= (e == (INF | SIGN) ? ONE : 0u) << sh;
-                out[3] |= (mag >= INF ? 0u : e) << sh;
-            }
-            ind[0][x][i] = out[0];
-            ind[1][x][i] = out[1];
-            ind[2][x][i] = out[2];
-            vb[x][i] = out[3];
-        }
+    for (int e = 0; e < 4; ++e) x[e] = to_elem<P>(o[e] / l);
+    if constexpr (P == Prec::BF16)
+        *reinterpret_cast<u32x2 *>(out) = *reinterpret_cast<const u32x2 *>(x);
+    else
+        *reinterpret_cast<u32x4 *>(out) = *reinterpret_cast<const u32x4 *>(x);
+    if (p.lse && col == 0) p.lse[(size_t)(r0 + token) * p.n_heads + head] = (M + log2f(l)) * kLn2;
 }
 
-// Unnormalised output of a chunk for 16 rows: o[dt][e] = O^T[16 dt + 4 g + e][row r16].
-//
-// A weight of 0 does not silence an infinite or NaN value in the product, and a weight's lo plane may turn
-// an infinity into a NaN. Both leave a NaN in some output, so outputs without one are right as they are;
-// behind one (rare) the values that are not finite are taken out of the operand, and each row gets what
-// those that it sees make of it: NaN for a NaN or an infinity of weight 0 (as 0 x inf is), the infinity
-// otherwise.
-template <Prec P, int HD>
-__device__ __forceinline__ void chunk_output(const uint8_t *V, const f32x4 (&st)[4], int qpos, int lane, f32x4 (&o)[HD / 16]) {
-    constexpr int N = P == Prec::BF16 ? 2 : 4, NPL = PrecT<P>::PLANES;
-    u32x4 pb[NPL][N];
-    weight_operand<P>(st, pb);
-    float sum = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < HD / 16; ++dt) {
-        u32x4 vb[N];
-        v_operand<P, HD>(V, dt, lane, vb);
-        o[dt] = v_product<P>(vb, pb);
-        sum += (o[dt][0] + o[dt][1]) + (o[dt][2] + o[dt][3]);
+// A unit, requested with the words that say whether the call is the plan's: one round trip.
+template <bool TILES>
+__device__ __forceinline__ bool next_unit(const PagedAttnParams &p, int i, int cap, PagedUnit &u, int &count) {
+    const int32_t *st = p.bk.status;
+    const int R = st[PS_ROWS], n = st[TILES ? PS_TILES : PS_UNITS], br = st[PS_BOUND_ROWS], bn = st[PS_BOUND_NEW],
+              bl = st[PS_BOUND_LEN];
+    const PagedUnit *list = TILES ? p.bk.tiles : p.bk.units;
+    u = list[min(i, cap - 1)];
+    request_together(R, n, br, bn, bl, u.slot, u.ctx, u.m, u.r0, u.row, u.k0, u.k1, u.part);
+    if (R > 0 && (br != p.rows || bn != p.max_new || bl != p.max_len)) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.bk.status[PS_LATE] = 1;
+        return false;
     }
-    if (!__any(sum != sum)) return;
-    const int g = lane >> 4;
-    f32x4 seen[4], pos[4], zero[4];
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const bool vis = 16 * kt + 4 * g + v <= qpos;
-            seen[kt][v] = vis ? 1.0f : 0.0f;
-            pos[kt][v] = vis && st[kt][v] > 0.0f ? 1.0f : 0.0f;
-            zero[kt][v] = vis && st[kt][v] == 0.0f ? 1.0f : 0.0f;
-        }
-    u32x4 sb[1][N], pp[1][N], zb[1][N];
-    weight_operand<P>(seen, sb);
-    weight_operand<P>(pos, pp);
-    weight_operand<P>(zero, zb);
-#pragma unroll
-    for (int dt = 0; dt < HD / 16; ++dt) {
-        u32x4 vb[N], ind[3][N];
-        v_operand<P, HD>(V, dt, lane, vb);
-        split_nonfinite<P>(vb, ind);
-        const f32x4 nan = v_product<P>(ind[0], sb), up = v_product<P>(ind[1], pp), down = v_product<P>(ind[2], pp),
-                    z0 = v_product<P>(ind[1], zb), z1 = v_product<P>(ind[2], zb);
-        o[dt] = v_product<P>(vb, pb);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (nan[e] > 0.f || z0[e] > 0.f || z1[e] > 0.f)
-                o[dt][e] = NAN;
-            else
-                o[dt][e] += (up[e] > 0.f ? INFINITY : 0.f) + (down[e] > 0.f ? -INFINITY : 0.f);
-        }
-    }
-}
-
-// What a workgroup knows of its unit.
-struct Unit {
-    int slot, ctx, m, r0;  // the request's entry
-    int rb;                // first row of the block, in rows x heads of the group
-    int rows;              // rows of the block
-    int span0, span1;      // spans of keys
-    int part;              // first partial row (-1: none)
-};
-
-// Row r of a request's rows x heads: token r / group, head r % group of the group.
-__device__ __forceinline__ Unit unit_of(const PagedAttnParams &p, int4 u) {
-    const int4 e = p.bk.ent[u.x];
-    Unit t;
-    t.slot = e.x;
-    t.ctx = e.y;
-    t.m = e.z;
-    t.r0 = e.w;
-    t.rb = u.y * kPagedBlockRows;
-    t.rows = min(kPagedBlockRows, t.m * p.group - t.rb);
-    const int last = t.ctx + (t.rb + t.rows - 1) / p.group;
-    t.span0 = u.z < 0 ? 0 : u.z;
-    t.span1 = u.z < 0 ? last / kPagedSpanKeys + 1 : u.z + 1;
-    t.part = u.w;
-    return t;
+    count = n;
+    return R > 0 && i < n;
 }
 
 }  // namespace
 
-// Two buffers of a chunk's K and V (at most 128 of a CU's 160 KiB).
-template <Prec P, int HD>
-constexpr int paged_rows_lds() {
-    return 4 * Tile<P, HD>::BYTES;
+// LDS bytes of a wave of the span kernel: the chunk's V (bf16), then in its place the chunk's states of up
+// to 16 RG rows (padded rows, so that the writes of 16 rows hit different banks).
+template <Prec P, int HD, int RG>
+constexpr int span_wave_lds() {
+    constexpr int state = 16 * RG * (HD * 4 + 16), v = P == Prec::BF16 ? kKeys * HD * 2 : 0;
+    return state > v ? state : v;
 }
 
-// Workgroup: one key head of a unit, 4 waves x 16 rows; chunks of K and V come into LDS by DMA, once for
-// all waves, one chunk ahead. Workgroups take units in turn.
-template <Prec P, int HD>
-__global__ __launch_bounds__(4 * kWave) void paged_rows_kernel(PagedAttnParams p) {
+// One chunk of the span kernel, by one wave: the states of its NRG groups of 16 rows into s_mine ([row][column])
+// and s_m, s_l (this wave's rows). last_key: the request's last token; pages: its table.
+template <Prec P, int HD, int NRG>
+__device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const PagedUnit &u, int h, int rows, int key0, int last_key,
+                                           const int32_t *table, uint8_t *s_mine, float *s_m, float *s_l) {
     using PT = PrecT<P>;
     using T = typename PT::T;
-    using TL = Tile<P, HD>;
-    constexpr int NKK = HD / PT::KSTEP, NDT = HD / 16;
-    extern __shared__ u32x4 s_raw[];
-    uint8_t *s_kv = reinterpret_cast<uint8_t *>(s_raw);  // [buffer][K, V]
-    if (bounded_rows(p.bk, p.rows, p.max_new, p.max_len) == 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = lane >> 4, r16 = lane & 15, shift = p.bk.page_shift;
-    const int work = p.bk.status[PS_UNITS] * p.n_kv;
-    for (int idx = blockIdx.x; idx < work; idx += gridDim.x) {
-        const int h = idx % p.n_kv;
-        const Unit t = unit_of(p, p.bk.units[idx / p.n_kv]);
-        const int32_t *table = p.bk.table + (size_t)t.slot * p.bk.max_pages;
-        const int kvlen = t.ctx + t.m, last_tile = (kvlen - 1) >> 4;
-        const int blast = t.ctx + (t.rb + t.rows - 1) / p.group;  // the block's last position
-        const int c0 = t.span0 * kSpanChunks, c1 = min(t.span1 * kSpanChunks, blast / kKeys + 1);
-        const bool live = 16 * w < t.rows;  // uniform over the wave
-        const int rr = min(t.rb + 16 * w + r16, t.rb + t.rows - 1);  // rows past the block: its last one, not stored
-        const int token = rr / p.group, head = h * p.group + rr % p.group;
-        const int qpos = t.ctx + token;
-        // page ids of the 64 tiles of 16 keys from tile 64 j on, one per lane
-        auto page_ids = [&](int j) { return table[(min(64 * j + lane, last_tile) << 4) >> shift]; };
-        int pj = c0 / 16, pg = page_ids(pj), pg_next = page_ids(pj + 1);
-        auto issue = [&](int c, int buf) {
-            if (c / 16 != pj) {
-                pj = c / 16;
-                pg = pg_next;
-                pg_next = page_ids(pj + 1);
-            }
+    constexpr bool B = P == Prec::BF16;
+    constexpr int KSTEP = PT::KSTEP, VEC = PT::VEC, NKK = HD / KSTEP, NDT = HD / 16, N = B ? 2 : 4, NPL = PT::PLANES;
+    constexpr int W = Cols<P, HD>::W, SROW = HD + 4;  // floats of a state row
+    const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15, shift = p.bk.page_shift;
+    // pages of the four tiles of 16 keys (tiles past the request's end: its last one)
+    const int tl = min(key0 + 16 * (lane & 3), last_key) >> 4, pg = table[(tl << 4) >> shift];
+    // this lane's rows (those past the block: its last one, not stored)
+    int qpos[NRG];
+    u32x4 q[NRG][NKK];
 #pragma unroll
-            for (int i = 0; i < 2 * TL::KIB / 4; ++i) {
-                const int blk = w + 4 * i, isv = blk >= TL::KIB, kb = isv ? blk - TL::KIB : blk;
-                const int key = kb * TL::RPK + lane / (kWave / TL::RPK);  // within the chunk
-                const int tile = min(4 * c + kb * TL::RPK / 16, last_tile);
-                const int page = __builtin_amdgcn_readlane(pg, (4 * c + kb * TL::RPK / 16) & 63);
-                const int off = ((tile << 4) & ((1 << shift) - 1)) + (key & 15);
-                const int piece = (lane % TL::NC) ^ (isv ? TL::vswz(key) : TL::kswz(key));
-                const uint8_t *src = reinterpret_cast<const uint8_t *>(isv ? p.v_pages : p.k_pages) +
-                                     ((((size_t)page * p.n_kv + h) << shift) + off) * TL::ROWB + piece * 16;
-                __builtin_amdgcn_global_load_lds(
-                    static_cast<const void *>(src),
-                    (__attribute__((address_space(3))) void *)(s_kv + (size_t)buf * 2 * TL::BYTES + blk * 1024), 16, 0, 0);
-            }
-        };
-        __syncthreads();  // the unit before is done with the buffers
-        issue(c0, 0);
-        u32x4 q[NKK];
-        const T *qrow = reinterpret_cast<const T *>(p.q) + (size_t)(t.r0 + token) * p.q_stride + head * HD;
+    for (int rg = 0; rg < NRG; ++rg) {
+        const int r = u.row + min(16 * rg + r16, rows - 1), token = r / p.group, head = h * p.group + r % p.group;
+        qpos[rg] = u.ctx + token - key0;
+        const T *qrow = reinterpret_cast<const T *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + g * VEC;
 #pragma unroll
-        for (int kk = 0; kk < NKK; ++kk) q[kk] = *reinterpret_cast<const u32x4 *>(qrow + kk * PT::KSTEP + g * PT::VEC);
-        float M = -INFINITY, l = 0.f, Mr = -INFINITY, lr = 0.f;  // the span's state, the row's
-        f32x4 o[NDT], orow[NDT];
+        for (int kk = 0; kk < NKK; ++kk) q[rg][kk] = *reinterpret_cast<const u32x4 *>(qrow + kk * KSTEP);
+    }
+    size_t at[4];  // first element of each tile
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) o[dt] = orow[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int c = c0; c < c1; ++c) {
-            const int buf = (c - c0) & 1;
-            wait_vm_lds<0>();
-            barrier_no_fence();  // every wave's pieces of the chunk have landed
-            if (c + 1 < c1) issue(c + 1, buf ^ 1);
-            uint8_t *K = s_kv + (size_t)buf * 2 * TL::BYTES, *V = K + TL::BYTES;
-            if ((c + 1) * kKeys > kvlen) {  // values behind the request's last token: whatever the page holds
-                const int from = kvlen - c * kKeys;
-                for (int i = from * TL::NC + tid; i < kKeys * TL::NC; i += 4 * kWave)
-                    reinterpret_cast<u32x4 *>(V)[i] = u32x4{0u, 0u, 0u, 0u};
-                wait_vm_lds<63>();
-                barrier_no_fence();
-            }
-            if (live && c * kKeys <= t.ctx + min(t.rb + 16 * w + 15, t.rb + t.rows - 1) / p.group) {
-                f32x4 st[4], oc[NDT];
-                float mx, lc, wo, wc;
-                chunk_scores<P, HD>(K, q, lane, st);
-                chunk_softmax(st, qpos - c * kKeys, p.scale_log2, lane, mx, lc);
-                chunk_output<P, HD>(V, st, qpos - c * kKeys, lane, oc);
-                merge_weights(M, mx, wo, wc);
-                l = merge_value(l, lc, wo, wc);
+    for (int kt = 0; kt < 4; ++kt) {
+        const int tile = __builtin_amdgcn_readlane(tl, kt), page = __builtin_amdgcn_readlane(pg, kt);
+        at[kt] = ((((size_t)page * p.n_kv + h) << shift) + ((tile << 4) & ((1 << shift) - 1))) * HD;
+    }
+    u32x4 kf[4][NKK];
 #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
+    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[dt][e] = merge_value(o[dt][e], oc[dt][e], wo, wc);
-            }
-            if (c + 1 == c1 || (c + 1) % kSpanChunks == 0) {  // the span's end
-                float w0, w1;
-                merge_weights(Mr, M, w0, w1);
-                lr = merge_value(lr, l, w0, w1);
+        for (int kk = 0; kk < NKK; ++kk)
+            kf[kt][kk] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(p.k_pages) + at[kt] + r16 * HD + kk * KSTEP +
+                                                          g * VEC);
+    const int valid = last_key - key0 + 1;  // keys of the chunk that the request has
+    if constexpr (B) {
+        using TL = Tile<HD>;
 #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) orow[dt][e] = merge_value(orow[dt][e], o[dt][e], w0, w1);
-                M = -INFINITY;
-                l = 0.f;
-#pragma unroll
-                for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
+        for (int i = 0; i < TL::KIB; ++i) {
+            const int key = i * TL::RPK + lane / (kWave / TL::RPK), piece = (lane % TL::NC) ^ TL::vswz(key);
+            const T *src = reinterpret_cast<const T *>(p.v_pages) + at[i * TL::RPK / 16] + (key & 15) * HD + piece * 8;
+            __builtin_amdgcn_global_load_lds(static_cast<const void *>(src),
+                                             (__attribute__((address_space(3))) void *)(s_mine + i * 1024), 16, 0, 0);
         }
-        const bool stored = 16 * w + r16 < t.rows;
-        if (stored && t.part >= 0) {
-            const size_t pr = (size_t)(t.part + 16 * w + r16) * p.n_kv + h;
+    }
+    u32x4 pb[NRG][NPL][N];
+    float mx[NRG], lc[NRG];
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + 16 * dt + 4 * g) = orow[dt];
-            if (g == 0) {
-                p.part_m[pr] = Mr;
-                p.part_l[pr] = lr;
+    for (int rg = 0; rg < NRG; ++rg) {
+        f32x4 st[4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            st[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) st[kt] = mfma_kstep<P>(kf[kt][kk], q[rg][kk], st[kt]);
+        }
+        chunk_softmax(st, qpos[rg], p.scale_log2, lane, mx[rg], lc[rg]);
+        weight_operand<P>(st, pb[rg]);
+    }
+    if constexpr (B) {
+        wait_vm_lds<0>();
+        if (valid < kKeys)  // values behind the request's last token, whatever the page holds there
+            for (int i = valid * Tile<HD>::NC + lane; i < kKeys * Tile<HD>::NC; i += kWave)
+                reinterpret_cast<u32x4 *>(s_mine)[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+    // A weight of 0 does not silence an infinite or NaN value in the product, and a weight's lo plane may
+    // turn an infinity into a NaN. Both leave a NaN in some output, so outputs without one are right. Else
+    // (rare) the values that are not finite are taken out, the product is formed again, and what the rows
+    // that see them get from them is added behind it: a sum per row and column, as a class of two bits (0,
+    // +inf, -inf, NaN), 32 rows a word, of this lane's columns lane, lane + 64, ...
+    constexpr int NCOL = (HD + kWave - 1) / kWave;
+    uint64_t cls[NCOL];
+    bool taken = false;  // uniform over the wave
+    // V operands of the W tiles from tile dt on
+    auto operand = [&](int dt, u32x4(&vb)[W][N]) {
+        if constexpr (B) {
+            v_operand<HD>(s_mine, dt, lane, vb[0]);
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    alignas(4 * W) uint32_t x[W];
+                    load_words<W>(x, reinterpret_cast<const float *>(p.v_pages) + at[kt] + (4 * g + v) * HD +
+                                         Cols<P, HD>::vcol(dt, r16));
+#pragma unroll
+                    for (int y = 0; y < W; ++y) {
+                        const bool use = 16 * kt + 4 * g + v < valid && !(taken && (x[y] & 0x7f800000u) == 0x7f800000u);
+                        vb[y][kt][v] = use ? x[y] : 0u;
+                    }
+                }
+        }
+    };
+    f32x4 oc[NRG][NDT];
+    while (true) {
+        float sum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < NDT; dt += W) {
+            u32x4 vb[W][N];
+            operand(dt, vb);
+#pragma unroll
+            for (int y = 0; y < W; ++y)
+#pragma unroll
+                for (int rg = 0; rg < NRG; ++rg) {
+                    const f32x4 x = v_product<P>(vb[y], pb[rg]);
+                    oc[rg][dt + y] = x;
+                    sum += (x[0] + x[1]) + (x[2] + x[3]);
+                }
+        }
+        if (taken || !__any(sum != sum)) break;
+        taken = true;
+#pragma unroll 1
+        for (int j = 0; j < NCOL; ++j) {
+            const int col = lane + j * kWave;
+            uint64_t bits = 0;
+            float acc = 0.f;
+            int key = 0;
+#pragma unroll 1
+            for (int r = 0; r < 16 * NRG; ++r) {  // the rows' positions do not fall
+                const int last = min(min(__builtin_amdgcn_readlane(r < 16 ? qpos[0] : qpos[NRG - 1], r & 15), valid - 1), kKeys - 1);
+                for (; key <= last; ++key) {
+                    if (col >= HD) continue;
+                    uint32_t x;
+                    if constexpr (B) {
+                        using TL = Tile<HD>;
+                        uint16_t *v = reinterpret_cast<uint16_t *>(s_mine + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
+                        x = (uint32_t)*v << 16;
+                        if ((x & 0x7f800000u) == 0x7f800000u) *v = 0;
+                    } else {
+                        const size_t row = key < 16 ? at[0] : key < 32 ? at[1] : key < 48 ? at[2] : at[3];
+                        x = __float_as_uint(reinterpret_cast<const float *>(p.v_pages)[row + (key & 15) * HD + col]);
+                    }
+                    if ((x & 0x7f800000u) == 0x7f800000u) acc += __uint_as_float(x);
+                }
+                const uint64_t c = acc != acc ? 3 : acc == INFINITY ? 1 : acc == -INFINITY ? 2 : 0;
+                bits |= c << (2 * r);
             }
-        } else if (stored) {
-            T *out = reinterpret_cast<T *>(p.out) + (size_t)(t.r0 + token) * p.out_stride + head * HD;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) {
-                alignas(16) T x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = to_elem<P>(orow[dt][e] / lr);
-                if constexpr (P == Prec::BF16)
-                    *reinterpret_cast<u32x2 *>(out + 16 * dt + 4 * g) = *reinterpret_cast<const u32x2 *>(x);
-                else
-                    *reinterpret_cast<u32x4 *>(out + 16 * dt + 4 * g) = *reinterpret_cast<const u32x4 *>(x);
+            if constexpr (B) {  // what no row sees
+                for (; key < kKeys && col < HD; ++key) {
+                    using TL = Tile<HD>;
+                    uint16_t *v = reinterpret_cast<uint16_t *>(s_mine + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
+                    if ((*v & 0x7f80) == 0x7f80) *v = 0;
+                }
             }
-            if (p.lse && g == 0)
-                p.lse[(size_t)(t.r0 + token) * p.n_heads + head] = (Mr + log2f(lr)) * 0.6931471805599453f;
+#pragma unroll
+            for (int i = 0; i < NCOL; ++i)
+                if (i == j) cls[i] = bits;
+        }
+    }
+    // V has been read: the states in its place
+#pragma unroll
+    for (int rg = 0; rg < NRG; ++rg) {
+        float *s_o = reinterpret_cast<float *>(s_mine) + (16 * rg + r16) * SROW;
+        if constexpr (W == 1) {
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) *reinterpret_cast<f32x4 *>(s_o + 16 * dt + 4 * g) = oc[rg][dt];
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s_o[Cols<P, HD>::vcol(dt, 4 * g + e)] = oc[rg][dt][e];
+        }
+        if (g == 0) {
+            s_m[16 * rg + r16] = mx[rg];
+            s_l[16 * rg + r16] = lc[rg];
+        }
+    }
+    if (taken) {
+#pragma unroll
+        for (int j = 0; j < NCOL; ++j) {
+            const int col = lane + j * kWave;
+#pragma unroll 1
+            for (int r = 0; r < 16 * NRG; ++r) {
+                const int c = (int)(cls[j] >> (2 * r)) & 3;
+                if (col < HD && c != 0)
+                    reinterpret_cast<float *>(s_mine)[r * SROW + col] += c == 1 ? INFINITY : c == 2 ? -INFINITY : NAN;
+            }
         }
     }
 }
 
-// Joins the spans of split row blocks, in position order. A workgroup takes some rows of one key
-// head of an item, a lane four columns of a row.
+// Few rows. Workgroup: a block of up to 16 RG rows of one key head and one span of its keys (or every span,
+// one after another). A wave takes a chunk of 64 keys, K straight into registers in operand order, V through
+// LDS (bf16: transposing reads) or straight (fp32); then the workgroup merges the chunks' states. Loads of
+// a workgroup are all in flight at once: 256 KiB at head_dim 128.
+template <Prec P, int HD, int NW, int RG>
+__global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams p, int cap_units) {
+    constexpr int REGION = span_wave_lds<P, HD, RG>(), SROW = HD + 4, ROWS = 16 * RG;
+    constexpr int ITEMS = (ROWS * HD / 4 + NW * kWave - 1) / (NW * kWave);
+    extern __shared__ u32x4 s_raw[];
+    uint8_t *s_all = reinterpret_cast<uint8_t *>(s_raw);
+    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint8_t *s_mine = s_all + (size_t)w * REGION;
+    int count = 0;
+    PagedUnit u;
+    for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
+        const int h = idx % p.n_kv;
+        const int rows = min(ROWS, u.m * p.group - u.row);
+        const int blast = position_of(u, u.row + rows - 1, p.group);  // the block's last position
+        const int last_key = u.ctx + u.m - 1;
+        const int s0 = u.k0 < 0 ? 0 : u.k0, s1 = min(u.k0 < 0 ? INT32_MAX - 1 : u.k0, blast / kPagedSpanKeys) + 1;
+        const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
+        // the states of this thread's (row, four columns) items: the span's, the row's
+        float Mr[ITEMS], lr[ITEMS];
+        f32x4 orow[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) Mr[i] = -INFINITY, lr[i] = 0.f, orow[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = s0; s < s1; ++s) {
+            float M[ITEMS], l[ITEMS];
+            f32x4 o[ITEMS];
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) M[i] = -INFINITY, l[i] = 0.f, o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int c0 = s * kSpanChunks; c0 < (s + 1) * kSpanChunks && c0 * kKeys <= blast; c0 += NW) {
+                const int key0 = (c0 + w) * kKeys;
+                if (key0 <= blast) {  // uniform over the wave
+                    if (RG == 1 || rows <= 16)
+                        span_chunk<P, HD, 1>(p, u, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                    else
+                        span_chunk<P, HD, RG>(p, u, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
+                    if (row >= rows) break;
+                    const int pos = position_of(u, u.row + row, p.group);
+                    for (int k = 0; k < NW && (c0 + k) * kKeys <= pos; ++k) {
+                        const f32x4 oc = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_all + (size_t)k * REGION) +
+                                                                          row * SROW + col);
+                        float wo, wc;
+                        merge_weights(M[i], s_m[k][row], wo, wc);
+                        l[i] = merge_value(l[i], s_l[k][row], wo, wc);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[i][e] = merge_value(o[i][e], oc[e], wo, wc);
+                    }
+                }
+                __syncthreads();  // before the next chunks come into the regions
+            }
+            if (u.part >= 0) {  // one span: its state as it is
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) Mr[i] = M[i], lr[i] = l[i], orow[i] = o[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int row = (tid + i * NW * kWave) / (HD / 4);
+                    if (s * kPagedSpanKeys > position_of(u, u.row + min(row, rows - 1), p.group)) continue;
+                    float w0, w1;
+                    merge_weights(Mr[i], M[i], w0, w1);
+                    lr[i] = merge_value(lr[i], l[i], w0, w1);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) orow[i][e] = merge_value(orow[i][e], o[i][e], w0, w1);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
+            if (row >= rows) break;
+            if (u.part >= 0) {
+                const size_t pr = (size_t)(u.part + row) * p.n_kv + h;
+                *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = orow[i];
+                if (col == 0) {
+                    p.part_m[pr] = Mr[i];
+                    p.part_l[pr] = lr[i];
+                }
+            } else {
+                store_row<P>(p, u.r0, u.row + row, h, col, orow[i], Mr[i], lr[i]);
+            }
+        }
+    }
+}
+
+// Joins the partial states of split row blocks, in position order. Workgroup: some rows of one key head of
+// an item, a thread per four columns of a row.
 template <Prec P, int HD>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
-    using T = typename PrecT<P>::T;
-    constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedBlockRows + RPW - 1) / RPW;
-    if (bounded_rows(p.bk, p.rows, p.max_new, p.max_len) == 0) return;
-    const int work = p.bk.status[PS_ITEMS] * p.n_kv * NG;
-    const int col = threadIdx.x % LPR * 4;
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int cap_items) {
+    constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedItemRows + RPW - 1) / RPW;
+    const int32_t *st = p.bk.status;
+    const int R = st[PS_ROWS], n = st[PS_ITEMS], br = st[PS_BOUND_ROWS], bn = st[PS_BOUND_NEW], bl = st[PS_BOUND_LEN];
+    PagedItem it = p.bk.items[min((int)blockIdx.x / (p.n_kv * NG), cap_items - 1)];
+    request_together(R, n, br, bn, bl, it.ctx, it.m, it.r0, it.row, it.part, it.stride, it.count);
+    if (R == 0 || br != p.rows || bn != p.max_new || bl != p.max_len) return;
+    const int col = threadIdx.x % LPR * 4, work = n * p.n_kv * NG;
     for (int idx = blockIdx.x; idx < work; idx += gridDim.x) {
-        const int4 it = p.bk.items[idx / (p.n_kv * NG)];
+        if (idx != (int)blockIdx.x) it = p.bk.items[idx / (p.n_kv * NG)];
         const int h = idx % p.n_kv, row = idx / p.n_kv % NG * RPW + threadIdx.x / LPR;
-        const int4 e = p.bk.ent[it.x];
-        const int rb = it.y * kPagedBlockRows, rows = min(kPagedBlockRows, e.z * p.group - rb);
-        if (row >= rows) continue;
+        if (row >= min(kPagedItemRows, it.m * p.group - it.row)) continue;
+        const int count = it.count > 0 ? it.count : (it.ctx + (it.row + row) / p.group) / kPagedSpanKeys + 1;
         float M = -INFINITY, l = 0.f;
         f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int s = 0; s < it.w; ++s) {
-            const size_t pr = (size_t)(it.z + s * rows + row) * p.n_kv + h;
+        for (int s = 0; s < count; ++s) {
+            const size_t pr = (size_t)(it.part + s * it.stride + row) * p.n_kv + h;
             const f32x4 os = *reinterpret_cast<const f32x4 *>(p.part_o + pr * HD + col);
             const float Ms = p.part_m[pr], ls = p.part_l[pr];
             float w0, w1;
@@ -451,50 +524,51 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = merge_value(o[i], os[i], w0, w1);
         }
-        const int token = (rb + row) / p.group, head = h * p.group + (rb + row) % p.group;
-        T *out = reinterpret_cast<T *>(p.out) + (size_t)(e.w + token) * p.out_stride + head * HD + col;
-        alignas(16) T x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = to_elem<P>(o[i] / l);
-        if constexpr (P == Prec::BF16)
-            *reinterpret_cast<u32x2 *>(out) = *reinterpret_cast<const u32x2 *>(x);
-        else
-            *reinterpret_cast<u32x4 *>(out) = *reinterpret_cast<const u32x4 *>(x);
-        if (p.lse && col == 0)
-            p.lse[(size_t)(e.w + token) * p.n_heads + head] = (M + log2f(l)) * 0.6931471805599453f;
+        store_row<P>(p, it.r0, it.row + row, h, col, o, M, l);
     }
 }
 
 namespace {
 
-template <Prec P, int HD>
-hipError_t launch_shape(int64_t units, bool split, const PagedAttnParams &p, hipStream_t s) {
-    constexpr int lds = paged_rows_lds<P, HD>();
-    const int per_cu = std::min(160 * 1024 / lds, 2);
-    const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, kCUs * per_cu));
-    hipLaunchKernelGGL((paged_rows_kernel<P, HD>), grid, dim3(4 * kWave), lds, s, p);
-    if (split) {
-        const int64_t join = std::min<int64_t>(units, kPagedSplitBelow) * p.n_kv * 16;
-        hipLaunchKernelGGL((paged_join_kernel<P, HD>), dim3((unsigned)std::min<int64_t>(join, 8 * kCUs)), dim3(256), 0, s, p);
+// NW: waves, as many chunks at a time; RG: groups of 16 rows of a block, as paged_block_rows() says.
+template <Prec P, int HD, int NW, int RG>
+hipError_t launch_spans(int64_t units, const PagedAttnParams &p, hipStream_t s) {
+    constexpr int lds = NW * span_wave_lds<P, HD, RG>();
+    static_assert(lds + NW * RG * 16 * 8 <= 160 * 1024, "the LDS of a CU");
+    static_assert(16 * RG == paged_block_rows(P == Prec::BF16, HD), "the plan's row blocks");
+    const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs));
+    hipLaunchKernelGGL((paged_span_kernel<P, HD, NW, RG>), grid, dim3(NW * kWave), lds, s, p, p.bk.cap_units);
+    return hipGetLastError();
+}
+
+template <Prec P, int HD, int NW, int RG>
+hipError_t launch_shape(int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
+    hipError_t e = launch_spans<P, HD, NW, RG>(units, p, s);
+    if (e != hipSuccess) return e;
+    if (join) {
+        const int64_t groups = (kPagedItemRows + 1024 / HD - 1) / (1024 / HD);
+        const int64_t work = std::min<int64_t>(units + 4 * tiles, p.bk.cap_items) * p.n_kv * groups;
+        hipLaunchKernelGGL((paged_join_kernel<P, HD>), dim3((unsigned)std::min<int64_t>(work, 8 * kCUs)), dim3(256), 0, s, p,
+                           p.bk.cap_items);
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attn(bool bf16, int64_t units, bool split, const PagedAttnParams &p, hipStream_t s) {
-    if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0) return hipErrorInvalidValue;
-    if (units == 0 || p.rows == 0) return hipSuccess;
+hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
+    if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0 || tiles < 0) return hipErrorInvalidValue;
+    if (units + tiles == 0 || p.rows == 0) return hipSuccess;
     if (bf16) {
-        if (p.hd == 32) return launch_shape<Prec::BF16, 32>(units, split, p, s);
-        if (p.hd == 64) return launch_shape<Prec::BF16, 64>(units, split, p, s);
-        if (p.hd == 128) return launch_shape<Prec::BF16, 128>(units, split, p, s);
-        if (p.hd == 256) return launch_shape<Prec::BF16, 256>(units, split, p, s);
+        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 4, 1>(units, tiles, join, p, s);
     } else {
-        if (p.hd == 16) return launch_shape<Prec::F32, 16>(units, split, p, s);
-        if (p.hd == 32) return launch_shape<Prec::F32, 32>(units, split, p, s);
-        if (p.hd == 64) return launch_shape<Prec::F32, 64>(units, split, p, s);
-        if (p.hd == 128) return launch_shape<Prec::F32, 128>(units, split, p, s);
+        if (p.hd == 16) return launch_shape<Prec::F32, 16, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::F32, 32, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::F32, 64, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::F32, 128, 8, 1>(units, tiles, join, p, s);
     }
     return hipErrorInvalidValue;
 }

@@ -24,7 +24,8 @@ struct cllm_paged {
     PagedBooks bk{};
     float *rcos = nullptr, *rsin = nullptr;  // null without rotation
     float *part_o = nullptr, *part_m = nullptr, *part_l = nullptr;
-    int cap_units = 0, cap_items = 0, cap_part = 0;
+    bool tiled = false;  // long chunks take tiles
+    int block_rows = 32, cap_part = 0;
     void *own = nullptr;  // library-allocated workspace
     bool planned = false, dead = false;
     int n = 0, rows = 0, max_new = 0, max_len = 0;  // the last plan's bounds
@@ -103,17 +104,22 @@ std::vector<Buf> buffers(cllm_paged *c) {
     bk.max_pages = (f.max_ctx + f.page_size - 1) / f.page_size;
     bk.n_pages = f.n_pages;
     bk.page_shift = __builtin_ctz((unsigned)f.page_size);
-    // Split row blocks are fewer than kPagedSplitBelow / n_kv; a block's spans are its request's, so
-    // requests of one block each have no more spans than the pool and one each. A plan that needs more
-    // (several blocks of a request over most of a large pool) is not split.
-    const int64_t blocks = (int64_t)f.max_rows * c->group / kPagedBlockRows + f.max_seqs;
-    const int64_t few = kPagedSplitBelow / f.n_kv_heads + 1;
+    // Attention units. Row blocks and tiles of any plan, unsplit; split row blocks are fewer than
+    // kPagedSplitBelow / n_kv, and their spans no more than the pool holds and one each (where requests
+    // have no more than kPagedFewRows rows; a plan that needs more is not split); split tiles are fewer than
+    // kPagedTileGroups / n_kv, in about that many ranges.
+    c->tiled = false;
+    c->block_rows = paged_block_rows(c->bf16, f.head_dim);
+    const int64_t nrows = (int64_t)f.max_rows * c->group, blocks = nrows / c->block_rows + f.max_seqs;
+    const int64_t tiles = c->tiled ? nrows / kPagedTileRows + f.max_seqs : 0;
+    const int64_t few = kPagedSplitBelow / f.n_kv_heads + 1, few_tiles = kPagedTileGroups / f.n_kv_heads + 1;
     const int64_t spans = (f.max_ctx + kPagedSpanKeys - 1) / kPagedSpanKeys;
     const int64_t split = std::min(std::min(few, blocks) * spans,
-                                   ((int64_t)f.n_pages * f.page_size + kPagedSpanKeys - 1) / kPagedSpanKeys + 2 * few);
-    c->cap_units = (int)std::max(blocks, split);
-    c->cap_items = (int)few;
-    c->cap_part = (int)std::min<int64_t>(split * kPagedBlockRows, INT32_MAX / 2);
+                                   kPagedFewRows / c->block_rows * (((int64_t)f.n_pages * f.page_size + kPagedSpanKeys - 1) / kPagedSpanKeys + few));
+    bk.cap_units = (int)std::max(blocks, split);
+    bk.cap_tiles = (int)(tiles + 2 * few_tiles);
+    bk.cap_items = (int)(few + 4 * few_tiles);
+    c->cap_part = (int)std::min<int64_t>(split * c->block_rows + 2 * few_tiles * kPagedTileRows, INT32_MAX / 2);
     auto P = [](auto **q) { return reinterpret_cast<void **>(q); };
     const size_t part = (size_t)c->cap_part * f.n_kv_heads;
     std::vector<Buf> b{
@@ -124,9 +130,9 @@ std::vector<Buf> buffers(cllm_paged *c) {
         {P(&bk.row_start), (size_t)(f.max_seqs + 1) * 4},
         {P(&bk.row_slot), (size_t)f.max_rows * 4},
         {P(&bk.row_pos), (size_t)f.max_rows * 4},
-        {P(&bk.ent), (size_t)f.max_seqs * sizeof(int4)},
-        {P(&bk.units), (size_t)c->cap_units * sizeof(int4)},
-        {P(&bk.items), (size_t)c->cap_items * sizeof(int4)},
+        {P(&bk.units), (size_t)bk.cap_units * sizeof(PagedUnit)},
+        {P(&bk.tiles), (size_t)bk.cap_tiles * sizeof(PagedUnit)},
+        {P(&bk.items), (size_t)bk.cap_items * sizeof(PagedItem)},
         {P(&c->part_o), part * f.head_dim * 4},
         {P(&c->part_m), part * 4},
         {P(&c->part_l), part * 4},
@@ -297,8 +303,8 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
     p.max_len = max_len;
     p.group = c->group;
     p.n_kv = c->cfg.n_kv_heads;
-    p.cap_units = c->cap_units;
-    p.cap_items = c->cap_items;
+    p.tiled = c->tiled;
+    p.block_rows = c->block_rows;
     p.cap_part = c->cap_part;
     HIPCHK(c, launch_paged_plan(p, c->stream));
     c->planned = true;
@@ -389,10 +395,14 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     const double sc = scale == 0.0f ? 1.0 / std::sqrt((double)f.head_dim) : (double)scale;
     p.scale_log2 = (float)(1.4426950408889634 * sc);
     // bounds of the launch: row blocks of the rows and requests, spans of the longest request
-    const int64_t per = ((int64_t)c->max_new * c->group + kPagedBlockRows - 1) / kPagedBlockRows;
-    const int64_t blocks = std::min(c->n * per, (int64_t)c->rows * c->group / kPagedBlockRows + c->n);
-    const int64_t spans = (c->max_len + kPagedSpanKeys - 1) / kPagedSpanKeys;
-    HIPCHK(c, launch_paged_attn(c->bf16, blocks * spans, spans > 1, p, c->stream));
+    auto pieces = [&](int64_t most, int rows) {  // of requests of at most `most` rows each
+        return std::min(c->n * ((most + rows - 1) / rows), (int64_t)c->rows * c->group / rows + c->n);
+    };
+    const int64_t most = (int64_t)c->max_new * c->group, spans = (c->max_len + kPagedSpanKeys - 1) / kPagedSpanKeys;
+    const int64_t units = pieces(c->tiled ? std::min<int64_t>(most, kPagedFewRows) : most, c->block_rows) * spans;
+    int64_t tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
+    if (tiles) tiles = std::min<int64_t>(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
+    HIPCHK(c, launch_paged_attn(c->bf16, units, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
 }
 
