@@ -495,6 +495,232 @@ __global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams 
     }
 }
 
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return (uint32_t)f2bf(a) | ((uint32_t)f2bf(b) << 16); }
+
+// LDS of the tile kernel: two buffers of a chunk's K and V, and the classes of values that are not finite.
+template <int HD>
+constexpr int tile_lds() {
+    return 4 * Tile<HD>::BYTES + kPagedTileRows / 16 * HD * 4;
+}
+
+// Long chunks (bf16). Workgroup: a tile of 128 rows of one key head and a range of its keys, 4 waves x 32
+// rows. Chunks of 64 keys of K and V come into LDS by DMA, once for all waves, one chunk ahead. Per chunk
+// and wave: S^T = K Q^T (32 keys x 32 rows a product), so that a lane holds half the keys of one row: the
+// softmax is lane-local but for one exchange, and the weights are the next product's operand as they lie;
+// O^T += V^T P^T with transposing reads of V. The weights are rounded to bf16 (half a step, 2^-9 of each
+// weight, of random sign: less than the output's own rounding), their sum is not. The reference of the
+// exponentials follows the running maximum only when that has grown by 2^8: weights are then at most 2^8
+// in place of 1, which neither type minds, and the output is rescaled rarely.
+template <int HD>
+__global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
+    using TL = Tile<HD>;
+    constexpr int NKK = HD / 16, NDT = HD / 32;
+    extern __shared__ u32x4 s_raw[];
+    uint8_t *s_kv = reinterpret_cast<uint8_t *>(s_raw);  // [buffer][K, V]
+    uint32_t *s_cls = reinterpret_cast<uint32_t *>(s_kv + 4 * TL::BYTES);  // [column][16 rows]
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r32 = lane & 31, hb = lane >> 5, shift = p.bk.page_shift;
+    const float scale = fabsf(p.scale_log2);
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;  // the scale's sign goes into the queries
+    int count = 0;
+    PagedUnit u;
+    for (int idx = blockIdx.x; next_unit<true>(p, idx / p.n_kv, cap_tiles, u, count); idx += gridDim.x) {
+        const int h = idx % p.n_kv;
+        const int rows = min(kPagedTileRows, u.m * p.group - u.row);
+        const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
+        const int kvlen = u.ctx + u.m, last_tile = (kvlen - 1) >> 4;
+        const int tfirst = position_of(u, u.row, p.group), tlast = position_of(u, u.row + rows - 1, p.group);
+        const int wfirst = position_of(u, u.row + min(32 * w, rows - 1), p.group);
+        const int wlast = position_of(u, u.row + min(32 * w + 31, rows - 1), p.group);
+        const int c0 = u.k0, c1 = min(u.k1, tlast / kKeys + 1);
+        const bool live = 32 * w < rows;  // uniform over the wave
+        const int rr = u.row + min(32 * w + r32, rows - 1), token = rr / p.group, head = h * p.group + rr % p.group;
+        const int qpos = u.ctx + token;
+        // page ids of the 64 tiles of 16 keys from tile 64 j on, one per lane
+        auto page_ids = [&](int j) { return table[(min(64 * j + lane, last_tile) << 4) >> shift]; };
+        int pj = c0 / 16, pg = page_ids(pj), pg_next = page_ids(pj + 1);
+        auto issue = [&](int c, int buf) {
+            if (c / 16 != pj) {
+                pj = c / 16;
+                pg = pg_next;
+                pg_next = page_ids(pj + 1);
+            }
+#pragma unroll
+            for (int i = 0; i < TL::KIB / 2; ++i) {
+                const int blk = w + 4 * i, isv = blk >= TL::KIB, kb = isv ? blk - TL::KIB : blk;
+                const int key = kb * TL::RPK + lane / (kWave / TL::RPK);  // within the chunk
+                const int tile = 4 * c + kb * TL::RPK / 16;
+                const int page = __builtin_amdgcn_readlane(pg, tile & 63);
+                const int off = ((min(tile, last_tile) << 4) & ((1 << shift) - 1)) + (key & 15);
+                const int piece = (lane % TL::NC) ^ (isv ? TL::vswz(key) : TL::kswz(key));
+                const uint8_t *src = reinterpret_cast<const uint8_t *>(isv ? p.v_pages : p.k_pages) +
+                                     ((((size_t)page * p.n_kv + h) << shift) + off) * TL::ROWB + piece * 16;
+                __builtin_amdgcn_global_load_lds(
+                    static_cast<const void *>(src),
+                    (__attribute__((address_space(3))) void *)(s_kv + (size_t)buf * 2 * TL::BYTES + blk * 1024), 16, 0, 0);
+            }
+        };
+        __syncthreads();  // the unit before is done with the buffers
+        if (c0 < c1) issue(c0, 0);
+        u32x4 q[NKK];
+        const uint16_t *qrow = reinterpret_cast<const uint16_t *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + hb * 8;
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) q[kk] = *reinterpret_cast<const u32x4 *>(qrow + kk * 16) ^ flip;
+        float M = -INFINITY, l = 0.f;  // l: this lane's half of the keys
+        f32x16 o[NDT];
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+        for (int c = c0; c < c1; ++c) {
+            const int buf = (c - c0) & 1, key0 = c * kKeys;
+            wait_vm_lds<0>();
+            barrier_no_fence();  // every wave's pieces of the chunk have landed, and the other buffer has been read
+            if (c + 1 < c1) issue(c + 1, buf ^ 1);
+            const uint8_t *K = s_kv + (size_t)buf * 2 * TL::BYTES;
+            uint8_t *V = s_kv + (size_t)buf * 2 * TL::BYTES + TL::BYTES;
+            if (key0 + kKeys - 1 > tfirst) {  // uniform: keys that some row does not see
+                // A weight of 0 does not silence a NaN or an infinity in the product. Values behind the
+                // request's last token are cleared, whatever the page holds there; others that are not
+                // finite (rare) are taken out, and what the rows that see them get from them is added to
+                // their outputs: a sum per row and column, as a class of two bits (0, +inf, -inf, NaN).
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < TL::BYTES / 16 / 256; ++i) {
+                    u32x4 *v = reinterpret_cast<u32x4 *>(V) + tid + 256 * i;
+                    if ((tid + 256 * i) / TL::NC >= kvlen - key0) {
+                        *v = u32x4{0u, 0u, 0u, 0u};
+                    } else {
+                        const u32x4 x = *v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+                    }
+                }
+                if (__syncthreads_or(bad)) {
+                    for (int col = tid; col < HD; col += 256) {
+                        float acc = 0.f;
+                        int key = 0;
+                        auto next = [&]() {
+                            uint16_t *v = reinterpret_cast<uint16_t *>(V + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
+                            const uint32_t x = (uint32_t)*v << 16;
+                            if ((x & 0x7f800000u) == 0x7f800000u) {
+                                acc += __uint_as_float(x);
+                                *v = 0;
+                            }
+                            ++key;
+                        };
+                        for (int r0 = 0; r0 < kPagedTileRows; r0 += 16) {
+                            uint32_t bits = 0;
+                            for (int r = r0; r < r0 + 16; ++r) {
+                                const int last = min(position_of(u, u.row + min(r, rows - 1), p.group) - key0, kKeys - 1);
+                                while (key <= last) next();
+                                bits |= (acc != acc ? 3u : acc == INFINITY ? 1u : acc == -INFINITY ? 2u : 0u) << (2 * (r - r0));
+                            }
+                            s_cls[col * (kPagedTileRows / 16) + r0 / 16] = bits;
+                        }
+                        while (key < kKeys) next();
+                    }
+                    __syncthreads();
+                    const int row = 32 * w + r32;
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int col = 32 * dt + 8 * (i / 4) + 4 * hb + i % 4;
+                            const uint32_t k = s_cls[col * (kPagedTileRows / 16) + row / 16] >> (2 * (row % 16)) & 3;
+                            o[dt][i] += k == 0 ? 0.f : k == 1 ? INFINITY : k == 2 ? -INFINITY : NAN;
+                        }
+                    __syncthreads();  // the classes have been read
+                }
+            }
+            if (!live || key0 > wlast) continue;
+            f32x16 st[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+                const int key = 32 * kt + r32;
+#pragma unroll
+                for (int kk = 0; kk < NKK; ++kk)
+                    st[kt] = mfma32(*reinterpret_cast<const u32x4 *>(K + key * TL::ROWB + ((2 * kk + hb) ^ TL::kswz(r32)) * 16), q[kk],
+                                    st[kt]);
+            }
+            // st[kt][i] = S^T[key 32 kt + 8 (i / 4) + 4 hb + i % 4][row r32]
+            if (key0 + kKeys - 1 > wfirst) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key0 + 32 * kt + 8 * (i / 4) + 4 * hb + i % 4 > qpos) st[kt][i] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+            if (__any(mx > M + 8.f)) {
+                const float Mn = fmaxf(M, mx), f = M == -INFINITY ? 0.f : exp2_weight(M - Mn);
+                l *= f;
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[dt][i] *= f;
+                M = Mn;
+            }
+            const float ref = M == -INFINITY ? 0.f : M;  // nothing seen: every weight is 0
+            u32x4 pb[4];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float a = exp2_weight(__builtin_fmaf(st[kt][i], scale, -ref));
+                    const float b = exp2_weight(__builtin_fmaf(st[kt][i + 1], scale, -ref));
+                    l += a + b;
+                    pb[2 * kt + i / 8][i / 2 % 4] = pack_bf16(a, b);
+                }
+            // slot j of half hb of step ks: key 16 ks + 8 (j / 4) + 4 hb + j % 4
+            const int vkey = 4 * hb + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {
+                    u32x2 x[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        x[y] = read_tr(V + vkey * TL::ROWB + ((4 * dt + vc) ^ TL::vswz(vkey)) * 16 + (lane & 1) * 8 +
+                                       (16 * ks + 8 * y) * TL::ROWB);
+                    o[dt] = mfma32(u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}, pb[ks], o[dt]);
+                }
+        }
+        l += __shfl_xor(l, 32);
+        const int row = 32 * w + r32;
+        if (row < rows) {
+            const size_t pr = (size_t)(u.part + row) * p.n_kv + h;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 x = f32x4{o[dt][i], o[dt][i + 1], o[dt][i + 2], o[dt][i + 3]};
+                    const int col = 32 * dt + 8 * (i / 4) + 4 * hb;
+                    if (u.part >= 0)
+                        *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = x;
+                    else
+                        store_row<Prec::BF16>(p, u.r0, u.row + row, h, col, x, M, l);
+                }
+            if (u.part >= 0 && hb == 0) {
+                p.part_m[pr] = M;
+                p.part_l[pr] = l;
+            }
+        }
+    }
+}
+
 // Joins the partial states of split row blocks, in position order. Workgroup: some rows of one key head of
 // an item, a thread per four columns of a row.
 template <Prec P, int HD>
@@ -545,6 +771,11 @@ template <Prec P, int HD, int NW, int RG>
 hipError_t launch_shape(int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
     hipError_t e = launch_spans<P, HD, NW, RG>(units, p, s);
     if (e != hipSuccess) return e;
+    if constexpr (P == Prec::BF16) {
+        if (tiles > 0)
+            hipLaunchKernelGGL((paged_tile_kernel<HD>), dim3((unsigned)std::min<int64_t>(tiles * p.n_kv, 16 * kCUs)),
+                               dim3(4 * kWave), tile_lds<HD>(), s, p, p.bk.cap_tiles);
+    }
     if (join) {
         const int64_t groups = (kPagedItemRows + 1024 / HD - 1) / (1024 / HD);
         const int64_t work = std::min<int64_t>(units + 4 * tiles, p.bk.cap_items) * p.n_kv * groups;

@@ -108,7 +108,7 @@ std::vector<Buf> buffers(cllm_paged *c) {
     // kPagedSplitBelow / n_kv, and their spans no more than the pool holds and one each (where requests
     // have no more than kPagedFewRows rows; a plan that needs more is not split); split tiles are fewer than
     // kPagedTileGroups / n_kv, in about that many ranges.
-    c->tiled = false;
+    c->tiled = c->bf16;
     c->block_rows = paged_block_rows(c->bf16, f.head_dim);
     const int64_t nrows = (int64_t)f.max_rows * c->group, blocks = nrows / c->block_rows + f.max_seqs;
     const int64_t tiles = c->tiled ? nrows / kPagedTileRows + f.max_seqs : 0;
