@@ -437,8 +437,10 @@ class PagedCache:
         if st != CLLM_OK:
             raise CllmError(st, "cllm_paged_workspace_bytes failed")
         self.device = torch.device("cuda", device)
-        self._current = torch.cuda.current_stream
-        cur = self._current(self.device)
+        # the address of the current stream (2 us less per call than by a Stream object)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._current = (lambda: raw(device)) if raw else (lambda: torch.cuda.current_stream(self.device).cuda_stream)
+        cur = torch.cuda.current_stream(self.device)
         self.stream = cur.cuda_stream if stream is None else stream
         self._ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
         if self.stream != cur.cuda_stream:
@@ -484,7 +486,7 @@ class PagedCache:
     def _on_stream(self):
         if not self.h:
             raise ValueError("the cache is closed")
-        if self._current(self.device).cuda_stream != self.stream:
+        if self._current() != self.stream:
             raise ValueError("PyTorch's current stream is not the cache's")
 
     def _lens(self, x, n):

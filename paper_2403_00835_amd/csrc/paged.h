@@ -14,8 +14,9 @@ constexpr int kPagedTileRows = 128;
 constexpr int kPagedItemRows = 32;    // rows that are joined together
 // A wave holds a chunk of keys in registers beside its rows: of 512-byte keys, half the rows.
 constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >= 512 ? 16 : 32; }
-constexpr int kPagedSpanKeys = 512;   // keys of a span, at absolute positions
-constexpr int kPagedSplitBelow = 2048;  // workgroups below which row blocks are split into their spans
+constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
+constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
+constexpr int kNoSpans = 1 << 30;
 constexpr int kPagedTileGroups = 512;   // workgroups that tiles of few requests are split into, about
 
 // Words of the status block, written by the plan.
@@ -37,8 +38,8 @@ enum PagedFlags { PF_ARG = 1, PF_ROWS = 2, PF_PAGES = 4 };
 struct alignas(16) PagedUnit {
     int slot, ctx, m, r0;  // the request: slot, context, new tokens, first row of the plan
     int row;               // first row of the block or tile
-    int k0, k1;            // row blocks: the span and -, or -1: every span; tiles: chunks [k0, k1)
-    int part;              // partial row of the first row, or -1: none, the output is written
+    int k0, k1;            // row blocks: spans [k0, k1), kNoSpans: to the last; tiles: chunks [k0, k1)
+    int part;              // partial row of the first row (row blocks: in span k0), or -1: none, the output is written
 };
 struct alignas(16) PagedItem {
     int ctx, m, r0, row;

@@ -13,52 +13,76 @@ namespace cllm {
 
 namespace {
 
-constexpr int kPlanThreads = kPagedMaxSeqs;
-static_assert(kPlanThreads == 1024, "one thread per request");
+constexpr int kPlanThreads = kPagedMaxSeqs;  // at most; blockDim.x, a multiple of 256 and at least the requests
+constexpr int kPlanWaves = kPlanThreads / kWave;
+static_assert(kPlanThreads == 1024 && kPlanWaves == 16, "one thread per request, one row of lanes for the waves' sums");
 
-// Exclusive prefix sums of N values over the workgroup, in place; total: the sums. s_wave: LDS.
+// Inclusive prefix sum over a row of 16 lanes, over a wave: lane moves in the ALU (a step through LDS
+// shuffles took ten times as long).
+__device__ __forceinline__ int row_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // the lane 1, 2, 4, 8 before, in its row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+    x = row_scan(x);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next, rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+    return x;
+}
+
+// Exclusive prefix sums of N values over the workgroup, in place; total: the sums. s_wave: LDS, zero past
+// the workgroup's waves.
 template <int N>
-__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (&s_wave)[N][kPlanThreads / kWave]) {
+__device__ __forceinline__ void block_scan(int (&v)[N], int (&total)[N], int (&s_wave)[N][kPlanWaves]) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int x[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = v[k];
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int y = __shfl_up(x[k], off);
-            if (lane >= off) x[k] += y;
-        }
+    for (int k = 0; k < N; ++k) x[k] = wave_scan(v[k]);
     if (lane == 63)
 #pragma unroll
         for (int k = 0; k < N; ++k) s_wave[k][w] = x[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        int t = s_wave[k][lane & (kPlanThreads / kWave - 1)];
-#pragma unroll
-        for (int off = 1; off < kPlanThreads / kWave; off <<= 1) {
-            const int y = __shfl_up(t, off);
-            if (lane >= off) t += y;
-        }
-        total[k] = __builtin_amdgcn_readlane(t, kPlanThreads / kWave - 1);
+        const int t = row_scan(s_wave[k][lane & (kPlanWaves - 1)]);
+        total[k] = __builtin_amdgcn_readlane(t, kPlanWaves - 1);
         const int before = w > 0 ? __builtin_amdgcn_readlane(t, w - 1) : 0;
         v[k] = before + x[k] - v[k];
     }
 }
 
-// The entry e with start[e] <= i < start[e + 1] (start: n + 1 ascending words of LDS).
+// The entry e with start[e] <= i < start[e + 1] of a wave's uniform item i (start: n + 1 ascending words of
+// LDS): 16 entries apart, then between.
 __device__ __forceinline__ int entry_of(const int *start, int n, int i) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= i)
-            lo = mid;
-        else
-            hi = mid;
+    const int lane = threadIdx.x & 63;
+    const uint64_t far = __ballot(16 * lane < n && start[min(16 * lane, n)] <= i);
+    const int c = 16 * (__popcll(far) - 1);
+    const uint64_t near = __ballot(lane < 16 && c + lane < n && start[min(c + lane, n)] <= i);
+    return c + __popcll(near) - 1;
+}
+
+// f(e, i) for all items i < total of the entries, every PER-th one and the entry that it is in: a wave takes
+// runs of 64. The entries of a run's first and last item by the whole wave, those between by a search in
+// that window (a search per lane over all entries is bound by LDS conflicts, and the kernel, on one CU,
+// by its instructions).
+template <int PER, class F>
+__device__ __forceinline__ void for_items(const int *start, int n, int total, F f) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int i0 = w * kWave * PER; i0 < total; i0 += blockDim.x * PER) {
+        const int i = i0 + lane * PER, last = min(i0 + (kWave - 1) * PER, total - 1);
+        int e = entry_of(start, n, i0);
+        const int window = entry_of(start, n, last) - e;
+        int step = 1;
+        while (step <= window) step <<= 1;
+        for (step >>= 1; step > 0; step >>= 1) {
+            const int at = min(e + step, n);
+            if (at < n && start[at] <= i) e = at;
+        }
+        if (i < total) f(e, i);
     }
-    return lo;
 }
 
 }  // namespace
@@ -85,13 +109,13 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // (bad slot or length, more rows than the bound, too few pages) leaves the books as they were and has
 // no rows.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
-    __shared__ int s_wave[5][kPlanThreads / kWave], s_wave2[4][kPlanThreads / kWave];
+    __shared__ int s_wave[6][kPlanWaves], s_wave2[4][kPlanWaves];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
-    __shared__ int s_unit[kPlanThreads + 1], s_tile[kPlanThreads + 1], s_item[kPlanThreads + 1], s_part[kPlanThreads];
+    __shared__ int s_unit[kPlanThreads + 1], s_tile[kPlanThreads + 1], s_item[kPlanThreads + 1], s_part[kPlanThreads], s_ranges[kPlanThreads];
     __shared__ int s_seq[kPlanThreads], s_ctx[kPlanThreads], s_m[kPlanThreads], s_own[kPlanThreads];
     __shared__ uint32_t s_seen[kPagedMaxSeqs / 32];
     const PagedBooks bk = p.bk;
-    const int b = threadIdx.x, n = p.n, P = 1 << bk.page_shift;
+    const int b = threadIdx.x, n = p.n, P = 1 << bk.page_shift, row_shift = 31 - __clz(p.block_rows);
     const int free0 = bk.status[PS_FREE];
     int seq = 0, ctx = 0, m = 0;
     if (b < n) {
@@ -100,6 +124,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         m = p.neu[b];
     }
     if (b < kPagedMaxSeqs / 32) s_seen[b] = 0;
+    if (b < 6 * kPlanWaves) (&s_wave[0][0])[b] = 0;
+    if (b < 4 * kPlanWaves) (&s_wave2[0][0])[b] = 0;
     __syncthreads();
     bool bad = false;
     int own = 0, need = 0;
@@ -118,7 +144,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     const bool tiled = p.tiled && T0 > kPagedFewRows;
     const int nrb = tiled ? 0 : (T0 + p.block_rows - 1) / p.block_rows;
     const int ntile = tiled ? (T0 + kPagedTileRows - 1) / kPagedTileRows : 0;
-    int v[5] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile}, total[5];
+    const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
+    int v[6] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)1 << 20)}, total[6];
     block_scan(v, total, s_wave);
     const int R = total[0], G = total[1], T = total[2];
     if (R > p.rows) flags |= PF_ROWS;
@@ -131,21 +158,25 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         }
         return;
     }
-    // Attention units. Row blocks: all the keys that the rows see, or, where that leaves workgroups idle,
-    // a unit per span (of the request's last token: units of spans that a block does not see do nothing).
-    // Tiles: ranges of keys, as many as make kPagedTileGroups workgroups of the plan's tiles, none under
-    // a span's keys. What the partial states' memory does not hold is not split.
-    int U = total[3], UT = total[4], I = 0, u0 = v[3], t0 = v[4], i0 = 0, p0 = 0, nspan = 1, nrange = 1;
+    // Attention units. Row blocks: as many spans of the request's keys (up to its last token: a unit of
+    // spans that its block does not see does nothing) as make about kPagedUnits workgroups of the plan. Tiles:
+    // ranges of keys, as many as make about kPagedTileGroups workgroups of the plan's tiles, none under a
+    // span's keys. What the partial states' memory does not hold is not split.
+    const int per = max((int)(((int64_t)total[5] * p.n_kv + kPagedUnits - 1) / kPagedUnits), 1);
+    int U = total[3], UT = total[4], I = 0, u0 = v[3], t0 = v[4], i0 = 0, p0 = 0;
+    int nr = 1;
+    bool parts = false, split = false;
     {
-        const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
         const int ranges = UT > 0 ? (kPagedTileGroups + UT * p.n_kv - 1) / (UT * p.n_kv) : 1;
-        const int ns = nrb && U * p.n_kv < kPagedSplitBelow ? spans : 1, nr = ntile ? min(ranges, spans) : 1;
-        const bool parts = ns > 1 || nr > 1;
-        int x[4] = {nrb * ns, ntile * nr, parts ? (T0 + kPagedItemRows - 1) / kPagedItemRows : 0, parts ? max(ns, nr) * T0 : 0};
+        const int ns = nrb ? (spans + per - 1) / per : 1;
+        nr = ntile ? min(ranges, spans) : 1;
+        parts = ns > 1 || nr > 1;
+        int x[4] = {nrb * ns, ntile * nr, parts ? (T0 + kPagedItemRows - 1) / kPagedItemRows : 0,
+                    parts ? (ns > 1 ? spans : nr) * T0 : 0};
         int y[4];
         block_scan(x, y, s_wave2);
-        if (y[0] <= bk.cap_units && y[1] <= bk.cap_tiles && y[2] <= bk.cap_items && y[3] <= p.cap_part)
-            U = y[0], UT = y[1], I = y[2], u0 = x[0], t0 = x[1], i0 = x[2], p0 = x[3], nspan = ns, nrange = nr;
+        split = y[0] <= bk.cap_units && y[1] <= bk.cap_tiles && y[2] <= bk.cap_items && y[3] <= p.cap_part;
+        if (split) U = y[0], UT = y[1], I = y[2], u0 = x[0], t0 = x[1], i0 = x[2], p0 = x[3];
     }
     s_seq[b] = seq;
     s_ctx[b] = ctx;
@@ -157,54 +188,86 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     s_unit[b] = u0;
     s_tile[b] = t0;
     s_item[b] = i0;
-    s_part[b] = nspan > 1 || nrange > 1 ? p0 : -1;
-    if (b == 0) {
-        s_rows[kPlanThreads] = R;
-        s_give[kPlanThreads] = G;
-        s_take[kPlanThreads] = T;
-        s_unit[kPlanThreads] = U;
-        s_tile[kPlanThreads] = UT;
-        s_item[kPlanThreads] = I;
+    s_part[b] = split && parts ? p0 : -1;
+    s_ranges[b] = !ntile ? 0 : split ? nr : 1;
+    if (b == 0) {  // behind the last thread's
+        const int end = blockDim.x;
+        s_rows[end] = R;
+        s_give[end] = G;
+        s_take[end] = T;
+        s_unit[end] = U;
+        s_tile[end] = UT;
+        s_item[end] = I;
     }
     __syncthreads();
-    for (int i = b; i < G; i += kPlanThreads) {
-        const int e = entry_of(s_give, n, i), k = i - s_give[e];
-        int32_t *at = bk.table + (size_t)s_seq[e] * bk.max_pages + s_own[e] - 1 - k;
-        bk.free_list[free0 + G - s_give[e + 1] + k] = *at;
-        *at = -1;
+    if (G > 0) {  // uniform
+        auto at = [&](int e, int i) { return bk.table + (size_t)s_seq[e] * bk.max_pages + s_own[e] - 1 - (i - s_give[e]); };
+        for_items<1>(s_give, n, G, [&](int e, int i) { bk.free_list[free0 + G - s_give[e + 1] + i - s_give[e]] = *at(e, i); });
+        __syncthreads();  // before the entries are cleared, and taken from the list
+        for_items<1>(s_give, n, G, [&](int e, int i) { *at(e, i) = -1; });
     }
-    if (G > 0) __syncthreads();  // uniform
-    for (int i = b; i < T; i += kPlanThreads) {
-        const int e = entry_of(s_take, n, i);
-        bk.table[(size_t)s_seq[e] * bk.max_pages + s_own[e] + i - s_take[e]] = bk.free_list[free0 + G - 1 - i];
-    }
+    // Pages taken, and the rows: a row's page is an old entry of the table or a new one, read off the stack
+    // here too, so the rows need not wait for the table.
+    if (T > 0)
+        for_items<1>(s_take, n, T, [&](int e, int i) {
+            bk.table[(size_t)s_seq[e] * bk.max_pages + s_own[e] + i - s_take[e]] = bk.free_list[free0 + G - 1 - i];
+        });
+    if (R > 0)
+        for_items<4>(s_rows, n, R, [&](int e, int i) {
+            alignas(16) int slot[4], pos[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = min(i + k, R - 1);
+                while (s_rows[e + 1] <= row) ++e;
+                pos[k] = s_ctx[e] + row - s_rows[e];
+                const int at = pos[k] >> bk.page_shift, fresh = at - s_own[e];
+                slot[k] = fresh < 0 ? bk.table[(size_t)s_seq[e] * bk.max_pages + at]
+                                    : bk.free_list[free0 + G - 1 - s_take[e] - fresh];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) slot[k] = (slot[k] << bk.page_shift) + (pos[k] & (P - 1));
+            if (i + 4 <= R) {
+                *reinterpret_cast<u32x4 *>(bk.row_slot + i) = *reinterpret_cast<const u32x4 *>(slot);
+                *reinterpret_cast<u32x4 *>(bk.row_pos + i) = *reinterpret_cast<const u32x4 *>(pos);
+            } else {
+                for (int k = 0; i + k < R; ++k) {
+                    bk.row_slot[i + k] = slot[k];
+                    bk.row_pos[i + k] = pos[k];
+                }
+            }
+        });
     if (b < n) {
         bk.seq_pages[seq] = need;
         bk.row_start[b] = v[0];
     }
     if (b == 0) bk.row_start[n] = R;
-    for (int i = b; i < U; i += kPlanThreads) {
-        const int e = entry_of(s_unit, n, i), k = i - s_unit[e], rows = s_m[e] * p.group;
-        const int blocks = (rows + p.block_rows - 1) / p.block_rows, part = s_part[e];
-        // the blocks of a span next to each other: they read the same keys
-        const int row = k % blocks * p.block_rows, span = k / blocks;
-        bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, part < 0 ? -1 : span, 0,
-                                part < 0 ? -1 : part + span * rows + row};
-    }
-    for (int i = b; i < UT; i += kPlanThreads) {
-        const int e = entry_of(s_tile, n, i), k = i - s_tile[e], rows = s_m[e] * p.group;
-        const int tiles = (rows + kPagedTileRows - 1) / kPagedTileRows, part = s_part[e];
-        const int ranges = (s_tile[e + 1] - s_tile[e]) / tiles, j = k / tiles;
-        const int row = (tiles - 1 - k % tiles) * kPagedTileRows;  // the tiles that see most keys first
-        const int chunks = (s_ctx[e] + s_m[e] + kAttnChunk - 1) / kAttnChunk, per = (chunks + ranges - 1) / ranges;
-        bk.tiles[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, j * per, min(chunks, (j + 1) * per),
-                                part < 0 ? -1 : part + j * rows + row};
-    }
-    for (int i = b; i < I; i += kPlanThreads) {
-        const int e = entry_of(s_item, n, i), row = (i - s_item[e]) * kPagedItemRows, rows = s_m[e] * p.group;
-        const int tiles = (rows + kPagedTileRows - 1) / kPagedTileRows;
-        bk.items[i] = PagedItem{s_ctx[e], s_m[e], s_rows[e], row, s_part[e] + row, rows, (s_tile[e + 1] - s_tile[e]) / tiles, 0};
-    }
+    if (U > 0)
+        for_items<1>(s_unit, n, U, [&](int e, int i) {
+            const int rows = s_m[e] * p.group, blocks = (rows + p.block_rows - 1) >> row_shift, part = s_part[e];
+            // the blocks of the same spans next to each other: they read the same keys
+            int k0 = i - s_unit[e], row = 0;
+            if (blocks > 1) {
+                row = k0 % blocks << row_shift;
+                k0 = k0 / blocks;
+            }
+            k0 = part < 0 ? 0 : k0 * per;
+            bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, k0, part < 0 ? kNoSpans : k0 + per,
+                                    part < 0 ? -1 : part + k0 * rows + row};
+        });
+    if (UT > 0)
+        for_items<1>(s_tile, n, UT, [&](int e, int i) {
+            const int rows = s_m[e] * p.group, tiles = (rows + kPagedTileRows - 1) / kPagedTileRows, part = s_part[e];
+            const int ranges = s_ranges[e], k = i - s_tile[e], j = k / tiles;
+            const int row = (tiles - 1 - (k - j * tiles)) * kPagedTileRows;  // the tiles that see most keys first
+            const int chunks = (s_ctx[e] + s_m[e] + kAttnChunk - 1) / kAttnChunk, len = (chunks + ranges - 1) / ranges;
+            bk.tiles[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, j * len, min(chunks, (j + 1) * len),
+                                    part < 0 ? -1 : part + j * rows + row};
+        });
+    if (I > 0)
+        for_items<1>(s_item, n, I, [&](int e, int i) {
+            const int row = (i - s_item[e]) * kPagedItemRows;
+            bk.items[i] = PagedItem{s_ctx[e], s_m[e], s_rows[e], row, s_part[e] + row, s_m[e] * p.group, s_ranges[e], 0};
+        });
     if (b == 0) {
         bk.status[PS_ROWS] = R;
         bk.status[PS_ENTRIES] = n;
@@ -217,13 +280,6 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         bk.status[PS_BOUND_NEW] = p.max_new;
         bk.status[PS_BOUND_LEN] = p.max_len;
         bk.status[PS_LATE] = 0;
-    }
-    if (R > 0) __syncthreads();  // the tables
-    for (int i = b; i < R; i += kPlanThreads) {
-        const int e = entry_of(s_rows, n, i), pos = s_ctx[e] + i - s_rows[e];
-        const int page = bk.table[(size_t)s_seq[e] * bk.max_pages + (pos >> bk.page_shift)];
-        bk.row_slot[i] = (page << bk.page_shift) + (pos & (P - 1));
-        bk.row_pos[i] = pos;
     }
 }
 
@@ -288,7 +344,9 @@ hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int
 
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s) {
     if (p.n < 1 || p.n > kPagedMaxSeqs || p.bk.max_seqs > kPagedMaxSeqs) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    // four waves unless there are requests or rows for more (their barriers and sums cost 2 us)
+    const int threads = p.n <= 256 && p.rows <= 2048 ? 256 : kPlanThreads;
+    hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(threads), 0, s, p);
     return hipGetLastError();
 }
 

@@ -211,6 +211,46 @@ __device__ __forceinline__ bool next_unit(const PagedAttnParams &p, int i, int c
 
 }  // namespace
 
+namespace {
+
+// Four columns of one row of an item: the states of its spans (those up to the row's position) or ranges.
+template <Prec P, int HD>
+__device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedItem &it, int h, int row, int col) {
+    if (row >= min(kPagedItemRows, it.m * p.group - it.row)) return;
+    const int count = it.count > 0 ? it.count : (it.ctx + (it.row + row) / p.group) / kPagedSpanKeys + 1;
+    float M = -INFINITY, l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 4;  // states in flight (of short rows, more repeat the last one's loads)
+    for (int s0 = 0; s0 < count; s0 += U) {
+        f32x4 os[U];
+        float Ms[U], ls[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const size_t pr = (size_t)(it.part + min(s0 + i, count - 1) * it.stride + row) * p.n_kv + h;
+            os[i] = *reinterpret_cast<const f32x4 *>(p.part_o + pr * HD + col);
+            Ms[i] = p.part_m[pr];
+            ls[i] = p.part_l[pr];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool use = s0 + i < count;  // a select: a branch would sink the loads behind it
+            float Mn = M, w0, w1;
+            merge_weights(Mn, Ms[i], w0, w1);
+            const float ln = merge_value(l, ls[i], w0, w1);
+            M = use ? Mn : M;
+            l = use ? ln : l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = merge_value(o[e], os[i][e], w0, w1);
+                o[e] = use ? x : o[e];
+            }
+        }
+    }
+    store_row<P>(p, it.r0, it.row + row, h, col, o, M, l);
+}
+
+}  // namespace
+
 // LDS bytes of a wave of the span kernel: the chunk's V (bf16), then in its place the chunk's states of up
 // to 16 RG rows (padded rows, so that the writes of 16 rows hit different banks).
 template <Prec P, int HD, int RG>
@@ -408,7 +448,7 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
 // LDS (bf16: transposing reads) or straight (fp32); then the workgroup merges the chunks' states. Loads of
 // a workgroup are all in flight at once: 256 KiB at head_dim 128.
 template <Prec P, int HD, int NW, int RG>
-__global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams p, int cap_units) {
+__global__ __launch_bounds__(NW * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p, int cap_units) {
     constexpr int REGION = span_wave_lds<P, HD, RG>(), SROW = HD + 4, ROWS = 16 * RG;
     constexpr int ITEMS = (ROWS * HD / 4 + NW * kWave - 1) / (NW * kWave);
     extern __shared__ u32x4 s_raw[];
@@ -423,7 +463,7 @@ __global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams 
         const int rows = min(ROWS, u.m * p.group - u.row);
         const int blast = position_of(u, u.row + rows - 1, p.group);  // the block's last position
         const int last_key = u.ctx + u.m - 1;
-        const int s0 = u.k0 < 0 ? 0 : u.k0, s1 = min(u.k0 < 0 ? INT32_MAX - 1 : u.k0, blast / kPagedSpanKeys) + 1;
+        const int s0 = u.k0, s1 = min(u.k1, blast / kPagedSpanKeys + 1);
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
         // the states of this thread's (row, four columns) items: the span's, the row's
         float Mr[ITEMS], lr[ITEMS];
@@ -461,14 +501,18 @@ __global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams 
                 }
                 __syncthreads();  // before the next chunks come into the regions
             }
-            if (u.part >= 0) {  // one span: its state as it is
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) Mr[i] = M[i], lr[i] = l[i], orow[i] = o[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    const int row = (tid + i * NW * kWave) / (HD / 4);
-                    if (s * kPagedSpanKeys > position_of(u, u.row + min(row, rows - 1), p.group)) continue;
+            for (int i = 0; i < ITEMS; ++i) {
+                const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
+                if (row >= rows || s * kPagedSpanKeys > position_of(u, u.row + row, p.group)) continue;
+                if (u.part >= 0) {  // the span's state as it is
+                    const size_t pr = (size_t)(u.part + (s - s0) * u.m * p.group + row) * p.n_kv + h;
+                    *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = o[i];
+                    if (col == 0) {
+                        p.part_m[pr] = M[i];
+                        p.part_l[pr] = l[i];
+                    }
+                } else {
                     float w0, w1;
                     merge_weights(Mr[i], M[i], w0, w1);
                     lr[i] = merge_value(lr[i], l[i], w0, w1);
@@ -477,20 +521,11 @@ __global__ __launch_bounds__(NW * kWave) void paged_span_kernel(PagedAttnParams 
                 }
             }
         }
+        if (u.part >= 0) continue;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
-            if (row >= rows) break;
-            if (u.part >= 0) {
-                const size_t pr = (size_t)(u.part + row) * p.n_kv + h;
-                *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = orow[i];
-                if (col == 0) {
-                    p.part_m[pr] = Mr[i];
-                    p.part_l[pr] = lr[i];
-                }
-            } else {
-                store_row<P>(p, u.r0, u.row + row, h, col, orow[i], Mr[i], lr[i]);
-            }
+            if (row < rows) store_row<P>(p, u.r0, u.row + row, h, col, orow[i], Mr[i], lr[i]);
         }
     }
 }
@@ -731,26 +766,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int 
     PagedItem it = p.bk.items[min((int)blockIdx.x / (p.n_kv * NG), cap_items - 1)];
     request_together(R, n, br, bn, bl, it.ctx, it.m, it.r0, it.row, it.part, it.stride, it.count);
     if (R == 0 || br != p.rows || bn != p.max_new || bl != p.max_len) return;
-    const int col = threadIdx.x % LPR * 4, work = n * p.n_kv * NG;
+    const int work = n * p.n_kv * NG;
     for (int idx = blockIdx.x; idx < work; idx += gridDim.x) {
         if (idx != (int)blockIdx.x) it = p.bk.items[idx / (p.n_kv * NG)];
-        const int h = idx % p.n_kv, row = idx / p.n_kv % NG * RPW + threadIdx.x / LPR;
-        if (row >= min(kPagedItemRows, it.m * p.group - it.row)) continue;
-        const int count = it.count > 0 ? it.count : (it.ctx + (it.row + row) / p.group) / kPagedSpanKeys + 1;
-        float M = -INFINITY, l = 0.f;
-        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int s = 0; s < count; ++s) {
-            const size_t pr = (size_t)(it.part + s * it.stride + row) * p.n_kv + h;
-            const f32x4 os = *reinterpret_cast<const f32x4 *>(p.part_o + pr * HD + col);
-            const float Ms = p.part_m[pr], ls = p.part_l[pr];
-            float w0, w1;
-            merge_weights(M, Ms, w0, w1);
-            l = merge_value(l, ls, w0, w1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = merge_value(o[i], os[i], w0, w1);
-        }
-        store_row<P>(p, it.r0, it.row + row, h, col, o, M, l);
+        join_row<P, HD>(p, it, idx % p.n_kv, idx / p.n_kv % NG * RPW + threadIdx.x / LPR, threadIdx.x % LPR * 4);
     }
 }
 
@@ -791,15 +810,15 @@ hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join,
     if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0 || tiles < 0) return hipErrorInvalidValue;
     if (units + tiles == 0 || p.rows == 0) return hipSuccess;
     if (bf16) {
-        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 8, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 8, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 8, 2>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 4, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 4, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 4, 2>(units, tiles, join, p, s);
         if (p.hd == 256) return launch_shape<Prec::BF16, 256, 4, 1>(units, tiles, join, p, s);
     } else {
-        if (p.hd == 16) return launch_shape<Prec::F32, 16, 8, 2>(units, tiles, join, p, s);
-        if (p.hd == 32) return launch_shape<Prec::F32, 32, 8, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::F32, 64, 8, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::F32, 128, 8, 1>(units, tiles, join, p, s);
+        if (p.hd == 16) return launch_shape<Prec::F32, 16, 4, 2>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::F32, 32, 4, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::F32, 64, 4, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::F32, 128, 4, 1>(units, tiles, join, p, s);
     }
     return hipErrorInvalidValue;
 }

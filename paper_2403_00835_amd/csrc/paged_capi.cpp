@@ -104,22 +104,23 @@ std::vector<Buf> buffers(cllm_paged *c) {
     bk.max_pages = (f.max_ctx + f.page_size - 1) / f.page_size;
     bk.n_pages = f.n_pages;
     bk.page_shift = __builtin_ctz((unsigned)f.page_size);
-    // Attention units. Row blocks and tiles of any plan, unsplit; split row blocks are fewer than
-    // kPagedSplitBelow / n_kv, and their spans no more than the pool holds and one each (where requests
-    // have no more than kPagedFewRows rows; a plan that needs more is not split); split tiles are fewer than
-    // kPagedTileGroups / n_kv, in about that many ranges.
+    // Attention units: row blocks and tiles of any plan, and what splitting adds (kPagedUnits /
+    // n_kv_heads row blocks, twice kPagedTileGroups / n_kv_heads tiles, about). Partial states: of the spans
+    // of the pool and one of each request, for requests of few rows; split tiles. A plan that needs more is not
+    // split.
     c->tiled = c->bf16;
     c->block_rows = paged_block_rows(c->bf16, f.head_dim);
-    const int64_t nrows = (int64_t)f.max_rows * c->group, blocks = nrows / c->block_rows + f.max_seqs;
-    const int64_t tiles = c->tiled ? nrows / kPagedTileRows + f.max_seqs : 0;
-    const int64_t few = kPagedSplitBelow / f.n_kv_heads + 1, few_tiles = kPagedTileGroups / f.n_kv_heads + 1;
+    const int64_t nrows = (int64_t)f.max_rows * c->group;
+    const int64_t few = kPagedUnits / f.n_kv_heads + 1, few_tiles = 2 * (kPagedTileGroups / f.n_kv_heads + 1);
+    const int64_t blocks = nrows / c->block_rows + f.max_seqs, tiles = c->tiled ? nrows / kPagedTileRows + f.max_seqs : 0;
     const int64_t spans = (f.max_ctx + kPagedSpanKeys - 1) / kPagedSpanKeys;
-    const int64_t split = std::min(std::min(few, blocks) * spans,
-                                   kPagedFewRows / c->block_rows * (((int64_t)f.n_pages * f.page_size + kPagedSpanKeys - 1) / kPagedSpanKeys + few));
-    bk.cap_units = (int)std::max(blocks, split);
-    bk.cap_tiles = (int)(tiles + 2 * few_tiles);
-    bk.cap_items = (int)(few + 4 * few_tiles);
-    c->cap_part = (int)std::min<int64_t>(split * c->block_rows + 2 * few_tiles * kPagedTileRows, INT32_MAX / 2);
+    const int64_t pool = std::min(((int64_t)f.n_pages * f.page_size + kPagedSpanKeys - 1) / kPagedSpanKeys + f.max_seqs,
+                                  f.max_seqs * spans);
+    bk.cap_units = (int)(blocks + few);
+    bk.cap_tiles = (int)(tiles + few_tiles);
+    bk.cap_items = (int)std::min(nrows / kPagedItemRows + f.max_seqs, few + 4 * few_tiles + f.max_seqs);
+    c->cap_part = (int)std::min<int64_t>(std::min(nrows, kPagedFewRows * (int64_t)f.max_seqs) * std::min(spans, pool), INT32_MAX / 4);
+    c->cap_part = (int)std::min<int64_t>(c->cap_part, kPagedFewRows * pool) + (int)(few_tiles * kPagedTileRows);
     auto P = [](auto **q) { return reinterpret_cast<void **>(q); };
     const size_t part = (size_t)c->cap_part * f.n_kv_heads;
     std::vector<Buf> b{
@@ -394,14 +395,15 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     p.group = c->group;
     const double sc = scale == 0.0f ? 1.0 / std::sqrt((double)f.head_dim) : (double)scale;
     p.scale_log2 = (float)(1.4426950408889634 * sc);
-    // bounds of the launch: row blocks of the rows and requests, spans of the longest request
+    // bounds of the launch
     auto pieces = [&](int64_t most, int rows) {  // of requests of at most `most` rows each
         return std::min(c->n * ((most + rows - 1) / rows), (int64_t)c->rows * c->group / rows + c->n);
     };
     const int64_t most = (int64_t)c->max_new * c->group, spans = (c->max_len + kPagedSpanKeys - 1) / kPagedSpanKeys;
-    const int64_t units = pieces(c->tiled ? std::min<int64_t>(most, kPagedFewRows) : most, c->block_rows) * spans;
+    int64_t units = pieces(c->tiled ? std::min<int64_t>(most, kPagedFewRows) : most, c->block_rows);
+    units = std::min(units * spans, units + kPagedUnits / f.n_kv_heads + 1);
     int64_t tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
-    if (tiles) tiles = std::min<int64_t>(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
+    tiles = std::min(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
     HIPCHK(c, launch_paged_attn(c->bf16, units, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
 }
