@@ -16,7 +16,7 @@ constexpr int kPagedItemRows = 32;    // rows that are joined together
 constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >= 512 ? 16 : 32; }
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
 constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
-constexpr int kNoSpans = 1 << 30;
+constexpr int kAllSpans = 1 << 30;
 constexpr int kPagedTileGroups = 512;   // workgroups that tiles of few requests are split into, about
 
 // Words of the status block, written by the plan.
@@ -38,7 +38,7 @@ enum PagedFlags { PF_ARG = 1, PF_ROWS = 2, PF_PAGES = 4 };
 struct alignas(16) PagedUnit {
     int slot, ctx, m, r0;  // the request: slot, context, new tokens, first row of the plan
     int row;               // first row of the block or tile
-    int k0, k1;            // row blocks: spans [k0, k1), kNoSpans: to the last; tiles: chunks [k0, k1)
+    int k0, k1;            // row blocks: spans [k0, k1), kAllSpans: to the last; tiles: chunks [k0, k1)
     int part;              // partial row of the first row (row blocks: in span k0), or -1: none, the output is written
 };
 struct alignas(16) PagedItem {
@@ -71,7 +71,7 @@ struct PagedPlanParams {
     int group, n_kv;                // query heads per key head, key heads
     bool tiled;                     // long chunks take tiles
     int block_rows;                 // of the others
-    int cap_part;                   // partial rows
+    int cap_part, cap_tile_part;    // partial rows of row blocks, and of tiles behind them
 };
 
 struct PagedAppendParams {
@@ -93,6 +93,7 @@ struct PagedAttnParams {
     float *lse;                   // [rows][n_heads], or null
     float *part_o, *part_m, *part_l;  // [partial row][n_kv] (x hd)
     int n_heads, n_kv, hd, group;
+    uint32_t group_inv;           // 2^24 / group, rounded up
     float scale_log2;
 };
 

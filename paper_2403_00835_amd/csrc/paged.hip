@@ -109,7 +109,7 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // (bad slot or length, more rows than the bound, too few pages) leaves the books as they were and has
 // no rows.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
-    __shared__ int s_wave[6][kPlanWaves], s_wave2[4][kPlanWaves];
+    __shared__ int s_wave[6][kPlanWaves], s_wave2[6][kPlanWaves];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
     __shared__ int s_unit[kPlanThreads + 1], s_tile[kPlanThreads + 1], s_item[kPlanThreads + 1], s_part[kPlanThreads], s_ranges[kPlanThreads];
     __shared__ int s_seq[kPlanThreads], s_ctx[kPlanThreads], s_m[kPlanThreads], s_own[kPlanThreads];
@@ -124,8 +124,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         m = p.neu[b];
     }
     if (b < kPagedMaxSeqs / 32) s_seen[b] = 0;
-    if (b < 6 * kPlanWaves) (&s_wave[0][0])[b] = 0;
-    if (b < 4 * kPlanWaves) (&s_wave2[0][0])[b] = 0;
+    if (b < 6 * kPlanWaves) (&s_wave[0][0])[b] = (&s_wave2[0][0])[b] = 0;
     __syncthreads();
     bool bad = false;
     int own = 0, need = 0;
@@ -159,25 +158,20 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         return;
     }
     // Attention units. Row blocks: as many spans of the request's keys (up to its last token: a unit of
-    // spans that its block does not see does nothing) as make about kPagedUnits workgroups of the plan. Tiles:
-    // ranges of keys, as many as make about kPagedTileGroups workgroups of the plan's tiles, none under a
-    // span's keys. What the partial states' memory does not hold is not split.
+    // spans that its block does not see does nothing) as make about kPagedUnits workgroups of the plan, a
+    // partial state per span where there are several. Tiles: ranges of keys, as many as make about
+    // kPagedTileGroups workgroups of the plan's tiles, none under a span's keys. What the partials do not hold
+    // is not split (bf16 row blocks always fit).
     const int per = max((int)(((int64_t)total[5] * p.n_kv + kPagedUnits - 1) / kPagedUnits), 1);
-    int U = total[3], UT = total[4], I = 0, u0 = v[3], t0 = v[4], i0 = 0, p0 = 0;
-    int nr = 1;
-    bool parts = false, split = false;
-    {
-        const int ranges = UT > 0 ? (kPagedTileGroups + UT * p.n_kv - 1) / (UT * p.n_kv) : 1;
-        const int ns = nrb ? (spans + per - 1) / per : 1;
-        nr = ntile ? min(ranges, spans) : 1;
-        parts = ns > 1 || nr > 1;
-        int x[4] = {nrb * ns, ntile * nr, parts ? (T0 + kPagedItemRows - 1) / kPagedItemRows : 0,
-                    parts ? (ns > 1 ? spans : nr) * T0 : 0};
-        int y[4];
-        block_scan(x, y, s_wave2);
-        split = y[0] <= bk.cap_units && y[1] <= bk.cap_tiles && y[2] <= bk.cap_items && y[3] <= p.cap_part;
-        if (split) U = y[0], UT = y[1], I = y[2], u0 = x[0], t0 = x[1], i0 = x[2], p0 = x[3];
-    }
+    const int ranges = total[4] > 0 ? (kPagedTileGroups + total[4] * p.n_kv - 1) / (total[4] * p.n_kv) : 1;
+    const int nr = ntile ? min(ranges, spans) : 1, items = (T0 + kPagedItemRows - 1) / kPagedItemRows;
+    const bool dparts = nrb && spans > 1, tparts = nr > 1;
+    int x[6] = {nrb * ((spans + per - 1) / per), dparts ? items : 0, dparts ? (int)min((int64_t)spans * T0, (int64_t)1 << 20) : 0,
+                ntile * nr, tparts ? items : 0, tparts ? nr * T0 : 0}, y[6];
+    block_scan(x, y, s_wave2);
+    const bool dsplit = y[0] <= bk.cap_units && y[2] <= p.cap_part, tsplit = y[3] <= bk.cap_tiles && y[5] <= p.cap_tile_part;
+    const int U = dsplit ? y[0] : total[3], UT = tsplit ? y[3] : total[4];
+    const int I = (dsplit ? y[1] : 0) + (tsplit ? y[4] : 0);
     s_seq[b] = seq;
     s_ctx[b] = ctx;
     s_m[b] = m;
@@ -185,11 +179,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     s_rows[b] = v[0];
     s_give[b] = v[1];
     s_take[b] = v[2];
-    s_unit[b] = u0;
-    s_tile[b] = t0;
-    s_item[b] = i0;
-    s_part[b] = split && parts ? p0 : -1;
-    s_ranges[b] = !ntile ? 0 : split ? nr : 1;
+    s_unit[b] = dsplit ? x[0] : v[3];
+    s_tile[b] = tsplit ? x[3] : v[4];
+    s_item[b] = (dsplit ? x[1] : 0) + (tsplit ? x[4] : 0);
+    s_part[b] = dparts && dsplit ? x[2] : tparts && tsplit ? p.cap_part + x[5] : -1;
+    s_ranges[b] = !ntile ? 0 : tsplit ? nr : 1;
     if (b == 0) {  // behind the last thread's
         const int end = blockDim.x;
         s_rows[end] = R;
@@ -250,8 +244,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
                 row = k0 % blocks << row_shift;
                 k0 = k0 / blocks;
             }
-            k0 = part < 0 ? 0 : k0 * per;
-            bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, k0, part < 0 ? kNoSpans : k0 + per,
+            k0 = part < 0 ? 0 : k0 * per;  // no partials: one span, or all
+            bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], row, k0, part < 0 ? kAllSpans : k0 + per,
                                     part < 0 ? -1 : part + k0 * rows + row};
         });
     if (UT > 0)

@@ -173,15 +173,24 @@ __device__ __forceinline__ void weight_operand(const f32x4 (&st)[4], u32x4 (&pb)
     }
 }
 
-// Position of a unit's row.
-__device__ __forceinline__ int position_of(const PagedUnit &u, int row, int group) { return u.ctx + row / group; }
+// Rows of a unit, from its first: row j is token(j) of the chunk, head(j) of the group. The quotient of the
+// small number by the group is a product: exact below 2^24 / 1024 (group's largest).
+struct RowMap {
+    int token0, rem0, group;
+    uint32_t inv;  // 2^24 / group, rounded up
+    __device__ RowMap(const PagedAttnParams &p, int row)
+        : token0(row / p.group), rem0(row % p.group), group(p.group), inv(p.group_inv) {}
+    __device__ int past(int j) const { return (int)__umulhi((uint32_t)(rem0 + j) << 8, inv); }
+    __device__ int token(int j) const { return token0 + past(j); }
+    __device__ int head(int j) const { return rem0 + j - past(j) * group; }
+};
 
-// Four columns of a row's output, and with the first its log sum of exponentials.
+// Four columns of a row's output (token and head of the plan's rows), and with the first its log sum of
+// exponentials.
 template <Prec P>
-__device__ __forceinline__ void store_row(const PagedAttnParams &p, int r0, int row, int h, int col, f32x4 o, float M, float l) {
+__device__ __forceinline__ void store_row(const PagedAttnParams &p, int token, int head, int col, f32x4 o, float M, float l) {
     using T = typename PrecT<P>::T;
-    const int token = row / p.group, head = h * p.group + row % p.group;
-    T *out = reinterpret_cast<T *>(p.out) + (size_t)(r0 + token) * p.out_stride + head * p.hd + col;
+    T *out = reinterpret_cast<T *>(p.out) + (size_t)token * p.out_stride + head * p.hd + col;
     alignas(16) T x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = to_elem<P>(o[e] / l);
@@ -189,7 +198,7 @@ __device__ __forceinline__ void store_row(const PagedAttnParams &p, int r0, int 
         *reinterpret_cast<u32x2 *>(out) = *reinterpret_cast<const u32x2 *>(x);
     else
         *reinterpret_cast<u32x4 *>(out) = *reinterpret_cast<const u32x4 *>(x);
-    if (p.lse && col == 0) p.lse[(size_t)(r0 + token) * p.n_heads + head] = (M + log2f(l)) * kLn2;
+    if (p.lse && col == 0) p.lse[(size_t)token * p.n_heads + head] = (M + log2f(l)) * kLn2;
 }
 
 // A unit, requested with the words that say whether the call is the plan's: one round trip.
@@ -217,7 +226,8 @@ namespace {
 template <Prec P, int HD>
 __device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedItem &it, int h, int row, int col) {
     if (row >= min(kPagedItemRows, it.m * p.group - it.row)) return;
-    const int count = it.count > 0 ? it.count : (it.ctx + (it.row + row) / p.group) / kPagedSpanKeys + 1;
+    const RowMap map(p, it.row);
+    const int count = it.count > 0 ? it.count : (it.ctx + map.token(row)) / kPagedSpanKeys + 1;
     float M = -INFINITY, l = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr int U = 4;  // states in flight (of short rows, more repeat the last one's loads)
@@ -246,7 +256,7 @@ __device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedIt
             }
         }
     }
-    store_row<P>(p, it.r0, it.row + row, h, col, o, M, l);
+    store_row<P>(p, it.r0 + map.token(row), h * p.group + map.head(row), col, o, M, l);
 }
 
 }  // namespace
@@ -262,8 +272,8 @@ constexpr int span_wave_lds() {
 // One chunk of the span kernel, by one wave: the states of its NRG groups of 16 rows into s_mine ([row][column])
 // and s_m, s_l (this wave's rows). last_key: the request's last token; pages: its table.
 template <Prec P, int HD, int NRG>
-__device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const PagedUnit &u, int h, int rows, int key0, int last_key,
-                                           const int32_t *table, uint8_t *s_mine, float *s_m, float *s_l) {
+__device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const PagedUnit &u, const RowMap &map, int h, int rows, int key0,
+                                           int last_key, const int32_t *table, uint8_t *s_mine, float *s_m, float *s_l) {
     using PT = PrecT<P>;
     using T = typename PT::T;
     constexpr bool B = P == Prec::BF16;
@@ -277,7 +287,7 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
     u32x4 q[NRG][NKK];
 #pragma unroll
     for (int rg = 0; rg < NRG; ++rg) {
-        const int r = u.row + min(16 * rg + r16, rows - 1), token = r / p.group, head = h * p.group + r % p.group;
+        const int r = min(16 * rg + r16, rows - 1), token = map.token(r), head = h * p.group + map.head(r);
         qpos[rg] = u.ctx + token - key0;
         const T *qrow = reinterpret_cast<const T *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + g * VEC;
 #pragma unroll
@@ -443,17 +453,21 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
     }
 }
 
-// Few rows. Workgroup: a block of up to 16 RG rows of one key head and one span of its keys (or every span,
-// one after another). A wave takes a chunk of 64 keys, K straight into registers in operand order, V through
-// LDS (bf16: transposing reads) or straight (fp32); then the workgroup merges the chunks' states. Loads of
-// a workgroup are all in flight at once: 256 KiB at head_dim 128.
-template <Prec P, int HD, int NW, int RG>
-__global__ __launch_bounds__(NW * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p, int cap_units) {
-    constexpr int REGION = span_wave_lds<P, HD, RG>(), SROW = HD + 4, ROWS = 16 * RG;
+// Few rows. Workgroup: a block of up to 16 RG rows of one key head and some spans of its keys, one after
+// another, a wave per chunk of 64 keys: K straight into registers in operand order, V through LDS (bf16:
+// transposing reads) or straight (fp32). The loads of a workgroup are all in flight at once (128 KiB at
+// head_dim 128, and two workgroups per CU); then it merges the chunks' states. A span's state goes to the
+// partials, or, where the request has one span only (fp32: also where the partials do not hold the
+// request's), the rows are written.
+template <Prec P, int HD, int RG>
+__global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
+                                                                                                  int cap_units) {
+    constexpr bool WHOLE = P == Prec::F32;  // several spans without partials
+    constexpr int NW = kSpanChunks, REGION = span_wave_lds<P, HD, RG>(), SROW = HD + 4, ROWS = 16 * RG;
     constexpr int ITEMS = (ROWS * HD / 4 + NW * kWave - 1) / (NW * kWave);
     extern __shared__ u32x4 s_raw[];
     uint8_t *s_all = reinterpret_cast<uint8_t *>(s_raw);
-    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];  // the chunks' statistics
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint8_t *s_mine = s_all + (size_t)w * REGION;
     int count = 0;
@@ -461,71 +475,75 @@ __global__ __launch_bounds__(NW * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) v
     for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
         const int h = idx % p.n_kv;
         const int rows = min(ROWS, u.m * p.group - u.row);
-        const int blast = position_of(u, u.row + rows - 1, p.group);  // the block's last position
+        const RowMap map(p, u.row);
+        const int blast = u.ctx + map.token(rows - 1);  // the block's last position
         const int last_key = u.ctx + u.m - 1;
         const int s0 = u.k0, s1 = min(u.k1, blast / kPagedSpanKeys + 1);
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
-        // the states of this thread's (row, four columns) items: the span's, the row's
-        float Mr[ITEMS], lr[ITEMS];
-        f32x4 orow[ITEMS];
+        // states of this thread's (row, four columns) items over the spans
+        float Mr[WHOLE ? ITEMS : 1], lr[WHOLE ? ITEMS : 1];
+        f32x4 orow[WHOLE ? ITEMS : 1];
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) Mr[i] = -INFINITY, lr[i] = 0.f, orow[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < ITEMS; ++i) Mr[i] = -INFINITY, lr[i] = 0.f, orow[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         for (int s = s0; s < s1; ++s) {
-            float M[ITEMS], l[ITEMS];
-            f32x4 o[ITEMS];
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) M[i] = -INFINITY, l[i] = 0.f, o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int c0 = s * kSpanChunks; c0 < (s + 1) * kSpanChunks && c0 * kKeys <= blast; c0 += NW) {
-                const int key0 = (c0 + w) * kKeys;
-                if (key0 <= blast) {  // uniform over the wave
-                    if (RG == 1 || rows <= 16)
-                        span_chunk<P, HD, 1>(p, u, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
-                    else
-                        span_chunk<P, HD, RG>(p, u, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
-                }
-                __syncthreads();
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
-                    if (row >= rows) break;
-                    const int pos = position_of(u, u.row + row, p.group);
-                    for (int k = 0; k < NW && (c0 + k) * kKeys <= pos; ++k) {
-                        const f32x4 oc = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_all + (size_t)k * REGION) +
-                                                                          row * SROW + col);
-                        float wo, wc;
-                        merge_weights(M[i], s_m[k][row], wo, wc);
-                        l[i] = merge_value(l[i], s_l[k][row], wo, wc);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[i][e] = merge_value(o[i][e], oc[e], wo, wc);
-                    }
-                }
-                __syncthreads();  // before the next chunks come into the regions
+            const int c0 = s * kSpanChunks, key0 = (c0 + w) * kKeys;
+            if (key0 <= blast) {  // uniform over the wave
+                if (RG == 1 || rows <= 16)
+                    span_chunk<P, HD, 1>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                else
+                    span_chunk<P, HD, RG>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
             }
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
                 const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
-                if (row >= rows || s * kPagedSpanKeys > position_of(u, u.row + row, p.group)) continue;
-                if (u.part >= 0) {  // the span's state as it is
-                    const size_t pr = (size_t)(u.part + (s - s0) * u.m * p.group + row) * p.n_kv + h;
-                    *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = o[i];
-                    if (col == 0) {
-                        p.part_m[pr] = M[i];
-                        p.part_l[pr] = l[i];
-                    }
-                } else {
-                    float w0, w1;
-                    merge_weights(Mr[i], M[i], w0, w1);
-                    lr[i] = merge_value(lr[i], l[i], w0, w1);
+                if (row >= rows) break;
+                const int pos = u.ctx + map.token(row);
+                float M = -INFINITY, l = 0.f;
+                f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) orow[i][e] = merge_value(orow[i][e], o[i][e], w0, w1);
+                for (int k = 0; k < NW; ++k) {
+                    if ((c0 + k) * kKeys > pos) break;  // chunks that the row does not see
+                    const f32x4 oc = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_all + (size_t)k * REGION) +
+                                                                      row * SROW + col);
+                    float wo, wc;
+                    merge_weights(M, s_m[k][row], wo, wc);
+                    l = merge_value(l, s_l[k][row], wo, wc);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = merge_value(o[e], oc[e], wo, wc);
                 }
-            }
-        }
-        if (u.part >= 0) continue;
+                if (u.part >= 0) {
+                    const size_t pr = (size_t)(u.part + (s - s0) * u.m * p.group + row) * p.n_kv + h;
+                    *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = o;
+                    if (col == 0) {
+                        p.part_m[pr] = M;
+                        p.part_l[pr] = l;
+                    }
+                    continue;
+                }
+                float Mo = -INFINITY, v, vc;
+                if constexpr (WHOLE) {
+                    if (c0 * kKeys <= pos) {
+                        merge_weights(Mr[i], M, v, vc);
+                        lr[i] = merge_value(lr[i], l, v, vc);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
-            if (row < rows) store_row<P>(p, u.r0, u.row + row, h, col, orow[i], Mr[i], lr[i]);
+                        for (int e = 0; e < 4; ++e) orow[i][e] = merge_value(orow[i][e], o[e], v, vc);
+                    }
+                    if (s + 1 < s1) continue;
+                    Mo = Mr[i];
+                    l = lr[i];
+                    o = orow[i];
+                } else {
+                    merge_weights(Mo, M, v, vc);  // the span into an empty state, as a join does
+                    l = merge_value(0.f, l, v, vc);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = merge_value(0.f, o[e], v, vc);
+                }
+                store_row<P>(p, u.r0 + map.token(row), h * p.group + map.head(row), col, o, Mo, l);
+            }
+            __syncthreads();  // before the next chunks come into the regions
         }
     }
 }
@@ -568,12 +586,12 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
         const int rows = min(kPagedTileRows, u.m * p.group - u.row);
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
         const int kvlen = u.ctx + u.m, last_tile = (kvlen - 1) >> 4;
-        const int tfirst = position_of(u, u.row, p.group), tlast = position_of(u, u.row + rows - 1, p.group);
-        const int wfirst = position_of(u, u.row + min(32 * w, rows - 1), p.group);
-        const int wlast = position_of(u, u.row + min(32 * w + 31, rows - 1), p.group);
+        const RowMap map(p, u.row);
+        const int tfirst = u.ctx + map.token(0), tlast = u.ctx + map.token(rows - 1);
+        const int wfirst = u.ctx + map.token(min(32 * w, rows - 1)), wlast = u.ctx + map.token(min(32 * w + 31, rows - 1));
         const int c0 = u.k0, c1 = min(u.k1, tlast / kKeys + 1);
         const bool live = 32 * w < rows;  // uniform over the wave
-        const int rr = u.row + min(32 * w + r32, rows - 1), token = rr / p.group, head = h * p.group + rr % p.group;
+        const int rr = min(32 * w + r32, rows - 1), token = map.token(rr), head = h * p.group + map.head(rr);
         const int qpos = u.ctx + token;
         // page ids of the 64 tiles of 16 keys from tile 64 j on, one per lane
         auto page_ids = [&](int j) { return table[(min(64 * j + lane, last_tile) << 4) >> shift]; };
@@ -652,7 +670,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                         for (int r0 = 0; r0 < kPagedTileRows; r0 += 16) {
                             uint32_t bits = 0;
                             for (int r = r0; r < r0 + 16; ++r) {
-                                const int last = min(position_of(u, u.row + min(r, rows - 1), p.group) - key0, kKeys - 1);
+                                const int last = min(u.ctx + map.token(min(r, rows - 1)) - key0, kKeys - 1);
                                 while (key <= last) next();
                                 bits |= (acc != acc ? 3u : acc == INFINITY ? 1u : acc == -INFINITY ? 2u : 0u) << (2 * (r - r0));
                             }
@@ -746,7 +764,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                     if (u.part >= 0)
                         *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = x;
                     else
-                        store_row<Prec::BF16>(p, u.r0, u.row + row, h, col, x, M, l);
+                        store_row<Prec::BF16>(p, u.r0 + token, head, col, x, M, l);
                 }
             if (u.part >= 0 && hb == 0) {
                 p.part_m[pr] = M;
@@ -775,20 +793,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int 
 
 namespace {
 
-// NW: waves, as many chunks at a time; RG: groups of 16 rows of a block, as paged_block_rows() says.
-template <Prec P, int HD, int NW, int RG>
+template <Prec P, int HD, int RG>
 hipError_t launch_spans(int64_t units, const PagedAttnParams &p, hipStream_t s) {
-    constexpr int lds = NW * span_wave_lds<P, HD, RG>();
-    static_assert(lds + NW * RG * 16 * 8 <= 160 * 1024, "the LDS of a CU");
+    constexpr int lds = kSpanChunks * span_wave_lds<P, HD, RG>();
+    static_assert(lds + 4096 <= 160 * 1024, "the LDS of a CU");
     static_assert(16 * RG == paged_block_rows(P == Prec::BF16, HD), "the plan's row blocks");
     const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs));
-    hipLaunchKernelGGL((paged_span_kernel<P, HD, NW, RG>), grid, dim3(NW * kWave), lds, s, p, p.bk.cap_units);
+    hipLaunchKernelGGL((paged_span_kernel<P, HD, RG>), grid, dim3(kSpanChunks * kWave), lds, s, p, p.bk.cap_units);
     return hipGetLastError();
 }
 
-template <Prec P, int HD, int NW, int RG>
+template <Prec P, int HD, int RG>
 hipError_t launch_shape(int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
-    hipError_t e = launch_spans<P, HD, NW, RG>(units, p, s);
+    hipError_t e = launch_spans<P, HD, RG>(units, p, s);
     if (e != hipSuccess) return e;
     if constexpr (P == Prec::BF16) {
         if (tiles > 0)
@@ -810,15 +827,15 @@ hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join,
     if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0 || tiles < 0) return hipErrorInvalidValue;
     if (units + tiles == 0 || p.rows == 0) return hipSuccess;
     if (bf16) {
-        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 4, 1>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 2>(units, tiles, join, p, s);
+        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 1>(units, tiles, join, p, s);
     } else {
-        if (p.hd == 16) return launch_shape<Prec::F32, 16, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 32) return launch_shape<Prec::F32, 32, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::F32, 64, 4, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::F32, 128, 4, 1>(units, tiles, join, p, s);
+        if (p.hd == 16) return launch_shape<Prec::F32, 16, 2>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::F32, 32, 2>(units, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::F32, 64, 2>(units, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::F32, 128, 1>(units, tiles, join, p, s);
     }
     return hipErrorInvalidValue;
 }

@@ -25,7 +25,7 @@ struct cllm_paged {
     float *rcos = nullptr, *rsin = nullptr;  // null without rotation
     float *part_o = nullptr, *part_m = nullptr, *part_l = nullptr;
     bool tiled = false;  // long chunks take tiles
-    int block_rows = 32, cap_part = 0;
+    int block_rows = 32, cap_part = 0, cap_tile_part = 0;
     void *own = nullptr;  // library-allocated workspace
     bool planned = false, dead = false;
     int n = 0, rows = 0, max_new = 0, max_len = 0;  // the last plan's bounds
@@ -105,24 +105,24 @@ std::vector<Buf> buffers(cllm_paged *c) {
     bk.n_pages = f.n_pages;
     bk.page_shift = __builtin_ctz((unsigned)f.page_size);
     // Attention units: row blocks and tiles of any plan, and what splitting adds (kPagedUnits /
-    // n_kv_heads row blocks, twice kPagedTileGroups / n_kv_heads tiles, about). Partial states: of the spans
-    // of the pool and one of each request, for requests of few rows; split tiles. A plan that needs more is not
-    // split.
+    // n_kv_heads row blocks, kPagedTileGroups / n_kv_heads tiles, about). Partial states of row blocks: a request
+    // of few rows has up to kPagedFewRows in each of its spans, which are those of the pool and one more each
+    // (every bf16 plan; fp32 chunks of more rows may need more, and are then not split). Of tiles: as many
+    // rows as split tiles have.
     c->tiled = c->bf16;
     c->block_rows = paged_block_rows(c->bf16, f.head_dim);
     const int64_t nrows = (int64_t)f.max_rows * c->group;
     const int64_t few = kPagedUnits / f.n_kv_heads + 1, few_tiles = 2 * (kPagedTileGroups / f.n_kv_heads + 1);
     const int64_t blocks = nrows / c->block_rows + f.max_seqs, tiles = c->tiled ? nrows / kPagedTileRows + f.max_seqs : 0;
     const int64_t spans = (f.max_ctx + kPagedSpanKeys - 1) / kPagedSpanKeys;
-    const int64_t pool = std::min(((int64_t)f.n_pages * f.page_size + kPagedSpanKeys - 1) / kPagedSpanKeys + f.max_seqs,
-                                  f.max_seqs * spans);
+    const int64_t pool = std::min((int64_t)f.n_pages * f.page_size / kPagedSpanKeys + f.max_seqs, f.max_seqs * spans);
     bk.cap_units = (int)(blocks + few);
     bk.cap_tiles = (int)(tiles + few_tiles);
-    bk.cap_items = (int)std::min(nrows / kPagedItemRows + f.max_seqs, few + 4 * few_tiles + f.max_seqs);
-    c->cap_part = (int)std::min<int64_t>(std::min(nrows, kPagedFewRows * (int64_t)f.max_seqs) * std::min(spans, pool), INT32_MAX / 4);
-    c->cap_part = (int)std::min<int64_t>(c->cap_part, kPagedFewRows * pool) + (int)(few_tiles * kPagedTileRows);
+    bk.cap_items = (int)(nrows / kPagedItemRows + f.max_seqs);
+    c->cap_part = (int)std::min(kPagedFewRows * pool, nrows * spans);
+    c->cap_tile_part = c->tiled ? (int)std::min(few_tiles * kPagedTileRows, nrows * spans) : 0;
     auto P = [](auto **q) { return reinterpret_cast<void **>(q); };
-    const size_t part = (size_t)c->cap_part * f.n_kv_heads;
+    const size_t part = ((size_t)c->cap_part + c->cap_tile_part) * f.n_kv_heads;
     std::vector<Buf> b{
         {P(&bk.status), PS_WORDS * 4},
         {P(&bk.table), (size_t)f.max_seqs * bk.max_pages * 4},
@@ -307,6 +307,7 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
     p.tiled = c->tiled;
     p.block_rows = c->block_rows;
     p.cap_part = c->cap_part;
+    p.cap_tile_part = c->cap_tile_part;
     HIPCHK(c, launch_paged_plan(p, c->stream));
     c->planned = true;
     c->n = n;
@@ -393,6 +394,7 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     p.n_kv = f.n_kv_heads;
     p.hd = f.head_dim;
     p.group = c->group;
+    p.group_inv = ((1u << 24) + c->group - 1) / c->group;
     const double sc = scale == 0.0f ? 1.0 / std::sqrt((double)f.head_dim) : (double)scale;
     p.scale_log2 = (float)(1.4426950408889634 * sc);
     // bounds of the launch
