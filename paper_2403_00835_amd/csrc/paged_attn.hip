@@ -55,6 +55,13 @@ __device__ __forceinline__ u32x2 read_tr(const uint8_t *lds) {
                                          (__attribute__((address_space(3))) s16x4 *)lds));
 }
 
+// Two values rounded to bf16 (nearest even), the first in the low half: one instruction.
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
 // Base-2 exponential of a value <= 0 (or NaN): the hardware instruction, results below 2^-126 are 0,
 // which a softmax weight may lose.
 __device__ __forceinline__ float exp2_weight(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -148,29 +155,19 @@ __device__ __forceinline__ f32x4 v_product(const u32x4 (&vb)[N], const u32x4 (&p
 // Sixteen weights of a lane as MFMA operands (bf16: hi and lo planes).
 template <Prec P, int NPL, int N>
 __device__ __forceinline__ void weight_operand(const f32x4 (&st)[4], u32x4 (&pb)[NPL][N]) {
-    if constexpr (P == Prec::BF16) {
 #pragma unroll
-        for (int x = 0; x < N; ++x) {
-            const f32x4 pa = st[2 * x], pc = st[2 * x + 1];
-            const float pv[8] = {pa[0], pa[1], pa[2], pa[3], pc[0], pc[1], pc[2], pc[3]};
-            uint32_t hi[8], lo[8];
+    for (int x = 0; x < N; ++x)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hi[i] = f2bf(pv[i]);
-                lo[i] = f2bf(pv[i] - bf2f((uint16_t)hi[i]));
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                pb[0][x][i] = hi[2 * i] | (hi[2 * i + 1] << 16);
-                if constexpr (NPL == 2) pb[NPL - 1][x][i] = lo[2 * i] | (lo[2 * i + 1] << 16);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (P == Prec::BF16) {
+                const float a = st[2 * x + i / 2][2 * (i % 2)], b = st[2 * x + i / 2][2 * (i % 2) + 1];
+                const uint32_t hi = pack_bf16(a, b);
+                pb[0][x][i] = hi;
+                pb[NPL - 1][x][i] = pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+            } else {
+                pb[0][x][i] = __float_as_uint(st[x][i]);
             }
         }
-    } else {
-#pragma unroll
-        for (int x = 0; x < N; ++x)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pb[0][x][i] = __float_as_uint(st[x][i]);
-    }
 }
 
 // Rows of a unit, from its first: row j is token(j) of the chunk, head(j) of the group. The quotient of the
@@ -552,7 +549,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return (uint32_t)f2bf(a) | ((uint32_t)f2bf(b) << 16); }
 
 // LDS of the tile kernel: two buffers of a chunk's K and V, and the classes of values that are not finite.
 template <int HD>
@@ -577,6 +573,16 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
     uint32_t *s_cls = reinterpret_cast<uint32_t *>(s_kv + 4 * TL::BYTES);  // [column][16 rows]
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r32 = lane & 31, hb = lane >> 5, shift = p.bk.page_shift;
+    // This lane's place in a wave's loads: 1 KiB of 16 keys, whose permutations repeat (a wave takes every
+    // fourth KiB: the same one of every 16 keys, or two in turn).
+    constexpr int LPT = 16 / TL::RPK, VAR = LPT > 4 ? LPT / 4 : 1;  // loads of 16 keys
+    uint32_t koff[VAR], voff[VAR];
+#pragma unroll
+    for (int i = 0; i < VAR; ++i) {
+        const int key = (w + 4 * i) % LPT * TL::RPK + lane / (kWave / TL::RPK), piece = lane % TL::NC;
+        koff[i] = key * TL::ROWB + (piece ^ TL::kswz(key)) * 16;
+        voff[i] = key * TL::ROWB + (piece ^ TL::vswz(key)) * 16;
+    }
     const float scale = fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;  // the scale's sign goes into the queries
     int count = 0;
@@ -603,18 +609,17 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                 pg_next = page_ids(pj + 1);
             }
 #pragma unroll
-            for (int i = 0; i < TL::KIB / 2; ++i) {
-                const int blk = w + 4 * i, isv = blk >= TL::KIB, kb = isv ? blk - TL::KIB : blk;
-                const int key = kb * TL::RPK + lane / (kWave / TL::RPK);  // within the chunk
-                const int tile = 4 * c + kb * TL::RPK / 16;
-                const int page = __builtin_amdgcn_readlane(pg, tile & 63);
-                const int off = ((min(tile, last_tile) << 4) & ((1 << shift) - 1)) + (key & 15);
-                const int piece = (lane % TL::NC) ^ (isv ? TL::vswz(key) : TL::kswz(key));
-                const uint8_t *src = reinterpret_cast<const uint8_t *>(isv ? p.v_pages : p.k_pages) +
-                                     ((((size_t)page * p.n_kv + h) << shift) + off) * TL::ROWB + piece * 16;
+            for (int i = 0; i < TL::KIB / 4; ++i) {
+                const int kb = w + 4 * i, tile = 4 * c + kb / LPT;
+                const size_t page = __builtin_amdgcn_readlane(pg, tile & 63);
+                const size_t base = (((page * p.n_kv + h) << shift) + ((min(tile, last_tile) << 4) & ((1 << shift) - 1))) * TL::ROWB;
+                uint8_t *dst = s_kv + (size_t)buf * 2 * TL::BYTES + kb * 1024;
                 __builtin_amdgcn_global_load_lds(
-                    static_cast<const void *>(src),
-                    (__attribute__((address_space(3))) void *)(s_kv + (size_t)buf * 2 * TL::BYTES + blk * 1024), 16, 0, 0);
+                    static_cast<const void *>(static_cast<const uint8_t *>(p.k_pages) + base + koff[i % VAR]),
+                    (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+                __builtin_amdgcn_global_load_lds(
+                    static_cast<const void *>(static_cast<const uint8_t *>(p.v_pages) + base + voff[i % VAR]),
+                    (__attribute__((address_space(3))) void *)(dst + TL::BYTES), 16, 0, 0);
             }
         };
         __syncthreads();  // the unit before is done with the buffers
@@ -692,17 +697,37 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                 }
             }
             if (!live || key0 > wlast) continue;
+            // Reads run ahead of the products that take them (the scheduler would put each next to its
+            // product, behind a wait for it alone).
+            u32x4 kf[NKK][2];
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+                    kf[kk][kt] = *reinterpret_cast<const u32x4 *>(K + (32 * kt + r32) * TL::ROWB + ((2 * kk + hb) ^ TL::kswz(r32)) * 16);
+            __builtin_amdgcn_sched_barrier(0);
             f32x16 st[2];
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
+            for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
-                const int key = 32 * kt + r32;
 #pragma unroll
-                for (int kk = 0; kk < NKK; ++kk)
-                    st[kt] = mfma32(*reinterpret_cast<const u32x4 *>(K + key * TL::ROWB + ((2 * kk + hb) ^ TL::kswz(r32)) * 16), q[kk],
-                                    st[kt]);
-            }
+            for (int kk = 0; kk < NKK; ++kk)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) st[kt] = mfma32(kf[kk][kt], q[kk], st[kt]);
+            // slot j of half hb of step ks: key 16 ks + 8 (j / 4) + 4 hb + j % 4
+            const int vkey = 4 * hb + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            u32x2 vf[2][4][2];
+            auto read_v = [&](int dt) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        vf[dt & 1][ks][y] = read_tr(V + vkey * TL::ROWB + ((4 * dt + vc) ^ TL::vswz(vkey)) * 16 + (lane & 1) * 8 +
+                                                    (16 * ks + 8 * y) * TL::ROWB);
+            };
+            read_v(0);
+            __builtin_amdgcn_sched_barrier(0);
             // st[kt][i] = S^T[key 32 kt + 8 (i / 4) + 4 hb + i % 4][row r32]
             if (key0 + kKeys - 1 > wfirst) {
 #pragma unroll
@@ -737,19 +762,18 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                     l += a + b;
                     pb[2 * kt + i / 8][i / 2 % 4] = pack_bf16(a, b);
                 }
-            // slot j of half hb of step ks: key 16 ks + 8 (j / 4) + 4 hb + j % 4
-            const int vkey = 4 * hb + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt)
+            for (int dt = 0; dt < NDT; ++dt) {
+                if (dt + 1 < NDT) {
+                    read_v(dt + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) {
-                    u32x2 x[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        x[y] = read_tr(V + vkey * TL::ROWB + ((4 * dt + vc) ^ TL::vswz(vkey)) * 16 + (lane & 1) * 8 +
-                                       (16 * ks + 8 * y) * TL::ROWB);
-                    o[dt] = mfma32(u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}, pb[ks], o[dt]);
+                    const u32x2 x = vf[dt & 1][ks][0], y = vf[dt & 1][ks][1];
+                    o[dt] = mfma32(u32x4{x[0], x[1], y[0], y[1]}, pb[ks], o[dt]);
                 }
+            }
         }
         l += __shfl_xor(l, 32);
         const int row = 32 * w + r32;
