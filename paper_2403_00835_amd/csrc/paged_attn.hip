@@ -355,11 +355,20 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
                     load_words<W>(x, reinterpret_cast<const float *>(p.v_pages) + at[kt] + (4 * g + v) * HD +
                                          Cols<P, HD>::vcol(dt, r16));
 #pragma unroll
-                    for (int y = 0; y < W; ++y) {
-                        const bool use = 16 * kt + 4 * g + v < valid && !(taken && (x[y] & 0x7f800000u) == 0x7f800000u);
-                        vb[y][kt][v] = use ? x[y] : 0u;
-                    }
+                    for (int y = 0; y < W; ++y) vb[y][kt][v] = x[y];
                 }
+            if (valid < kKeys || taken) {  // uniform: values to leave out
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int y = 0; y < W; ++y) {
+                            const uint32_t x = vb[y][kt][v];
+                            const bool use = 16 * kt + 4 * g + v < valid && !(taken && (x & 0x7f800000u) == 0x7f800000u);
+                            vb[y][kt][v] = use ? x : 0u;
+                        }
+            }
         }
     };
     f32x4 oc[NRG][NDT];
@@ -741,7 +750,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[kt][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * scale;
             if (__any(mx > M + 8.f)) {
                 const float Mn = fmaxf(M, mx), f = M == -INFINITY ? 0.f : exp2_weight(M - Mn);
                 l *= f;
