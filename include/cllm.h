@@ -415,7 +415,7 @@ cllm_status cllm_timing_read(cllm_ctx *ctx, int64_t *launches, double *total_ms)
  * cllm_paged_workspace_bytes() bytes (books, rotary factors, attention partials); it need not be zero.
  *
  * Work is queued on the stream given at creation; calls on one cache share its books and partials, so
- * whatever runs them (this thread, replayed graphs) is ordered by that stream. Calls may be made
+ * whatever runs them (calls, replayed graphs) is ordered by that stream. A cache is not thread-safe. Calls may be made
  * with any device current. Each array is memory that the cache's GPU can access (checked, else
  * ERR_ARG); rows and pools are 16-byte aligned with row strides (in elements) of whole 16-byte
  * vectors, the heads of a row contiguous. Sizes are not checked: an array of rows holds the plan's

@@ -17,6 +17,7 @@ constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
 constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
 constexpr int kAllSpans = 1 << 30;
+constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cache
 constexpr int kPagedTileGroups = 512;   // workgroups that tiles of few requests are split into, about
 
 // Words of the status block, written by the plan.

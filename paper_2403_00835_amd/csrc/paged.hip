@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     const int nrb = tiled ? 0 : (T0 + p.block_rows - 1) / p.block_rows;
     const int ntile = tiled ? (T0 + kPagedTileRows - 1) / kPagedTileRows : 0;
     const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
-    int v[6] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)1 << 20)}, total[6];
+    int v[6] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)kPartRows)}, total[6];
     block_scan(v, total, s_wave);
     const int R = total[0], G = total[1], T = total[2];
     if (R > p.rows) flags |= PF_ROWS;
@@ -166,8 +166,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     const int ranges = total[4] > 0 ? (kPagedTileGroups + total[4] * p.n_kv - 1) / (total[4] * p.n_kv) : 1;
     const int nr = ntile ? min(ranges, spans) : 1, items = (T0 + kPagedItemRows - 1) / kPagedItemRows;
     const bool dparts = nrb && spans > 1, tparts = nr > 1;
-    int x[6] = {nrb * ((spans + per - 1) / per), dparts ? items : 0, dparts ? (int)min((int64_t)spans * T0, (int64_t)1 << 20) : 0,
-                ntile * nr, tparts ? items : 0, tparts ? nr * T0 : 0}, y[6];
+    // (an fp32 chunk of 2^20 or more partial rows asks for more than there can be, and nothing is split)
+    const int64_t want = (int64_t)spans * T0;
+    const int few = want < kPartRows ? (spans + per - 1) / per : 1;
+    int x[6] = {nrb * few, dparts ? items : 0, dparts ? (int)min(want, (int64_t)kPartRows) : 0, ntile * nr, tparts ? items : 0,
+                tparts ? nr * T0 : 0}, y[6];
     block_scan(x, y, s_wave2);
     const bool dsplit = y[0] <= bk.cap_units && y[2] <= p.cap_part, tsplit = y[3] <= bk.cap_tiles && y[5] <= p.cap_tile_part;
     const int U = dsplit ? y[0] : total[3], UT = tsplit ? y[3] : total[4];

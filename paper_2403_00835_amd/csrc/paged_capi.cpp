@@ -120,6 +120,7 @@ std::vector<Buf> buffers(cllm_paged *c) {
     bk.cap_tiles = (int)(tiles + few_tiles);
     bk.cap_items = (int)(nrows / kPagedItemRows + f.max_seqs);
     c->cap_part = (int)std::min(kPagedFewRows * pool, nrows * spans);
+    if (!c->bf16) c->cap_part = std::min(c->cap_part, kPartRows - 1);
     c->cap_tile_part = c->tiled ? (int)std::min(few_tiles * kPagedTileRows, nrows * spans) : 0;
     auto P = [](auto **q) { return reinterpret_cast<void **>(q); };
     const size_t part = ((size_t)c->cap_part + c->cap_tile_part) * f.n_kv_heads;

@@ -292,6 +292,7 @@ ATTN = [  # dtype, heads, kv heads, head dim, page, contexts, new tokens
     ("bf16", 4, 4, 32, 64, [20], [200]), ("bf16", 2, 1, 256, 64, [65], [140]), ("bf16", 16, 1, 128, 128, [5, 600, 90], [4, 5, 128]),
     ("bf16", 1, 1, 128, 64, [0], [129]), ("bf16", 32, 8, 128, 64, [1500], [40]), ("bf16", 2, 2, 128, 16, [0, 3000], [640, 100]),
     ("bf16", 8, 1, 32, 16, [2500, 10], [9, 1]), ("bf16", 6, 2, 256, 64, [1300, 0, 7], [30, 500, 2]),
+    ("bf16", 64, 1, 64, 16, [300, 0], [1, 3]), ("f32", 2, 2, 64, 64, [900], [130]),
     ("f32", 4, 4, 16, 16, [16], [8]), ("f32", 12, 12, 64, 32, [5, 700, 301], [41, 3, 17]), ("f32", 4, 1, 128, 64, [1030, 1], [30, 1]),
     ("f32", 6, 2, 32, 16, [0, 15], [130, 1]), ("f32", 2, 2, 128, 256, [513], [70])]
 
@@ -308,9 +309,11 @@ def test_attention(binding, case):
     books.plan(seq, half, [0] * n)
     c.plan(ints(seq), ints(half), ints([0] * n), rows=0)
     check_attn(c, books, seq, ctx, new, seed=hd + n)
-    # the tightest bounds, strided rows, another scale
-    check_attn(c, books, seq, ctx, new, seed=hd, scale=-0.11, strided=True,
-               bounds=dict(max_new=max(new), max_len=max(total)))
+    # the tightest bounds, strided rows, another scale; then in place: the same bits
+    q, kp, vp, out, _ = check_attn(c, books, seq, ctx, new, seed=hd, scale=-0.11, strided=True,
+                                     bounds=dict(max_new=max(new), max_len=max(total)))
+    c.attn(q, kp, vp, q, scale=-0.11)
+    assert torch.equal(q[:sum(new)], out[:sum(new)])
 
 
 @pytest.mark.parametrize("dtype,heads,kv,hd,ctx,m", [("bf16", 4, 4, 128, 500, 40), ("bf16", 8, 2, 64, 70, 16),
