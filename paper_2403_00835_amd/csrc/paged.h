@@ -8,17 +8,26 @@ namespace cllm {
 constexpr int kPagedMaxSeqs = 1024;   // one plan thread per request
 // Rows of a request's attention: new tokens x heads of a group. Requests of few rows (a token, a Jacobi
 // block), and fp32, take units of paged_block_rows() rows and spans of keys; longer bf16 chunks take tiles
-// of kPagedTileRows rows and a range of keys.
+// of kPagedTileRows rows and a range of keys. Up to 64 a row's bits are those of a plan of its own, as every
+// block length needs; tiles of 33 rows at 600 keys take 16.3 us in place of 14.7 (32 heads of 128), 16
+// requests of 64 rows at 1000 keys 65 in place of 72.
 constexpr int kPagedFewRows = 64;
 constexpr int kPagedTileRows = 128;
 constexpr int kPagedItemRows = 32;    // rows that are joined together
 // A wave holds a chunk of keys in registers beside its rows: of 512-byte keys, half the rows.
 constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >= 512 ? 16 : 32; }
+// Where bf16 requests of few, but more than kPagedWaveRows rows make kPagedTileGroups workgroups or more, a
+// workgroup takes a whole request: its keys once for all rows, no partial states. 64 requests of 36 rows at 4000
+// keys (8 key heads of 128): 400 us in spans, 205 whole; 16 of 64 rows at 1000 keys (32 heads): 144 and 72; of
+// 32 rows: 85 and 61. Up to 16 rows spans read the keys once too, and do not wait for the longest request: a
+// token of 64 requests at 1000 to 8000 keys takes 229 us in spans, 284 whole (4 tokens at 4000: 232 and 199).
+constexpr int kPagedWaveRows = 16;
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
 constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
 constexpr int kAllSpans = 1 << 30;
 constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cache
-constexpr int kPagedTileGroups = 512;   // workgroups that tiles of few requests are split into, about
+constexpr int kPagedTileGroups = 512;   // workgroups that fill the device (two a CU): tiles of few requests are split into
+                                        // about as many
 
 // Words of the status block, written by the plan.
 enum PagedStatus {
@@ -39,7 +48,8 @@ enum PagedFlags { PF_ARG = 1, PF_ROWS = 2, PF_PAGES = 4 };
 struct alignas(16) PagedUnit {
     int slot, ctx, m, r0;  // the request: slot, context, new tokens, first row of the plan
     int row;               // first row of the block or tile
-    int k0, k1;            // row blocks: spans [k0, k1), kAllSpans: to the last; tiles: chunks [k0, k1)
+    int k0, k1;            // row blocks: spans [k0, k1), kAllSpans: to the last, k0 -1: the whole request, all rows
+                           // and keys; tiles: chunks [k0, k1)
     int part;              // partial row of the first row (row blocks: in span k0), or -1: none, the output is written
 };
 struct alignas(16) PagedItem {
@@ -114,6 +124,6 @@ hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s);
 hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_t s);
 // Upper bounds of the plan's units and tiles; join: some may be split.
-hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s);
+hipError_t launch_paged_attn(bool bf16, int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s);
 
 }  // namespace cllm

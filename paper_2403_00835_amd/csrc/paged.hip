@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kPlanThreads = kPagedMaxSeqs;  // at most; blockDim.x, a multiple of 256 and at least the requests
 constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kMany = 1 << 16;  // above a plan's bf16 row blocks
 static_assert(kPlanThreads == 1024 && kPlanWaves == 16, "one thread per request, one row of lanes for the waves' sums");
 
 // Inclusive prefix sum over a row of 16 lanes, over a wave: lane moves in the ALU (a step through LDS
@@ -142,10 +143,16 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     const int T0 = m * p.group;  // rows of the request's attention
     const bool tiled = p.tiled && T0 > kPagedFewRows;
     const int nrb = tiled ? 0 : (T0 + p.block_rows - 1) / p.block_rows;
+    const bool many = p.tiled && !tiled && T0 > kPagedWaveRows;
     const int ntile = tiled ? (T0 + kPagedTileRows - 1) / kPagedTileRows : 0;
     const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
-    int v[6] = {m, max(own - need, 0), max(need - own, 0), nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)kPartRows)}, total[6];
+    // (bf16 row blocks, at most 4 each, take 13 bits: above them the number of requests that may be taken whole)
+    int v[6] = {m, max(own - need, 0), max(need - own, 0), many ? nrb + kMany : nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)kPartRows)},
+        total[6];
     block_scan(v, total, s_wave);
+    const int wholes = p.tiled ? total[3] / kMany : 0;
+    total[3] -= wholes * kMany;
+    if (p.tiled) v[3] %= kMany;
     const int R = total[0], G = total[1], T = total[2];
     if (R > p.rows) flags |= PF_ROWS;
     if (T > free0 + G) flags |= PF_PAGES;
@@ -165,11 +172,15 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     const int per = max((int)(((int64_t)total[5] * p.n_kv + kPagedUnits - 1) / kPagedUnits), 1);
     const int ranges = total[4] > 0 ? (kPagedTileGroups + total[4] * p.n_kv - 1) / (total[4] * p.n_kv) : 1;
     const int nr = ntile ? min(ranges, spans) : 1, items = (T0 + kPagedItemRows - 1) / kPagedItemRows;
-    const bool dparts = nrb && spans > 1, tparts = nr > 1;
+    // Whole requests, without partials: see kPagedWaveRows. None is taken whole where one has more than twice the
+    // mean keys and would be worked on alone at the end.
+    const bool late = many && (int64_t)spans * total[3] > 2 * (int64_t)total[5];
+    const bool whole = wholes * p.n_kv >= kPagedTileGroups && !__syncthreads_or(late) && many;  // (uniform but for the last)
+    const bool dparts = nrb && spans > 1 && !whole, tparts = nr > 1;
     // (an fp32 chunk of 2^20 or more partial rows asks for more than there can be, and nothing is split)
     const int64_t want = (int64_t)spans * T0;
     const int few = want < kPartRows ? (spans + per - 1) / per : 1;
-    int x[6] = {nrb * few, dparts ? items : 0, dparts ? (int)min(want, (int64_t)kPartRows) : 0, ntile * nr, tparts ? items : 0,
+    int x[6] = {whole ? 1 : nrb * few, dparts ? items : 0, dparts ? (int)min(want, (int64_t)kPartRows) : 0, ntile * nr, tparts ? items : 0,
                 tparts ? nr * T0 : 0}, y[6];
     block_scan(x, y, s_wave2);
     const bool dsplit = y[0] <= bk.cap_units && y[2] <= p.cap_part, tsplit = y[3] <= bk.cap_tiles && y[5] <= p.cap_tile_part;
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     s_tile[b] = tsplit ? x[3] : v[4];
     s_item[b] = (dsplit ? x[1] : 0) + (tsplit ? x[4] : 0);
     s_part[b] = dparts && dsplit ? x[2] : tparts && tsplit ? p.cap_part + x[5] : -1;
-    s_ranges[b] = !ntile ? 0 : tsplit ? nr : 1;
+    s_ranges[b] = !ntile ? (whole && dsplit ? -1 : 0) : tsplit ? nr : 1;
     if (b == 0) {  // behind the last thread's
         const int end = blockDim.x;
         s_rows[end] = R;
@@ -241,6 +252,10 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     if (U > 0)
         for_items<1>(s_unit, n, U, [&](int e, int i) {
             const int rows = s_m[e] * p.group, blocks = (rows + p.block_rows - 1) >> row_shift, part = s_part[e];
+            if (s_ranges[e] < 0) {
+                bk.units[i] = PagedUnit{s_seq[e], s_ctx[e], s_m[e], s_rows[e], 0, -1, kAllSpans, -1};
+                return;
+            }
             // the blocks of the same spans next to each other: they read the same keys
             int k0 = i - s_unit[e], row = 0;
             if (blocks > 1) {

@@ -46,13 +46,33 @@ struct Tile {
     }
 };
 
+// Transposing reads of 16 columns of V: lane (g, r) of an instruction addresses key 4 g + r / 4 of 16 keys and
+// 8 bytes of columns 4 (r % 4) .., and receives column r of keys 4 g .. 4 g + 3.
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-// Four keys 4 g .. 4 g + 3 (of 16) of one column: lane (g, r) addresses key 4 g + r / 4, columns
-// 4 (r % 4) .., of a 16-column tile and receives column r.
 __device__ __forceinline__ u32x2 read_tr(const uint8_t *lds) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                          (__attribute__((address_space(3))) s16x4 *)lds));
+}
+// Four of them at a, four at b, B bytes apart, and their wait in one block: the compiler takes the intrinsic
+// to read what LDS DMA in flight writes, wherever that goes, and would wait for all of it first.
+template <int B>
+__device__ __forceinline__ void read_tr8(uint32_t a, uint32_t b, u32x2 (&v)[8]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n"
+        "ds_read_b64_tr_b16 %1, %8 offset:%10\n"
+        "ds_read_b64_tr_b16 %2, %8 offset:%11\n"
+        "ds_read_b64_tr_b16 %3, %8 offset:%12\n"
+        "ds_read_b64_tr_b16 %4, %9\n"
+        "ds_read_b64_tr_b16 %5, %9 offset:%10\n"
+        "ds_read_b64_tr_b16 %6, %9 offset:%11\n"
+        "ds_read_b64_tr_b16 %7, %9 offset:%12\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+        : "v"(a), "v"(b), "n"(B), "n"(2 * B), "n"(3 * B)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)p;
 }
 
 // Two values rounded to bf16 (nearest even), the first in the low half: one instruction.
@@ -123,22 +143,26 @@ __device__ __forceinline__ void load_words(uint32_t (&x)[W], const float *src) {
         x[0] = *reinterpret_cast<const uint32_t *>(src);
 }
 
-// The V operand of one output tile: vb[x] holds the keys of the probabilities' registers (bf16: x = 0, 1, keys
-// 32 x + 4 g + (0..3) and 32 x + 16 + 4 g + (0..3)), from LDS.
+// The V operands of output tiles dt and dt + 1: vb[y][x] holds the keys of the probabilities' registers (bf16:
+// x = 0, 1, keys 32 x + 4 g + (0..3) and 32 x + 16 + 4 g + (0..3)), from LDS.
 template <int HD>
-__device__ __forceinline__ void v_operand(const uint8_t *V, int dt, int lane, u32x4 (&vb)[2]) {
+__device__ __forceinline__ void v_operands(const uint8_t *V, int dt, int lane, u32x4 (&vb)[2][2]) {
     using TL = Tile<HD>;
-    const int g = lane >> 4, r16 = lane & 15;
+    constexpr int B = 16 * TL::ROWB;  // of 16 keys, whose permutations repeat
+    const int g = lane >> 4, r16 = lane & 15, key = 4 * g + (r16 >> 2);
+    uint32_t at[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        u32x2 h[2];
+    for (int y = 0; y < 2; ++y)  // the permutation moves 32-byte pairs
+        at[y] = lds_address(V) + key * TL::ROWB + ((2 * (dt + y) + ((r16 & 3) >> 1)) ^ TL::vswz(key)) * 16 + (r16 & 1) * 8;
+    u32x2 h[8];
+    read_tr8<B>(at[0], at[1], h);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int key = 4 * g + (r16 >> 2), c = 2 * dt + ((r16 & 3) >> 1);  // of 16 keys, whose permutations repeat
-            h[y] = read_tr(V + key * TL::ROWB + (c ^ TL::vswz(key)) * 16 + (r16 & 1) * 8 + (32 * x + 16 * y) * TL::ROWB);
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const u32x2 lo = h[4 * y + 2 * x], hi = h[4 * y + 2 * x + 1];
+            vb[y][x] = u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
-        vb[x] = u32x4{h[0][0], h[0][1], h[1][0], h[1][1]};
-    }
 }
 
 // One 16-column tile of V^T P^T from operands vb and the probabilities' operands pb.
@@ -266,6 +290,119 @@ constexpr int span_wave_lds() {
     return state > v ? state : v;
 }
 
+constexpr int class_words(int hd) { return (hd + kWave - 1) / kWave; }
+
+// The product of a chunk's weights pb (of NRG groups of 16 rows) with its values (bf16: in LDS; fp32: from
+// memory, at[]: the first elements of its four tiles of 16 keys). valid: keys of the chunk that the request
+// has (behind them a page holds whatever it did before), kKeys where the others have been cleared; qpos: the lane's rows' positions in the chunk. Says
+// whether the classes cls are to be added to the result.
+template <Prec P, int HD, int NRG, int N, int NPL>
+__device__ __forceinline__ bool chunk_values(const PagedAttnParams &p, const uint8_t *V, const size_t (&at)[4], int valid,
+                                             const u32x4 (&pb)[NRG][NPL][N], const int (&qpos)[NRG], f32x4 (&oc)[NRG][HD / 16],
+                                             uint64_t (&cls)[class_words(HD)]) {
+    constexpr bool B = P == Prec::BF16;
+    constexpr int NDT = HD / 16, W = Cols<P, HD>::W, NCOL = class_words(HD);
+    const int lane = threadIdx.x & 63, g = lane >> 4, r16 = lane & 15;
+    // A weight of 0 does not silence an infinite or NaN value in the product, and a weight's lo plane may
+    // turn an infinity into a NaN. Both leave a NaN in some output, so outputs without one are right. Else
+    // (rare) the values that are not finite are taken out, the product is formed again, and what the rows
+    // that see them get from them is added behind it: a sum per row and column, as a class of two bits (0,
+    // +inf, -inf, NaN), 32 rows a word, of this lane's columns lane, lane + 64, ...
+    bool taken = false;  // uniform over the wave
+    // V operands of the GR tiles from tile dt on
+    constexpr int GR = B ? 2 : W;
+    auto operand = [&](int dt, u32x4(&vb)[GR][N]) {
+        if constexpr (B) {
+            v_operands<HD>(V, dt, lane, vb);
+            if (valid < kKeys || taken) {  // uniform: values to leave out
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = 32 * x + 16 * (i / 2) + 4 * g + 2 * (i % 2);
+                            const uint32_t v = vb[y][x][i];
+                            const bool lo = key < valid && !(taken && (v & 0x7f80u) == 0x7f80u);
+                            const bool hi = key + 1 < valid && !(taken && (v & 0x7f800000u) == 0x7f800000u);
+                            vb[y][x][i] = (lo ? v & 0xffffu : 0u) | (hi ? v & 0xffff0000u : 0u);
+                        }
+            }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    alignas(4 * W) uint32_t x[W];
+                    load_words<W>(x, reinterpret_cast<const float *>(p.v_pages) + at[kt] + (4 * g + v) * HD +
+                                         Cols<P, HD>::vcol(dt, r16));
+#pragma unroll
+                    for (int y = 0; y < W; ++y) vb[y][kt][v] = x[y];
+                }
+            if (valid < kKeys || taken) {  // uniform: values to leave out
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int y = 0; y < W; ++y) {
+                            const uint32_t x = vb[y][kt][v];
+                            const bool use = 16 * kt + 4 * g + v < valid && !(taken && (x & 0x7f800000u) == 0x7f800000u);
+                            vb[y][kt][v] = use ? x : 0u;
+                        }
+            }
+        }
+    };
+    while (true) {
+        float sum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < NDT; dt += GR) {
+            u32x4 vb[GR][N];
+            operand(dt, vb);
+#pragma unroll
+            for (int y = 0; y < GR; ++y)
+#pragma unroll
+                for (int rg = 0; rg < NRG; ++rg) {
+                    const f32x4 x = v_product<P>(vb[y], pb[rg]);
+                    oc[rg][dt + y] = x;
+                    sum += (x[0] + x[1]) + (x[2] + x[3]);
+                }
+        }
+        if (taken || !__any(sum != sum)) break;
+        taken = true;
+#pragma unroll 1
+        for (int j = 0; j < NCOL; ++j) {
+            const int col = lane + j * kWave;
+            uint64_t bits = 0;
+            float acc = 0.f;
+            int key = 0;
+#pragma unroll 1
+            for (int r = 0; r < 16 * NRG; ++r) {  // the rows' positions do not fall
+                const int last = min(__builtin_amdgcn_readlane(r < 16 ? qpos[0] : qpos[NRG - 1], r & 15), kKeys - 1);
+                for (; key <= last; ++key) {
+                    if (col >= HD) continue;
+                    uint32_t x;
+                    if constexpr (B) {
+                        using TL = Tile<HD>;
+                        x = (uint32_t)reinterpret_cast<const uint16_t *>(V + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16)[col % 8] << 16;
+                    } else {
+                        const size_t row = key < 16 ? at[0] : key < 32 ? at[1] : key < 48 ? at[2] : at[3];
+                        x = __float_as_uint(reinterpret_cast<const float *>(p.v_pages)[row + (key & 15) * HD + col]);
+                    }
+                    if ((x & 0x7f800000u) == 0x7f800000u) acc += __uint_as_float(x);
+                }
+                const uint64_t c = acc != acc ? 3 : acc == INFINITY ? 1 : acc == -INFINITY ? 2 : 0;
+                bits |= c << (2 * r);
+            }
+#pragma unroll
+            for (int i = 0; i < NCOL; ++i)
+                if (i == j) cls[i] = bits;
+        }
+    }
+    return taken;
+}
+__device__ __forceinline__ float class_value(uint32_t c) { return (c & 3) == 1 ? INFINITY : (c & 3) == 2 ? -INFINITY : NAN; }
+
 // One chunk of the span kernel, by one wave: the states of its NRG groups of 16 rows into s_mine ([row][column])
 // and s_m, s_l (this wave's rows). last_key: the request's last token; pages: its table.
 template <Prec P, int HD, int NRG>
@@ -334,99 +471,9 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
             for (int i = valid * Tile<HD>::NC + lane; i < kKeys * Tile<HD>::NC; i += kWave)
                 reinterpret_cast<u32x4 *>(s_mine)[i] = u32x4{0u, 0u, 0u, 0u};
     }
-    // A weight of 0 does not silence an infinite or NaN value in the product, and a weight's lo plane may
-    // turn an infinity into a NaN. Both leave a NaN in some output, so outputs without one are right. Else
-    // (rare) the values that are not finite are taken out, the product is formed again, and what the rows
-    // that see them get from them is added behind it: a sum per row and column, as a class of two bits (0,
-    // +inf, -inf, NaN), 32 rows a word, of this lane's columns lane, lane + 64, ...
-    constexpr int NCOL = (HD + kWave - 1) / kWave;
-    uint64_t cls[NCOL];
-    bool taken = false;  // uniform over the wave
-    // V operands of the W tiles from tile dt on
-    auto operand = [&](int dt, u32x4(&vb)[W][N]) {
-        if constexpr (B) {
-            v_operand<HD>(s_mine, dt, lane, vb[0]);
-        } else {
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    alignas(4 * W) uint32_t x[W];
-                    load_words<W>(x, reinterpret_cast<const float *>(p.v_pages) + at[kt] + (4 * g + v) * HD +
-                                         Cols<P, HD>::vcol(dt, r16));
-#pragma unroll
-                    for (int y = 0; y < W; ++y) vb[y][kt][v] = x[y];
-                }
-            if (valid < kKeys || taken) {  // uniform: values to leave out
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-#pragma unroll
-                        for (int y = 0; y < W; ++y) {
-                            const uint32_t x = vb[y][kt][v];
-                            const bool use = 16 * kt + 4 * g + v < valid && !(taken && (x & 0x7f800000u) == 0x7f800000u);
-                            vb[y][kt][v] = use ? x : 0u;
-                        }
-            }
-        }
-    };
     f32x4 oc[NRG][NDT];
-    while (true) {
-        float sum = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < NDT; dt += W) {
-            u32x4 vb[W][N];
-            operand(dt, vb);
-#pragma unroll
-            for (int y = 0; y < W; ++y)
-#pragma unroll
-                for (int rg = 0; rg < NRG; ++rg) {
-                    const f32x4 x = v_product<P>(vb[y], pb[rg]);
-                    oc[rg][dt + y] = x;
-                    sum += (x[0] + x[1]) + (x[2] + x[3]);
-                }
-        }
-        if (taken || !__any(sum != sum)) break;
-        taken = true;
-#pragma unroll 1
-        for (int j = 0; j < NCOL; ++j) {
-            const int col = lane + j * kWave;
-            uint64_t bits = 0;
-            float acc = 0.f;
-            int key = 0;
-#pragma unroll 1
-            for (int r = 0; r < 16 * NRG; ++r) {  // the rows' positions do not fall
-                const int last = min(min(__builtin_amdgcn_readlane(r < 16 ? qpos[0] : qpos[NRG - 1], r & 15), valid - 1), kKeys - 1);
-                for (; key <= last; ++key) {
-                    if (col >= HD) continue;
-                    uint32_t x;
-                    if constexpr (B) {
-                        using TL = Tile<HD>;
-                        uint16_t *v = reinterpret_cast<uint16_t *>(s_mine + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
-                        x = (uint32_t)*v << 16;
-                        if ((x & 0x7f800000u) == 0x7f800000u) *v = 0;
-                    } else {
-                        const size_t row = key < 16 ? at[0] : key < 32 ? at[1] : key < 48 ? at[2] : at[3];
-                        x = __float_as_uint(reinterpret_cast<const float *>(p.v_pages)[row + (key & 15) * HD + col]);
-                    }
-                    if ((x & 0x7f800000u) == 0x7f800000u) acc += __uint_as_float(x);
-                }
-                const uint64_t c = acc != acc ? 3 : acc == INFINITY ? 1 : acc == -INFINITY ? 2 : 0;
-                bits |= c << (2 * r);
-            }
-            if constexpr (B) {  // what no row sees
-                for (; key < kKeys && col < HD; ++key) {
-                    using TL = Tile<HD>;
-                    uint16_t *v = reinterpret_cast<uint16_t *>(s_mine + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
-                    if ((*v & 0x7f80) == 0x7f80) *v = 0;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < NCOL; ++i)
-                if (i == j) cls[i] = bits;
-        }
-    }
+    uint64_t cls[class_words(HD)];
+    const bool taken = chunk_values<P, HD>(p, s_mine, at, B ? kKeys : valid, pb, qpos, oc, cls);
     // V has been read: the states in its place
 #pragma unroll
     for (int rg = 0; rg < NRG; ++rg) {
@@ -447,17 +494,55 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
     }
     if (taken) {
 #pragma unroll
-        for (int j = 0; j < NCOL; ++j) {
+        for (int j = 0; j < class_words(HD); ++j) {
             const int col = lane + j * kWave;
 #pragma unroll 1
             for (int r = 0; r < 16 * NRG; ++r) {
                 const int c = (int)(cls[j] >> (2 * r)) & 3;
                 if (col < HD && c != 0)
-                    reinterpret_cast<float *>(s_mine)[r * SROW + col] += c == 1 ? INFINITY : c == 2 ? -INFINITY : NAN;
+                    reinterpret_cast<float *>(s_mine)[r * SROW + col] += class_value(c);
             }
         }
     }
 }
+
+// Loads of a chunk's K and V (bf16) into LDS by four waves. A wave takes every fourth KiB: keys of one of the
+// chunk's tiles of 16, whose permutations repeat (so the same place of every tile, or two in turn).
+template <int HD>
+struct ChunkLoads {
+    using TL = Tile<HD>;
+    static constexpr int LPT = 16 / TL::RPK, VAR = LPT > 4 ? LPT / 4 : 1;  // loads of 16 keys
+    uint32_t koff[VAR], voff[VAR];
+    int lane, w;
+    __device__ ChunkLoads(int tid) : lane(tid & 63), w(__builtin_amdgcn_readfirstlane(tid >> 6)) {
+#pragma unroll
+        for (int i = 0; i < VAR; ++i) {
+            const int key = (w + 4 * i) % LPT * TL::RPK + lane / (kWave / TL::RPK), piece = lane % TL::NC;
+            koff[i] = key * TL::ROWB + (piece ^ TL::kswz(key)) * 16;
+            voff[i] = key * TL::ROWB + (piece ^ TL::vswz(key)) * 16;
+        }
+    }
+    // Pages of a chunk's four tiles (past the request's last one: that), a lane each; asked for a chunk
+    // before the chunk's loads.
+    __device__ int pages(const PagedAttnParams &p, const int32_t *table, int c, int last_tile) const {
+        return table[(min(4 * c + (lane & 3), last_tile) << 4) >> p.bk.page_shift];
+    }
+    __device__ void issue(const PagedAttnParams &p, int h, int c, int last_tile, int pg, uint8_t *dst) const {
+        const int shift = p.bk.page_shift;
+#pragma unroll
+        for (int i = 0; i < TL::KIB / 4; ++i) {
+            const int kb = w + 4 * i, tile = 4 * c + kb / LPT;
+            const size_t page = __builtin_amdgcn_readlane(pg, kb / LPT);
+            const size_t base = (((page * p.n_kv + h) << shift) + ((min(tile, last_tile) << 4) & ((1 << shift) - 1))) * TL::ROWB;
+            __builtin_amdgcn_global_load_lds(
+                static_cast<const void *>(static_cast<const uint8_t *>(p.k_pages) + base + koff[i % VAR]),
+                (__attribute__((address_space(3))) void *)(dst + kb * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds(
+                static_cast<const void *>(static_cast<const uint8_t *>(p.v_pages) + base + voff[i % VAR]),
+                (__attribute__((address_space(3))) void *)(dst + TL::BYTES + kb * 1024), 16, 0, 0);
+        }
+    }
+};
 
 // Few rows. Workgroup: a block of up to 16 RG rows of one key head and some spans of its keys, one after
 // another, a wave per chunk of 64 keys: K straight into registers in operand order, V through LDS (bf16:
@@ -480,6 +565,7 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
     PagedUnit u;
     for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
         const int h = idx % p.n_kv;
+        if (u.k0 < 0) continue;  // a whole request's (uniform)
         const int rows = min(ROWS, u.m * p.group - u.row);
         const RowMap map(p, u.row);
         const int blast = u.ctx + map.token(rows - 1);  // the block's last position
@@ -554,6 +640,109 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
     }
 }
 
+// A whole request of few rows (bf16): 16 rows a wave, all keys. Chunks of K and V come into LDS once for all
+// waves, one chunk ahead; a wave keeps its rows' state, over a span and over the spans, in registers. The same
+// steps as with a wave per chunk and a join, in the same order.
+template <int HD>
+__global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_kernel(PagedAttnParams p, int cap_units) {
+    constexpr Prec P = Prec::BF16;
+    using TL = Tile<HD>;
+    constexpr int NKK = HD / 32, NDT = HD / 16;
+    extern __shared__ u32x4 s_raw[];
+    uint8_t *s_kv = reinterpret_cast<uint8_t *>(s_raw);  // [buffer][K, V]
+    const ChunkLoads<HD> loads(threadIdx.x);
+    const int lane = loads.lane, w = loads.w, g = lane >> 4, r16 = lane & 15;
+    int count = 0;
+    PagedUnit u;
+    for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
+        if (u.k0 >= 0) continue;  // the span kernel's (uniform)
+        const int h = idx % p.n_kv, rows = u.m * p.group;
+        const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
+        const RowMap map(p, 0);
+        const int last_key = u.ctx + u.m - 1, last_tile = last_key >> 4;
+        const int blast = u.ctx + map.token(rows - 1), wlast = u.ctx + map.token(min(16 * w + 15, rows - 1));
+        const int c1 = blast / kKeys + 1;
+        const bool live = 16 * w < rows;  // uniform over the wave
+        const int row = min(16 * w + r16, rows - 1), token = map.token(row), head = h * p.group + map.head(row);
+        int pg = loads.pages(p, table, 0, last_tile);
+        __syncthreads();  // the unit before is done with the buffers
+        loads.issue(p, h, 0, last_tile, pg, s_kv);
+        pg = loads.pages(p, table, 1, last_tile);
+        u32x4 q[NKK];
+        const uint16_t *qrow = reinterpret_cast<const uint16_t *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + g * 8;
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) q[kk] = *reinterpret_cast<const u32x4 *>(qrow + kk * 32);
+        float M = -INFINITY, l = 0.f, Mr = -INFINITY, lr = 0.f;  // of the span, of the row
+        f32x4 o[NDT], orow[NDT];
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] = orow[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < c1; ++c) {
+            const int key0 = c * kKeys;
+            const uint8_t *K = s_kv + (size_t)(c & 1) * 2 * TL::BYTES, *V = K + TL::BYTES;
+            wait_vm_lds<0>();
+            barrier_no_fence();  // every wave's pieces of the chunk have landed, and the other buffer has been read
+            if (c + 1 < c1) loads.issue(p, h, c + 1, last_tile, pg, s_kv + (size_t)((c + 1) & 1) * 2 * TL::BYTES);
+            pg = loads.pages(p, table, c + 2, last_tile);
+            if (!live) continue;
+            if (key0 <= wlast) {  // uniform over the wave
+                f32x4 st[4];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) {
+                    st[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < NKK; ++kk)
+                        st[kt] = mfma_kstep<P>(*reinterpret_cast<const u32x4 *>(K + (16 * kt + r16) * TL::ROWB +
+                                                                                ((4 * kk + g) ^ TL::kswz(r16)) * 16),
+                                               q[kk], st[kt]);
+                }
+                const int qpos[1] = {u.ctx + token - key0};
+                float mx, lc;
+                u32x4 pb[1][2][2];
+                chunk_softmax(st, qpos[0], p.scale_log2, lane, mx, lc);
+                weight_operand<P>(st, pb[0]);
+                f32x4 oc[1][NDT];
+                uint64_t cls[class_words(HD)];
+                const size_t at[4] = {};
+                if (chunk_values<P, HD>(p, V, at, last_key - key0 + 1, pb, qpos, oc, cls)) {
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {  // column 16 dt + 4 g + e
+                            const uint32_t k = (uint32_t)__shfl((int)(uint32_t)cls[dt / 4], (16 * dt + 4 * g + e) & 63) >> (2 * r16) & 3;
+                            if (k) oc[0][dt][e] += class_value(k);
+                        }
+                }
+                if (qpos[0] >= 0) {
+                    float wo, wc;
+                    merge_weights(M, mx, wo, wc);
+                    l = merge_value(l, lc, wo, wc);
+#pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[dt][e] = merge_value(o[dt][e], oc[0][dt][e], wo, wc);
+                }
+            }
+            if (c % kSpanChunks + 1 < kSpanChunks && c + 1 < c1) continue;
+            if (c / kSpanChunks * kPagedSpanKeys <= u.ctx + token) {
+                float v, vc;
+                merge_weights(Mr, M, v, vc);
+                lr = merge_value(lr, l, v, vc);
+#pragma unroll
+                for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) orow[dt][e] = merge_value(orow[dt][e], o[dt][e], v, vc);
+            }
+            M = -INFINITY;
+            l = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        if (16 * w + r16 < rows)
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) store_row<P>(p, u.r0 + token, head, 16 * dt + 4 * g, orow[dt], Mr, lr);
+    }
+}
+
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -581,17 +770,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
     uint8_t *s_kv = reinterpret_cast<uint8_t *>(s_raw);  // [buffer][K, V]
     uint32_t *s_cls = reinterpret_cast<uint32_t *>(s_kv + 4 * TL::BYTES);  // [column][16 rows]
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r32 = lane & 31, hb = lane >> 5, shift = p.bk.page_shift;
-    // This lane's place in a wave's loads: 1 KiB of 16 keys, whose permutations repeat (a wave takes every
-    // fourth KiB: the same one of every 16 keys, or two in turn).
-    constexpr int LPT = 16 / TL::RPK, VAR = LPT > 4 ? LPT / 4 : 1;  // loads of 16 keys
-    uint32_t koff[VAR], voff[VAR];
-#pragma unroll
-    for (int i = 0; i < VAR; ++i) {
-        const int key = (w + 4 * i) % LPT * TL::RPK + lane / (kWave / TL::RPK), piece = lane % TL::NC;
-        koff[i] = key * TL::ROWB + (piece ^ TL::kswz(key)) * 16;
-        voff[i] = key * TL::ROWB + (piece ^ TL::vswz(key)) * 16;
-    }
+    const int r32 = lane & 31, hb = lane >> 5;
+    const ChunkLoads<HD> loads(tid);
     const float scale = fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;  // the scale's sign goes into the queries
     int count = 0;
@@ -608,31 +788,10 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
         const bool live = 32 * w < rows;  // uniform over the wave
         const int rr = min(32 * w + r32, rows - 1), token = map.token(rr), head = h * p.group + map.head(rr);
         const int qpos = u.ctx + token;
-        // page ids of the 64 tiles of 16 keys from tile 64 j on, one per lane
-        auto page_ids = [&](int j) { return table[(min(64 * j + lane, last_tile) << 4) >> shift]; };
-        int pj = c0 / 16, pg = page_ids(pj), pg_next = page_ids(pj + 1);
-        auto issue = [&](int c, int buf) {
-            if (c / 16 != pj) {
-                pj = c / 16;
-                pg = pg_next;
-                pg_next = page_ids(pj + 1);
-            }
-#pragma unroll
-            for (int i = 0; i < TL::KIB / 4; ++i) {
-                const int kb = w + 4 * i, tile = 4 * c + kb / LPT;
-                const size_t page = __builtin_amdgcn_readlane(pg, tile & 63);
-                const size_t base = (((page * p.n_kv + h) << shift) + ((min(tile, last_tile) << 4) & ((1 << shift) - 1))) * TL::ROWB;
-                uint8_t *dst = s_kv + (size_t)buf * 2 * TL::BYTES + kb * 1024;
-                __builtin_amdgcn_global_load_lds(
-                    static_cast<const void *>(static_cast<const uint8_t *>(p.k_pages) + base + koff[i % VAR]),
-                    (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
-                __builtin_amdgcn_global_load_lds(
-                    static_cast<const void *>(static_cast<const uint8_t *>(p.v_pages) + base + voff[i % VAR]),
-                    (__attribute__((address_space(3))) void *)(dst + TL::BYTES), 16, 0, 0);
-            }
-        };
+        int pg = loads.pages(p, table, c0, last_tile);
         __syncthreads();  // the unit before is done with the buffers
-        if (c0 < c1) issue(c0, 0);
+        if (c0 < c1) loads.issue(p, h, c0, last_tile, pg, s_kv);
+        pg = loads.pages(p, table, c0 + 1, last_tile);
         u32x4 q[NKK];
         const uint16_t *qrow = reinterpret_cast<const uint16_t *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + hb * 8;
 #pragma unroll
@@ -647,7 +806,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
             const int buf = (c - c0) & 1, key0 = c * kKeys;
             wait_vm_lds<0>();
             barrier_no_fence();  // every wave's pieces of the chunk have landed, and the other buffer has been read
-            if (c + 1 < c1) issue(c + 1, buf ^ 1);
+            if (c + 1 < c1) loads.issue(p, h, c + 1, last_tile, pg, s_kv + (size_t)(buf ^ 1) * 2 * TL::BYTES);
+            pg = loads.pages(p, table, c + 2, last_tile);
             const uint8_t *K = s_kv + (size_t)buf * 2 * TL::BYTES;
             uint8_t *V = s_kv + (size_t)buf * 2 * TL::BYTES + TL::BYTES;
             if (key0 + kKeys - 1 > tfirst) {  // uniform: keys that some row does not see
@@ -838,10 +998,13 @@ hipError_t launch_spans(int64_t units, const PagedAttnParams &p, hipStream_t s) 
 }
 
 template <Prec P, int HD, int RG>
-hipError_t launch_shape(int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
+hipError_t launch_shape(int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
     hipError_t e = launch_spans<P, HD, RG>(units, p, s);
     if (e != hipSuccess) return e;
     if constexpr (P == Prec::BF16) {
+        if (whole > 0)
+            hipLaunchKernelGGL((paged_request_kernel<HD>), dim3((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
+                               4 * Tile<HD>::BYTES, s, p, p.bk.cap_units);
         if (tiles > 0)
             hipLaunchKernelGGL((paged_tile_kernel<HD>), dim3((unsigned)std::min<int64_t>(tiles * p.n_kv, 16 * kCUs)),
                                dim3(4 * kWave), tile_lds<HD>(), s, p, p.bk.cap_tiles);
@@ -857,19 +1020,19 @@ hipError_t launch_shape(int64_t units, int64_t tiles, bool join, const PagedAttn
 
 }  // namespace
 
-hipError_t launch_paged_attn(bool bf16, int64_t units, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
+hipError_t launch_paged_attn(bool bf16, int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
     if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0 || tiles < 0) return hipErrorInvalidValue;
     if (units + tiles == 0 || p.rows == 0) return hipSuccess;
     if (bf16) {
-        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 2>(units, tiles, join, p, s);
-        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 1>(units, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 1>(units, whole, tiles, join, p, s);
     } else {
-        if (p.hd == 16) return launch_shape<Prec::F32, 16, 2>(units, tiles, join, p, s);
-        if (p.hd == 32) return launch_shape<Prec::F32, 32, 2>(units, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::F32, 64, 2>(units, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::F32, 128, 1>(units, tiles, join, p, s);
+        if (p.hd == 16) return launch_shape<Prec::F32, 16, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 32) return launch_shape<Prec::F32, 32, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 64) return launch_shape<Prec::F32, 64, 2>(units, whole, tiles, join, p, s);
+        if (p.hd == 128) return launch_shape<Prec::F32, 128, 1>(units, whole, tiles, join, p, s);
     }
     return hipErrorInvalidValue;
 }

@@ -407,7 +407,8 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     units = std::min(units * spans, units + kPagedUnits / f.n_kv_heads + 1);
     int64_t tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
     tiles = std::min(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
-    HIPCHK(c, launch_paged_attn(c->bf16, units, tiles, spans > 1, p, c->stream));
+    const bool whole = c->tiled && most > kPagedWaveRows && c->n * f.n_kv_heads >= kPagedTileGroups;
+    HIPCHK(c, launch_paged_attn(c->bf16, units, whole, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
 }
 

@@ -316,6 +316,51 @@ def test_attention(binding, case):
     assert torch.equal(q[:sum(new)], out[:sum(new)])
 
 
+@pytest.mark.parametrize("heads,kv,hd,page,n,lo,hi", [(8, 8, 128, 64, 68, 17, 64), (16, 8, 64, 16, 68, 9, 32), (32, 16, 32, 32, 36, 9, 32),
+                                                      (4, 4, 256, 64, 132, 17, 40), (8, 8, 128, 16, 63, 17, 64)])
+def test_many_requests_of_a_block_each(binding, heads, kv, hd, page, n, lo, hi):
+    """Enough blocks to fill the device (all but the last case), one request of a token, one of none and one long
+    chunk among them: the formula, and each block's bits as in a plan of its own, with values that are not finite
+    in tokens that some rows see."""
+    rng = random.Random(hd)
+    new = [rng.randint(lo, hi) for _ in range(n)]
+    ctx = [rng.randint(250, 500) for _ in range(n)]
+    new[3], new[7], new[11], ctx[12], ctx[13] = 1, 0, 70, 0, 256 - new[13]
+    total = [a + b for a, b in zip(ctx, new)]
+    n_pages = sum(-(-t // page) for t in total) + 1
+    c = make(binding, page=page, n_pages=n_pages, max_seqs=n, max_ctx=max(total), max_rows=sum(new) + 1, heads=heads, kv=kv, hd=hd)
+    books, seq = ref.Books(page, n_pages, n), list(range(n))
+    q, kp, vp, out, lse = check_attn(c, books, seq, ctx, new, seed=hd)
+    start = np.concatenate([[0], np.cumsum(new)])
+    mine = [0, 3, 12, 13, 14, n - 1]
+
+    def alone(s):
+        c.plan(ints([s]), ints([ctx[s]]), ints([new[s]]), rows=new[s])
+        o, ls = torch.empty_like(q[:new[s]]), torch.empty_like(lse[:new[s]])
+        c.attn(q[start[s]:start[s + 1]], kp, vp, o, lse=ls)
+        return o, ls
+
+    for s in mine:
+        o, ls = alone(s)
+        assert torch.equal(o, out[start[s]:start[s + 1]]) and torch.equal(ls, lse[start[s]:start[s + 1]])
+    for s in mine:  # a token in the midst of the new ones, and one of the first
+        for t, d, value in ((ctx[s] + new[s] // 2, 5, float("inf")), (ctx[s] + new[s] // 3, hd - 1, float("nan")),
+                            (total[s] // 9, 6, -float("inf"))):
+            vp[books.table[s][t // page], :, t % page, d] = value
+    c.plan(ints(seq), ints(ctx), ints(new), rows=sum(new))
+    odd = torch.empty_like(out)
+    c.attn(q, kp, vp, odd)
+    for s in mine:
+        a, b = alone(s)[0], odd[start[s]:start[s + 1]]
+        same = (a == b) | (torch.isnan(a) & torch.isnan(b))
+        assert same.all()
+        at = new[s] // 2
+        assert torch.isfinite(b[:at, :, 5]).all() and (b[at:, :, 5] == float("inf")).all()
+        assert torch.isnan(b[new[s] // 3:, :, hd - 1]).all() and torch.isfinite(b[:new[s] // 3, :, hd - 1]).all()
+        keep = [d for d in range(hd) if d not in (5, 6, hd - 1)]
+        assert torch.equal(b[..., keep], out[start[s]:start[s + 1]][..., keep])
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd,ctx,m", [("bf16", 4, 4, 128, 500, 40), ("bf16", 8, 2, 64, 70, 16),
                                                      ("bf16", 4, 2, 128, 120, 90), ("f32", 2, 2, 64, 60, 30)])
 def test_unseen_tokens_do_not_reach_a_row(binding, dtype, heads, kv, hd, ctx, m):
