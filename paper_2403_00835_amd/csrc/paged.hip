@@ -109,6 +109,9 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // request. So giving back what a step took restores the stack, whatever the requests. A refused plan
 // (bad slot or length, more rows than the bound, too few pages) leaves the books as they were and has
 // no rows.
+// Bound: one CU's latency: four barriers and sums, then a round trip per dependent read (lengths, pages owned,
+// table). 16 requests: 3.5 to 4.9 us; 512 requests of 1 to 64 tokens: 26 us, of which the rows'
+// slots are most.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
     __shared__ int s_wave[6][kPlanWaves], s_wave2[6][kPlanWaves];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
@@ -298,6 +301,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
 // Rows of the step: queries and keys turned by their positions (rotate-half: (a c - b s, b c + a s) of
 // a head's halves a, b), in fp32 and rounded once; keys and values into their slots. A thread takes
 // 16 bytes of each half of one head of one row.
+// Bound: memory: 197 MB (5 prompts, 8000 rows of 32 and 8 heads of 128) in 31 us, 6.3 TB/s; 512 rows 6.1 us, 8
+// rows 2.1.
 template <Prec PR>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) {
     using PT = PrecT<PR>;
@@ -356,7 +361,7 @@ hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int
 
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s) {
     if (p.n < 1 || p.n > kPagedMaxSeqs || p.bk.max_seqs > kPagedMaxSeqs) return hipErrorInvalidValue;
-    // four waves unless there are requests or rows for more (their barriers and sums cost 2 us)
+    // four waves unless there are requests or rows for more (16 requests: 4 us with four waves, 6 with sixteen)
     const int threads = p.n <= 256 && p.rows <= 2048 ? 256 : kPlanThreads;
     hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(threads), 0, s, p);
     return hipGetLastError();

@@ -6,16 +6,17 @@
 //
 // Few rows (paged_span_kernel): the keys are walked in chunks of 64 at absolute positions. A chunk's
 // state per row is its maximum, its sum and its unnormalised output; the states of the chunks that hold
-// a key the row sees are merged in position order into that of a span of 512 keys, and the spans' into
+// a key the row sees are merged in position order into that of a span of 256 keys, and the spans' into
 // the row's. The order depends on positions alone: a row's bits are the same whichever rows, requests,
-// pages and launches it is computed with.
+// pages and launches it is computed with. Plans of many blocks (paged_request_kernel) take the same steps
+// without partial states between kernels.
 // Long chunks (paged_tile_kernel): tiles of 128 rows walk their keys with a running maximum; ranges of
 // keys are joined where there are few tiles.
 //
 // Values: scores and softmax statistics in fp32; the probabilities of few rows as hi + lo bf16 planes
 // (~2^-17), so the only rounding to bf16 is that of the output. Keys past a row's position contribute
 // nothing, whatever their values (NaN, infinities): scores are selected away, values by the rules in
-// paged_span_kernel.
+// chunk_values.
 #include <algorithm>
 
 #include "device.h"
@@ -550,6 +551,12 @@ struct ChunkLoads {
 // head_dim 128, and two workgroups per CU); then it merges the chunks' states. A span's state goes to the
 // partials, or, where the request has one span only (fp32: also where the partials do not hold the
 // request's), the rows are written.
+// Bound: reading the cache. Tokens of 64 requests at 1000 to 8000 keys (8 key heads of 128, pages of 16):
+// 1.18 GB in 222 us, 5.3 TB/s, and 13 in the join (a large copy here reaches 4.75). Short calls: latency, a
+// round trip each for the unit, the pages and the keys: one token at 512 keys 7.7 us and 3.2 in the join, 16
+// rows at 700 9.2 and 3.3, 64 rows at 2304 24.0 and 4.8 (32 heads); fp32, 29 to 82 KiB of keys a head, 13.8
+// and 3.9. Spans of 512 keys by eight waves leave one workgroup a CU: 259 us in place of 224. The last
+// workgroup of a row joining its spans in place of a kernel costs 10 us of fences.
 template <Prec P, int HD, int RG>
 __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
                                                                                                   int cap_units) {
@@ -640,9 +647,12 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
     }
 }
 
-// A whole request of few rows (bf16): 16 rows a wave, all keys. Chunks of K and V come into LDS once for all
-// waves, one chunk ahead; a wave keeps its rows' state, over a span and over the spans, in registers. The same
-// steps as with a wave per chunk and a join, in the same order.
+// A whole request of few rows (bf16) and one key head: 16 rows a wave, all keys. Chunks of K and V come into
+// LDS once for all waves, one chunk ahead; a wave keeps its rows' state, over a span and over the spans, in
+// registers. The same steps as with a wave per chunk and a join, in the same order, so the same bits.
+// Bound: reading the cache, one chunk of 32 KiB a workgroup (head_dim 128, two a CU) ahead. 64 requests of 36
+// rows at 4000 keys, 8 key heads: 205 us, 5.1 TB/s. 16 ragged requests of 32 rows at 256 to 1280 keys, 32
+// heads: 218 MB in 49 us. The unit list is the span kernel's, and each passes over the other's units.
 template <int HD>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_kernel(PagedAttnParams p, int cap_units) {
     constexpr Prec P = Prec::BF16;
@@ -762,6 +772,12 @@ constexpr int tile_lds() {
 // weight, of random sign: less than the output's own rounding), their sum is not. The reference of the
 // exponentials follows the running maximum only when that has grown by 2^8: weights are then at most 2^8
 // in place of 1, which neither type minds, and the output is rescaled rarely.
+// Bound: the matrix unit and, between its products, the softmax: 2048 tokens at 12288 (32 heads, 8 key heads
+// of 128) take 462 to 480 us, 930 to 970 TFLOP/s (a large bf16 product of the library reaches 1200 here).
+// Left out of a copy, the exponentials save 35 us, the DMA 60, three quarters of either product 105 to 125:
+// nothing waits for one thing alone. Reads that run ahead of the softmax, softmax and products of two chunks
+// interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 770
+// TFLOP/s, 32 wide 660, 256 wide 460 (one workgroup a CU, and 38 registers spilled).
 template <int HD>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
     using TL = Tile<HD>;
@@ -969,7 +985,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
 }
 
 // Joins the partial states of split row blocks, in position order. Workgroup: some rows of one key head of
-// an item, a thread per four columns of a row.
+// an item, a thread per four columns of a row. Bound: latency, four states in flight a thread: 3.2 us for one
+// span's worth, 13 us for 64 requests of 4 to 32 spans (16 in flight: 15.5 in place of 8.3 us at 16 requests).
 template <Prec P, int HD>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int cap_items) {
     constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedItemRows + RPW - 1) / RPW;
@@ -988,18 +1005,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int 
 namespace {
 
 template <Prec P, int HD, int RG>
-hipError_t launch_spans(int64_t units, const PagedAttnParams &p, hipStream_t s) {
+hipError_t launch_spans(int64_t units, bool whole, const PagedAttnParams &p, hipStream_t s) {
     constexpr int lds = kSpanChunks * span_wave_lds<P, HD, RG>();
     static_assert(lds + 4096 <= 160 * 1024, "the LDS of a CU");
     static_assert(16 * RG == paged_block_rows(P == Prec::BF16, HD), "the plan's row blocks");
-    const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs));
+    // (where requests may be taken whole, fewer: passing over 2560 units takes 6.5 us, 3.7 in a grid of 1024; spans in
+    // a grid of 1024 take up to 2% longer)
+    const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, whole ? 4 * kCUs : 16 * kCUs));
     hipLaunchKernelGGL((paged_span_kernel<P, HD, RG>), grid, dim3(kSpanChunks * kWave), lds, s, p, p.bk.cap_units);
     return hipGetLastError();
 }
 
 template <Prec P, int HD, int RG>
 hipError_t launch_shape(int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
-    hipError_t e = launch_spans<P, HD, RG>(units, p, s);
+    hipError_t e = launch_spans<P, HD, RG>(units, whole, p, s);
     if (e != hipSuccess) return e;
     if constexpr (P == Prec::BF16) {
         if (whole > 0)
