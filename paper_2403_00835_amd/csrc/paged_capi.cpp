@@ -407,7 +407,10 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     units = std::min(units * spans, units + kPagedUnits / f.n_kv_heads + 1);
     int64_t tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
     tiles = std::min(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
-    const bool whole = c->tiled && most > kPagedWaveRows && c->n * f.n_kv_heads >= kPagedTileGroups;
+    // whether a plan of these bounds may have whole requests: any plan, as a graph of this call may run behind one of
+    // more requests
+    const int64_t blocks = std::min<int64_t>(f.max_seqs, (int64_t)c->rows * c->group / (kPagedWaveRows + 1));
+    const bool whole = c->tiled && most > kPagedWaveRows && blocks * f.n_kv_heads >= kPagedTileGroups;
     HIPCHK(c, launch_paged_attn(c->bf16, units, whole, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
 }

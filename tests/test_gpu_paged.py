@@ -654,6 +654,34 @@ def test_captured_steps(binding):
         del graphs, attn_only
 
 
+def test_a_captured_call_behind_plans_of_more_requests(binding):
+    """Attention captured behind a plan of one request; the same bounds then hold many, whole or a long one among them."""
+    side = torch.cuda.Stream()
+    n, m, kv = 70, 20, 8
+    with torch.cuda.stream(side):
+        c = make(binding, page=16, n_pages=1400, max_seqs=n, max_ctx=3000, max_rows=n * m, heads=kv, kv=kv, hd=64)
+        bounds = dict(rows=n * m, max_new=m, max_len=3000)
+        pools = [torch.randn(c.pool_shape, device="cuda").bfloat16() for _ in range(2)]
+        q = torch.randn(n * m, kv, 64, device="cuda").bfloat16()
+        out, eager = torch.empty_like(q), torch.empty_like(q)
+        c.plan(ints([0]), ints([100]), ints([m]), **bounds)
+        c.attn(q, *pools, out)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.attn(q, *pools, out)
+        for first in (100, 2900, 250):
+            ctx = [first] + [90 + s for s in range(1, n)]
+            c.plan(ints(list(range(n))), ints(ctx), ints([m] * n), **bounds)
+            out.fill_(7)
+            graph.replay()
+            c.attn(q, *pools, eager)
+            assert c.status()[0] == n * m
+            assert torch.equal(out, eager) and (eager != 7).any()
+        side.synchronize()
+        del graph
+
+
 def test_two_caches_side_by_side(binding):
     """Two caches on two streams: neither's partials or books are the other's."""
     got = []
