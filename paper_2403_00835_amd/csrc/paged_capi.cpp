@@ -7,8 +7,6 @@
 #include <cstdarg>
 #include <cstdio>
 #include <new>
-#include <string>
-#include <vector>
 
 #include "../../include/cllm.h"
 #include "device.h"
@@ -29,7 +27,7 @@ struct cllm_paged {
     void *own = nullptr;  // library-allocated workspace
     bool planned = false, dead = false;
     int n = 0, rows = 0, max_new = 0, max_len = 0;  // the last plan's bounds
-    std::string err;
+    char err[512] = "";
 };
 
 namespace {
@@ -38,12 +36,10 @@ constexpr size_t kAlign = 256;
 constexpr int kMaxLen = 1 << 20;  // tokens of a request, rows of a plan
 
 cllm_status fail(cllm_paged *c, cllm_status s, const char *fmt, ...) {
-    char buf[512];
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
+    vsnprintf(c->err, sizeof c->err, fmt, ap);
     va_end(ap);
-    c->err = buf;
     if (s == CLLM_ERR_DEVICE) c->dead = true;
     return s;
 }
@@ -92,9 +88,16 @@ struct Buf {
     void **p;
     size_t bytes;
 };
+struct Bufs {  // (nothing here allocates host memory: no exception leaves an entry point)
+    Buf b[16];
+    int n = 0;
+    void push(Buf x) { b[n++] = x; }
+    const Buf *begin() const { return b; }
+    const Buf *end() const { return b + n; }
+};
 
 // Device memory of a cache, each buffer at a 256-byte boundary.
-std::vector<Buf> buffers(cllm_paged *c) {
+Bufs buffers(cllm_paged *c) {
     const cllm_paged_config &f = c->cfg;
     PagedBooks &bk = c->bk;
     c->bf16 = f.dtype == CLLM_DTYPE_BF16;
@@ -124,32 +127,33 @@ std::vector<Buf> buffers(cllm_paged *c) {
     c->cap_tile_part = c->tiled ? (int)std::min(few_tiles * kPagedTileRows, nrows * spans) : 0;
     auto P = [](auto **q) { return reinterpret_cast<void **>(q); };
     const size_t part = ((size_t)c->cap_part + c->cap_tile_part) * f.n_kv_heads;
-    std::vector<Buf> b{
-        {P(&bk.status), PS_WORDS * 4},
-        {P(&bk.table), (size_t)f.max_seqs * bk.max_pages * 4},
-        {P(&bk.seq_pages), (size_t)f.max_seqs * 4},
-        {P(&bk.free_list), (size_t)f.n_pages * 4},
-        {P(&bk.row_start), (size_t)(f.max_seqs + 1) * 4},
-        {P(&bk.row_slot), (size_t)f.max_rows * 4},
-        {P(&bk.row_pos), (size_t)f.max_rows * 4},
-        {P(&bk.units), (size_t)bk.cap_units * sizeof(PagedUnit)},
-        {P(&bk.tiles), (size_t)bk.cap_tiles * sizeof(PagedUnit)},
-        {P(&bk.items), (size_t)bk.cap_items * sizeof(PagedItem)},
-        {P(&c->part_o), part * f.head_dim * 4},
-        {P(&c->part_m), part * 4},
-        {P(&c->part_l), part * 4},
-    };
+    Bufs b;
+    for (const Buf &x : {
+            Buf{P(&bk.status), PS_WORDS * 4},
+            Buf{P(&bk.table), (size_t)f.max_seqs * bk.max_pages * 4},
+            Buf{P(&bk.seq_pages), (size_t)f.max_seqs * 4},
+            Buf{P(&bk.free_list), (size_t)f.n_pages * 4},
+            Buf{P(&bk.row_start), (size_t)(f.max_seqs + 1) * 4},
+            Buf{P(&bk.row_slot), (size_t)f.max_rows * 4},
+            Buf{P(&bk.row_pos), (size_t)f.max_rows * 4},
+            Buf{P(&bk.units), (size_t)bk.cap_units * sizeof(PagedUnit)},
+            Buf{P(&bk.tiles), (size_t)bk.cap_tiles * sizeof(PagedUnit)},
+            Buf{P(&bk.items), (size_t)bk.cap_items * sizeof(PagedItem)},
+            Buf{P(&c->part_o), part * f.head_dim * 4},
+            Buf{P(&c->part_m), part * 4},
+            Buf{P(&c->part_l), part * 4}})
+        b.push(x);
     if (f.rope_base > 0.0f) {
         const size_t n = (size_t)f.max_ctx * (f.head_dim / 2) * 4;
-        b.push_back({P(&c->rcos), n});
-        b.push_back({P(&c->rsin), n});
+        b.push({P(&c->rcos), n});
+        b.push({P(&c->rsin), n});
     }
     return b;
 }
 
 size_t round_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
-size_t total(const std::vector<Buf> &bufs) {
+size_t total(const Bufs &bufs) {
     size_t t = 0;
     for (const Buf &b : bufs) t += round_up(b.bytes);
     return t;
@@ -167,11 +171,7 @@ bool accessible(const cllm_paged *c, const void *p) {
 }
 
 cllm_status check(cllm_paged *c) {
-    if (c->dead) {
-        const std::string first = c->err;
-        return fail(c, CLLM_ERR_DEVICE, "cache unusable after a device error: %s", first.c_str());
-    }
-    return CLLM_OK;
+    return c->dead ? CLLM_ERR_DEVICE : CLLM_OK;  // the first error stays the last one
 }
 
 // Rows of `heads` heads: 16-byte vectors of whole heads.
@@ -228,7 +228,7 @@ cllm_status cllm_paged_create(const cllm_paged_config *cfg, cllm_paged **out) {
     };
     DeviceGuard dev(cfg->device);
     if (!dev.ok) return bail(CLLM_ERR_DEVICE);
-    const std::vector<Buf> bufs = buffers(c);
+    const Bufs bufs = buffers(c);
     const size_t need = total(bufs);
     uint8_t *base = static_cast<uint8_t *>(cfg->workspace);
     if (base) {
@@ -439,6 +439,6 @@ cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages)
     return CLLM_OK;
 }
 
-const char *cllm_paged_last_error(const cllm_paged *c) { return c ? c->err.c_str() : "null cache"; }
+const char *cllm_paged_last_error(const cllm_paged *c) { return c ? c->err : "null cache"; }
 
 }  // extern "C"
