@@ -929,7 +929,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
             const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             mx = fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1])) * scale;
             if (__any(mx > M + 8.f)) {
-                const float Mn = fmaxf(M, mx), f = M == -INFINITY ? 0.f : exp2_weight(M - Mn);
+                // (where M is -inf, l is 0 and o holds only what values that are not finite gave: kept)
+                const float Mn = fmaxf(M, mx), f = M == -INFINITY ? 1.f : exp2_weight(M - Mn);
                 l *= f;
 #pragma unroll
                 for (int dt = 0; dt < NDT; ++dt)

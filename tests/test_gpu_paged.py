@@ -414,6 +414,41 @@ def test_infinite_values_of_both_signs(binding):
     assert torch.isfinite(out[:, 0, 1:]).all()
 
 
+@pytest.mark.parametrize("heads,kv,hd,ctx,m,at", [
+    (2, 2, 64, 0, 140, 10), (8, 1, 128, 0, 130, 3), (8, 1, 128, 0, 130, 40), (2, 1, 32, 0, 70, 0), (1, 1, 256, 0, 129, 63),
+    (2, 2, 128, 30, 100, 50), (4, 4, 128, 40, 80, 20), (1, 1, 64, 250, 100, 252), (8, 1, 64, 700, 66, 705)])
+def test_infinities_in_the_first_chunk_that_a_tile_walks(binding, heads, kv, hd, ctx, m, at):
+    """Long chunks whose tiles begin (from context 0, or in a range of keys that starts at the new tokens) with a chunk
+    of keys that only some of the rows see: values that are not finite reach the rows that see them as they are."""
+    total, page = ctx + m, 16
+    n_pages = -(-total // page) + 1
+    c = make(binding, page=page, n_pages=n_pages, max_seqs=1, max_ctx=total, max_rows=m, heads=heads, kv=kv, hd=hd)
+    books = ref.Books(page, n_pages, 1)
+    books.plan([0], [ctx], [m])
+    c.plan(ints([0]), ints([ctx]), ints([m]), rows=m)
+    kp, vp = fill(c, books, [0], [total], seed=hd)
+    q = torch.randn(m, heads, hd, generator=torch.Generator(device="cuda").manual_seed(m), device="cuda").bfloat16()
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    c.attn(q, kp, vp, want)
+    assert torch.isfinite(want).all()
+    inf, nan = float("inf"), float("nan")
+    put = [(at, 3, inf), (at, 4, -inf), (at, 5, nan), (at, 6, inf), (at + 2, 6, -inf), (at + 1, hd - 1, inf)]
+    for t, d, value in put:
+        vp[books.table[0][t // page], :, t % page, d] = value
+    c.attn(q, kp, vp, out)
+    keep = [d for d in range(hd) if d not in (3, 4, 5, 6, hd - 1)]
+    assert torch.equal(out[..., keep], want[..., keep])
+    for d in (3, 4, 5, 6, hd - 1):
+        for i in range(m):
+            seen = [value for t, e, value in put if e == d and t <= ctx + i]
+            if not seen:
+                assert torch.equal(out[i, :, d], want[i, :, d])
+            elif sum(seen) != sum(seen):
+                assert torch.isnan(out[i, :, d]).all(), (i, d)
+            else:
+                assert (out[i, :, d] == seen[0]).all(), (i, d, out[i, :, d])
+
+
 def test_scores_far_apart_and_all_the_same(binding):
     """A row whose one key outweighs the others by more than fp32's range, and rows of equal scores."""
     c = make(binding, page=16, n_pages=80, max_seqs=2, max_ctx=1200, max_rows=4, heads=2, kv=1, hd=64)
