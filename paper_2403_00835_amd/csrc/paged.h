@@ -25,7 +25,7 @@ constexpr int kPagedWaveRows = 16;
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
 constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
 constexpr int kAllSpans = 1 << 30;
-constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cache
+constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cache: 1024 requests' sums fit 31 bits
 constexpr int kPagedTileGroups = 512;   // workgroups that fill the device (two a CU): tiles of few requests are split into
                                         // about as many
 
@@ -82,7 +82,7 @@ struct PagedPlanParams {
     int group, n_kv;                // query heads per key head, key heads
     bool tiled;                     // long chunks take tiles
     int block_rows;                 // of the others
-    int cap_part, cap_tile_part;    // partial rows of row blocks, and of tiles behind them
+    int cap_part;                   // partial rows of row blocks; those of tiles are behind them
 };
 
 struct PagedAppendParams {

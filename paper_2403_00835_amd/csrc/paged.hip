@@ -113,7 +113,7 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // table). 16 requests: 3.5 to 4.9 us; 512 requests of 1 to 64 tokens: 26 us, of which the rows'
 // slots are most.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
-    __shared__ int s_wave[6][kPlanWaves], s_wave2[6][kPlanWaves];
+    __shared__ int s_wave[8][kPlanWaves], s_wave2[5][kPlanWaves];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
     __shared__ int s_unit[kPlanThreads + 1], s_tile[kPlanThreads + 1], s_item[kPlanThreads + 1], s_part[kPlanThreads], s_ranges[kPlanThreads];
     __shared__ int s_seq[kPlanThreads], s_ctx[kPlanThreads], s_m[kPlanThreads], s_own[kPlanThreads];
@@ -128,7 +128,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         m = p.neu[b];
     }
     if (b < kPagedMaxSeqs / 32) s_seen[b] = 0;
-    if (b < 6 * kPlanWaves) (&s_wave[0][0])[b] = (&s_wave2[0][0])[b] = 0;
+    if (b < 8 * kPlanWaves) (&s_wave[0][0])[b] = 0;
+    if (b < 5 * kPlanWaves) (&s_wave2[0][0])[b] = 0;
     __syncthreads();
     bool bad = false;
     int own = 0, need = 0;
@@ -142,20 +143,26 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         if (bad) m = 0;
     }
     int flags = __syncthreads_or(bad) ? PF_ARG : 0;
-    // 1024 requests of at most 2^20 new tokens: the sums fit 31 bits
+    // (1024 requests of at most 2^20 new tokens: the sum of those fits 31 bits, and the others' are used only where
+    // it is within max_rows: at most 2^20 tokens of up to 2^10 rows)
     const int T0 = m * p.group;  // rows of the request's attention
     const bool tiled = p.tiled && T0 > kPagedFewRows;
     const int nrb = tiled ? 0 : (T0 + p.block_rows - 1) / p.block_rows;
     const bool many = p.tiled && !tiled && T0 > kPagedWaveRows;
     const int ntile = tiled ? (T0 + kPagedTileRows - 1) / kPagedTileRows : 0;
     const int spans = (ctx + max(m, 1) - 1) / kPagedSpanKeys + 1;
+    // Partial rows that splitting the request's row blocks takes. Requests of few rows have the first places in the
+    // partials: they always fit, but for fp32 pools of 2^20 such rows. Larger ones (fp32) come behind; one that alone
+    // is too large takes no place.
+    const int64_t rows_spans = (int64_t)T0 * spans;
+    const bool first = T0 <= kPagedFewRows;
+    const int want = nrb && spans > 1 && rows_spans <= p.cap_part ? (int)rows_spans : 0;
     // (bf16 row blocks, at most 4 each, take 13 bits: above them the number of requests that may be taken whole)
-    int v[6] = {m, max(own - need, 0), max(need - own, 0), many ? nrb + kMany : nrb, ntile, (int)min((int64_t)nrb * spans, (int64_t)kPartRows)},
-        total[6];
+    int v[8] = {m, max(own - need, 0), max(need - own, 0), many ? nrb + kMany : nrb, ntile, want ? nrb * spans : nrb,
+                first ? want : 0, first ? 0 : want}, total[8];
     block_scan(v, total, s_wave);
     const int wholes = p.tiled ? total[3] / kMany : 0;
     total[3] -= wholes * kMany;
-    if (p.tiled) v[3] %= kMany;
     const int R = total[0], G = total[1], T = total[2];
     if (R > p.rows) flags |= PF_ROWS;
     if (T > free0 + G) flags |= PF_PAGES;
@@ -169,9 +176,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     }
     // Attention units. Row blocks: as many spans of the request's keys (up to its last token: a unit of
     // spans that its block does not see does nothing) as make about kPagedUnits workgroups of the plan, a
-    // partial state per span where there are several. Tiles: ranges of keys, as many as make about
-    // kPagedTileGroups workgroups of the plan's tiles, none under a span's keys. What the partials do not hold
-    // is not split (bf16 row blocks always fit).
+    // partial state per span where there are several; a request that the partials do not hold (fp32) walks its spans
+    // in one unit. Tiles: ranges of keys, as many as make about kPagedTileGroups workgroups of the plan's tiles, none
+    // under a span's keys. (Units: nrb (spans / per + 1) summed is at most kPagedUnits / n_kv and the row blocks.
+    // Ranges: only fewer than kPagedTileGroups / n_kv tiles are split, into at most that many more. Both are
+    // within what the cache has room for.)
     const int per = max((int)(((int64_t)total[5] * p.n_kv + kPagedUnits - 1) / kPagedUnits), 1);
     const int ranges = total[4] > 0 ? (kPagedTileGroups + total[4] * p.n_kv - 1) / (total[4] * p.n_kv) : 1;
     const int nr = ntile ? min(ranges, spans) : 1, items = (T0 + kPagedItemRows - 1) / kPagedItemRows;
@@ -179,16 +188,12 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     // mean keys and would be worked on alone at the end.
     const bool late = many && (int64_t)spans * total[3] > 2 * (int64_t)total[5];
     const bool whole = wholes * p.n_kv >= kPagedTileGroups && !__syncthreads_or(late) && many;  // (uniform but for the last)
-    const bool dparts = nrb && spans > 1 && !whole, tparts = nr > 1;
-    // (an fp32 chunk of 2^20 or more partial rows asks for more than there can be, and nothing is split)
-    const int64_t want = (int64_t)spans * T0;
-    const int few = want < kPartRows ? (spans + per - 1) / per : 1;
-    int x[6] = {whole ? 1 : nrb * few, dparts ? items : 0, dparts ? (int)min(want, (int64_t)kPartRows) : 0, ntile * nr, tparts ? items : 0,
-                tparts ? nr * T0 : 0}, y[6];
+    const int place = first ? v[6] : total[6] + v[7];
+    const bool dparts = want && !whole && place <= p.cap_part - want, tparts = nr > 1;
+    int x[5] = {whole ? 1 : nrb * (dparts ? (spans + per - 1) / per : 1), dparts ? items : 0, ntile * nr, tparts ? items : 0,
+                tparts ? nr * T0 : 0}, y[5];
     block_scan(x, y, s_wave2);
-    const bool dsplit = y[0] <= bk.cap_units && y[2] <= p.cap_part, tsplit = y[3] <= bk.cap_tiles && y[5] <= p.cap_tile_part;
-    const int U = dsplit ? y[0] : total[3], UT = tsplit ? y[3] : total[4];
-    const int I = (dsplit ? y[1] : 0) + (tsplit ? y[4] : 0);
+    const int U = y[0], UT = y[2], I = y[1] + y[3];
     s_seq[b] = seq;
     s_ctx[b] = ctx;
     s_m[b] = m;
@@ -196,11 +201,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     s_rows[b] = v[0];
     s_give[b] = v[1];
     s_take[b] = v[2];
-    s_unit[b] = dsplit ? x[0] : v[3];
-    s_tile[b] = tsplit ? x[3] : v[4];
-    s_item[b] = (dsplit ? x[1] : 0) + (tsplit ? x[4] : 0);
-    s_part[b] = dparts && dsplit ? x[2] : tparts && tsplit ? p.cap_part + x[5] : -1;
-    s_ranges[b] = !ntile ? (whole && dsplit ? -1 : 0) : tsplit ? nr : 1;
+    s_unit[b] = x[0];
+    s_tile[b] = x[2];
+    s_item[b] = x[1] + x[3];
+    s_part[b] = dparts ? place : tparts ? p.cap_part + x[4] : -1;
+    s_ranges[b] = ntile ? nr : whole ? -1 : 0;
     if (b == 0) {  // behind the last thread's
         const int end = blockDim.x;
         s_rows[end] = R;

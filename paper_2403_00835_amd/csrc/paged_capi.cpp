@@ -110,8 +110,8 @@ Bufs buffers(cllm_paged *c) {
     // Attention units: row blocks and tiles of any plan, and what splitting adds (kPagedUnits /
     // n_kv_heads row blocks, kPagedTileGroups / n_kv_heads tiles, about). Partial states of row blocks: a request
     // of few rows has up to kPagedFewRows in each of its spans, which are those of the pool and one more each
-    // (every bf16 plan; fp32 chunks of more rows may need more, and are then not split). Of tiles: as many
-    // rows as split tiles have.
+    // (every bf16 plan; fp32 chunks of more rows get what is left, and are not split where that is too little). Of
+    // tiles: as many rows as split tiles have.
     c->tiled = c->bf16;
     c->block_rows = paged_block_rows(c->bf16, f.head_dim);
     const int64_t nrows = (int64_t)f.max_rows * c->group;
@@ -308,7 +308,6 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
     p.tiled = c->tiled;
     p.block_rows = c->block_rows;
     p.cap_part = c->cap_part;
-    p.cap_tile_part = c->cap_tile_part;
     HIPCHK(c, launch_paged_plan(p, c->stream));
     c->planned = true;
     c->n = n;

@@ -554,6 +554,46 @@ def test_offsets_past_32_bits(binding, new):
         assert (np.abs(host(out[i:i + 1]) - want) <= tol).all()
 
 
+def joined(c):
+    """Row blocks of the last plan whose spans are joined: those of requests that are split over several workgroups
+    (word 9 of the status block, the first words of the cache's memory)."""
+    return int(c._ws[:64].view(torch.int32)[9])
+
+
+@pytest.mark.parametrize("heads,kv,chunk", [(1, 1, 200), (1, 1, 2000), (8, 2, 90)])
+def test_a_long_fp32_chunk_leaves_the_others_their_split(binding, heads, kv, chunk):
+    """Tokens and a block over long contexts are worked on by many workgroups also beside a chunk that has more
+    partial states than the cache holds, wherever in the plan that is, with the bits of a plan of their own."""
+    page, hd, n = 64, 32, 4
+    seq, ctx, new = [3, 1, 0, 2], [5000, 9000, 3000, 4100], [1, chunk, 16, 1]
+    total = [a + b for a, b in zip(ctx, new)]
+    n_pages = sum(-(-t // page) for t in total)
+    c = make(binding, page=page, n_pages=n_pages, max_seqs=n, max_ctx=max(total), max_rows=sum(new), heads=heads, kv=kv, hd=hd,
+             dtype="f32")
+    g = torch.Generator(device="cuda").manual_seed(chunk)
+    pools = [torch.randn(c.pool_shape, generator=g, device="cuda") for _ in range(2)]
+    q = torch.randn(sum(new), heads, hd, generator=g, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(sum(new), heads, device="cuda")
+    c.plan(ints(seq), ints(ctx), ints(new), rows=sum(new))  # all pages are taken
+    whole = joined(c)
+    c.attn(q, *pools, out, lse=lse)
+    few, r = 0, 0
+    for s, a, m in zip(seq, ctx, new):
+        c.plan(ints([s]), ints([a]), ints([m]), rows=m)
+        few += joined(c) if m < chunk else 0
+        o, ls = torch.empty_like(q[:m]), torch.empty_like(lse[:m])
+        c.attn(q[r:r + m], *pools, o, lse=ls)
+        assert torch.equal(o, out[r:r + m]) and torch.equal(ls, lse[r:r + m])
+        pages = c.block_table[s, :-(-(a + m) // page)].cpu().numpy()
+        k, v = (ref.gather(host(p), pages, a + m) for p in pools)
+        for i in (0, m - 1):  # against the formula
+            want, wl, mag = ref.attend(host(q[r + i:r + i + 1]), k[:, :a + i + 1], v[:, :a + i + 1], a + i, hd ** -0.5)
+            tol, tl = tolerance(c, host(q[r + i:r + i + 1]), k[:, :a + i + 1], want, wl, mag, hd ** -0.5, a + i + 1)
+            assert (np.abs(host(out[r + i]) - want[0]) <= tol[0]).all() and (np.abs(host(lse[r + i]) - wl[0]) <= tl[0]).all()
+        r += m
+    assert few >= 3 and whole >= few
+
+
 # ---------------------------------------------------------------------------------- run together
 class Layers:
     """Two attention layers with random projections, in fp32: what a decoder does around the operators."""
