@@ -6,11 +6,14 @@
 namespace cllm {
 
 constexpr int kPagedMaxSeqs = 1024;   // one plan thread per request
-// Rows of a request's attention: new tokens x heads of a group. Requests of few rows (a token, a Jacobi
-// block), and fp32, take units of paged_block_rows() rows and spans of keys; longer bf16 chunks take tiles
-// of kPagedTileRows rows and a range of keys. Up to 64 a row's bits are those of a plan of its own, as every
-// block length needs; tiles of 33 rows at 600 keys take 16.3 us in place of 14.7 (32 heads of 128), 16
-// requests of 64 rows at 1000 keys 65 in place of 72.
+// Rows of a request's attention: new tokens x heads of a group. Requests of few rows, and fp32, take units of
+// paged_block_rows() rows and spans of keys; longer bf16 chunks take tiles of kPagedTileRows rows and a range of
+// keys. Up to 64 rows a row's bits are those of a plan of its own: every block length of the library's decoding has
+// them with one query head per key head, blocks of up to 64 / group tokens with grouped ones. Larger ones in spans, by
+// tokens in place of rows, would take longer: 32 over 8 heads of 128, one block of 64 tokens at 2304 keys 26.5 us
+// in place of 19.1, 16 of 17 at 1000 45.8 in place of 29.7, 64 of 32 at 2000 190 in place of 129, and the partials of a
+// 1.2 GB workspace. Tiles of 33 rows at 600 keys take 16.3 us in place of 14.7 (32 heads of 128), 16 requests of 64
+// rows at 1000 keys 65 in place of 72.
 constexpr int kPagedFewRows = 64;
 constexpr int kPagedTileRows = 128;
 constexpr int kPagedItemRows = 32;    // rows that are joined together

@@ -520,6 +520,50 @@ def test_a_rows_bits_do_not_depend_on_the_call(binding, dtype, heads, kv, hd, pa
     assert torch.equal(q2, out)
 
 
+@pytest.mark.parametrize("heads,kv,hd,page,ctx,m", [(32, 8, 128, 64, 900, 16), (24, 8, 64, 16, 505, 21), (8, 1, 128, 32, 250, 8),
+                                                    (14, 2, 64, 16, 0, 9), (64, 1, 32, 16, 700, 1), (8, 2, 256, 64, 300, 16)])
+def test_blocks_of_grouped_heads_at_the_limit(binding, heads, kv, hd, page, ctx, m):
+    """Blocks of 64 / group tokens, the most whose rows' bits do not depend on the call."""
+    assert (m + 1) * heads // kv > 64 >= m * heads // kv
+    test_a_rows_bits_do_not_depend_on_the_call(binding, "bf16", heads, kv, hd, page, ctx, m)
+
+
+@pytest.mark.parametrize("heads,kv,hd,m", [(32, 8, 128, 64), (8, 1, 64, 30), (64, 2, 32, 5)])
+def test_a_longer_block_of_grouped_heads_in_steps(binding, heads, kv, hd, m):
+    """A block above the limit, run in steps of 64 / group tokens beside other requests: the bits of its tokens one by one.
+    As one chunk it has the long chunks' weights, one bf16 plane."""
+    ctx, others, page, k = 700, 9, 32, 64 * kv // heads
+    total, n = ctx + m, others + 1
+    n_pages = -(-total // page) + others * -(-(400 + m) // page)
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    x = torch.randn(m, heads + 2 * kv, hd, generator=g, device="cuda").bfloat16()
+    first = [torch.randn(n_pages, kv, page, hd, generator=g, device="cuda").bfloat16() for _ in range(2)]
+
+    def run(step, beside):
+        c = make(binding, page=page, n_pages=n_pages, max_seqs=n, max_ctx=total, max_rows=m * n, heads=heads, kv=kv, hd=hd,
+                 rope_base=10000.0)
+        pools, out, r = [p.clone() for p in first], torch.empty(m, heads, hd, device="cuda").bfloat16(), 0
+        c.plan(ints([0]), ints([ctx]), ints([0]), rows=0)  # the context: the first pages
+        while r < m:
+            j = min(step, m - r)
+            new, ctxs = [j] + [step] * beside, [ctx + r] + [40 * b + r for b in range(beside)]
+            y = torch.randn(sum(new), heads + 2 * kv, hd, generator=g, device="cuda").bfloat16()
+            y[:j] = x[r:r + j]
+            q, o = y[:, :heads], torch.empty(sum(new), heads, hd, device="cuda").bfloat16()
+            c.plan(ints(list(range(1 + beside))), ints(ctxs), ints(new), rows=sum(new))
+            c.append(q, y[:, heads:heads + kv], y[:, heads + kv:], q, *pools)
+            c.attn(q, *pools, o)
+            out[r:r + j] = o[:j]
+            r += j
+        assert c.status()[0] == sum(new)
+        return out
+
+    want = run(1, 0)
+    assert torch.equal(run(k, 0), want) and torch.equal(run(k, others), want)
+    # against the tokens: two half steps of the output and the half step of the weights, of values up to 6
+    assert (run(m, 0).float() - want.float()).abs().max() <= 2.0**-8 * 3 * 6
+
+
 @pytest.mark.parametrize("new", [1, 130], ids=["token", "chunk"])
 def test_offsets_past_32_bits(binding, new):
     """A request in the last pages of pools of more than 2^31 elements."""
