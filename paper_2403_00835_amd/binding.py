@@ -415,6 +415,9 @@ class PagedCache:
         cache.plan(seq_ids, ctx_lens, new_lens, rows)      # pages and rows of the step
         per layer: cache.append(q, k, v, q, k_pages, v_pages); cache.attn(q, k_pages, v_pages, out)
 
+    The operators have no backward: a tensor that requires grad is refused unless gradients are off
+    (torch.no_grad(), torch.inference_mode()).
+
     Work is queued on the stream given at creation (None: PyTorch's current one), which has to be
     PyTorch's current stream in every call. block_table, seq_pages, free_list, row_start, row_slot and
     row_pos are int32 tensors over the cache's own books, to be read in that stream's order."""
@@ -489,6 +492,11 @@ class PagedCache:
         if self._current() != self.stream:
             raise ValueError("PyTorch's current stream is not the cache's")
 
+    def _no_backward(self, name):
+        import torch
+        if torch.is_grad_enabled():
+            raise ValueError(f"{name} requires grad, and the paged operators have no backward: call them under torch.no_grad()")
+
     def _lens(self, x, n):
         import torch
         if x.dtype != torch.int32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous() or x.device != self.device:
@@ -504,12 +512,16 @@ class PagedCache:
         if not whole or s[0] < self.rows or x.dtype != self.dtype or x.device != self.device:
             raise ValueError(f"{name}: at least {self.rows} rows of {heads} x {self.head_dim} {self.dtype} with contiguous "
                              f"heads on {self.device}, got {x.dtype} {tuple(s)} strides {tuple(t)} on {x.device}")
+        if x.requires_grad:
+            self._no_backward(name)
         return x.data_ptr(), (t[0] if s[0] > 1 else heads * self.head_dim)
 
     def _pool(self, x, name):
         if tuple(x.shape) != self.pool_shape or x.dtype != self.dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{name}: a contiguous {self.dtype} tensor {self.pool_shape} on {self.device}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
+        if x.requires_grad:
+            self._no_backward(name)
         return x.data_ptr()
 
     def plan(self, seq_ids, ctx_lens, new_lens, rows, max_new=0, max_len=0):
@@ -544,6 +556,8 @@ class PagedCache:
             if lse.dtype != torch.float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
                     not lse.is_contiguous() or lse.device != self.device:
                 raise ValueError(f"lse: a contiguous float32 tensor of at least {self.rows} x {self.n_heads} on {self.device}")
+            if lse.requires_grad:
+                self._no_backward("lse")
         self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
                                            self._pool(v_pages, "v_pages"), scale or 0.0, *self._rows(out, self.n_heads, "out"),
                                            None if lse is None else lse.data_ptr()))

@@ -1,0 +1,56 @@
+"""The checks of binding.PagedCache itself, on host tensors: a cache whose library only counts its calls."""
+import types
+
+import pytest
+
+from paper_2403_00835_amd import binding
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture
+def cache():
+    c = object.__new__(binding.PagedCache)
+    calls = []
+
+    def entry(name):
+        return lambda *a: calls.append((name, a)) or 0
+
+    c.L = types.SimpleNamespace(cllm_paged_append=entry("append"), cllm_paged_attn=entry("attn"), cllm_paged_plan=entry("plan"))
+    c.h, c.stream, c._current, c.device = 1, 0, lambda: 0, torch.device("cpu")
+    c.n_heads, c.n_kv_heads, c.head_dim, c.dtype, c.rows = 4, 2, 32, torch.float32, 3
+    c.pool_shape = (5, 2, 16, 32)
+    c._ws = torch.zeros(64, dtype=torch.uint8)
+    c.calls = calls
+    yield c
+    c.h = None
+
+
+def arrays():
+    q, k, v, out = (torch.zeros(3, h, 32) for h in (4, 2, 2, 4))
+    return dict(q=q, k=k, v=v, out=out, kp=torch.zeros(5, 2, 16, 32), vp=torch.zeros(5, 2, 16, 32), lse=torch.zeros(3, 4))
+
+
+def call(c, name, a):
+    if name == "append":
+        c.append(a["q"], a["k"], a["v"], a["out"], a["kp"], a["vp"])
+    elif name == "attn":
+        c.attn(a["q"], a["kp"], a["vp"], a["out"], lse=a["lse"])
+    else:
+        n = torch.ones(2, dtype=torch.int32)
+        c.plan(n, n, n, rows=3)
+
+
+@pytest.mark.parametrize("name,which", [("append", x) for x in ("q", "k", "v", "out", "kp", "vp")] +
+                         [("attn", x) for x in ("q", "out", "kp", "vp", "lse")])
+def test_tensors_that_require_grad_are_refused(cache, name, which):
+    a = arrays()
+    a[which].requires_grad_()
+    with pytest.raises(ValueError, match="grad"):
+        call(cache, name, a)
+    assert cache.calls == []
+    with torch.no_grad():  # as torch's own operators with an output argument have it
+        call(cache, name, a)
+    with torch.inference_mode():
+        call(cache, name, arrays())
+    assert [x[0] for x in cache.calls] == [name, name]
