@@ -408,6 +408,18 @@ def _dev_ptr(x, count, dtype):
     return x.data_ptr()
 
 
+_increment_version = None
+
+
+def _changed(*tensors):
+    """Tells autograd that a call has written the tensors (through their addresses, which it does not see)."""
+    global _increment_version
+    if _increment_version is None:
+        from torch.autograd.graph import increment_version
+        _increment_version = increment_version
+    _increment_version(tensors)
+
+
 class PagedCache:
     """A paged KV cache (cllm_paged_*): the books of a page pool that the requests of a server share,
     and the operators of a step on it, on PyTorch tensors of the cache's GPU:
@@ -432,6 +444,7 @@ class PagedCache:
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
         self.max_rows, self.rows = max_rows, 0
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self._int32, self._float32 = torch.int32, torch.float32
         self.pool_shape = (n_pages, n_kv_heads, page_size, head_dim)
         cfg = cllm_paged_config(n_heads, n_kv_heads, head_dim, 1 if dtype == "bf16" else 0, page_size, n_pages, max_seqs,
                                 max_ctx, max_rows, rope_base, device, None, None, 0)
@@ -498,8 +511,7 @@ class PagedCache:
             raise ValueError(f"{name} requires grad, and the paged operators have no backward: call them under torch.no_grad()")
 
     def _lens(self, x, n):
-        import torch
-        if x.dtype != torch.int32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous() or x.device != self.device:
+        if x.dtype != self._int32 or x.dim() != 1 or x.numel() != n or not x.is_contiguous() or x.device != self.device:
             raise ValueError(f"lengths: contiguous int32 tensors of one size on {self.device}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
         return x.data_ptr()
@@ -517,7 +529,7 @@ class PagedCache:
         return x.data_ptr(), (t[0] if s[0] > 1 else heads * self.head_dim)
 
     def _pool(self, x, name):
-        if tuple(x.shape) != self.pool_shape or x.dtype != self.dtype or x.device != self.device or not x.is_contiguous():
+        if x.shape != self.pool_shape or x.dtype != self.dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{name}: a contiguous {self.dtype} tensor {self.pool_shape} on {self.device}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
         if x.requires_grad:
@@ -531,6 +543,7 @@ class PagedCache:
         self._check(self.L.cllm_paged_plan(self.h, n, self._lens(seq_ids, n), self._lens(ctx_lens, n),
                                            self._lens(new_lens, n), rows, max_new, max_len))
         self.rows = rows
+        _changed(self._ws)
 
     def append(self, q, k, v, q_out, k_pages, v_pages):
         """cllm_paged_append: rows q [.., n_heads, head_dim] (or None, with q_out), k and v
@@ -544,6 +557,10 @@ class PagedCache:
         self._check(self.L.cllm_paged_append(self.h, *qa, *self._rows(k, self.n_kv_heads, "k"),
                                              *self._rows(v, self.n_kv_heads, "v"), *qo, self._pool(k_pages, "k_pages"),
                                              self._pool(v_pages, "v_pages")))
+        if q_out is None:
+            _changed(k_pages, v_pages)
+        else:
+            _changed(q_out, k_pages, v_pages)
 
     def attn(self, q, k_pages, v_pages, out, scale=None, lse=None):
         """cllm_paged_attn: rows q [.., n_heads, head_dim] over the pools into out (of q's shape); lse: a
@@ -552,8 +569,7 @@ class PagedCache:
         if scale is not None and not scale:
             raise ValueError("scale must not be 0")
         if lse is not None:
-            import torch
-            if lse.dtype != torch.float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
+            if lse.dtype != self._float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
                     not lse.is_contiguous() or lse.device != self.device:
                 raise ValueError(f"lse: a contiguous float32 tensor of at least {self.rows} x {self.n_heads} on {self.device}")
             if lse.requires_grad:
@@ -561,6 +577,10 @@ class PagedCache:
         self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
                                            self._pool(v_pages, "v_pages"), scale or 0.0, *self._rows(out, self.n_heads, "out"),
                                            None if lse is None else lse.data_ptr()))
+        if lse is None:
+            _changed(out)
+        else:
+            _changed(out, lse)
 
     def status(self):
         """cllm_paged_status: (rows of the last plan, free pages); raises when it was refused."""

@@ -19,6 +19,7 @@ def cache():
     c.L = types.SimpleNamespace(cllm_paged_append=entry("append"), cllm_paged_attn=entry("attn"), cllm_paged_plan=entry("plan"))
     c.h, c.stream, c._current, c.device = 1, 0, lambda: 0, torch.device("cpu")
     c.n_heads, c.n_kv_heads, c.head_dim, c.dtype, c.rows = 4, 2, 32, torch.float32, 3
+    c._int32, c._float32 = torch.int32, torch.float32
     c.pool_shape = (5, 2, 16, 32)
     c._ws = torch.zeros(64, dtype=torch.uint8)
     c.calls = calls
@@ -54,3 +55,30 @@ def test_tensors_that_require_grad_are_refused(cache, name, which):
     with torch.inference_mode():
         call(cache, name, arrays())
     assert [x[0] for x in cache.calls] == [name, name]
+
+
+@pytest.mark.parametrize("name,written", [("append", ("out", "kp", "vp")), ("attn", ("out", "lse"))])
+def test_written_tensors_count_as_changed(cache, name, written):
+    """What autograd saved before a call that overwrites it is refused in the backward pass, as after an in-place
+    operator of torch's own."""
+    a = arrays()
+    w = torch.ones(4, 32, requires_grad=True)
+    y = (a["out"] * w).sum()  # keeps out for w's gradient
+    before = {k: x._version for k, x in a.items()}
+    call(cache, name, a)
+    assert {k for k, x in a.items() if x._version != before[k]} == set(written)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    rows = torch.zeros(6, 4, 32)  # a view's base too
+    a["out"] = rows[1:4]
+    before = rows._version
+    call(cache, name, a)
+    assert rows._version > before
+    call(cache, name, dict(a, lse=None) if name == "attn" else a)
+
+
+def test_the_books_count_as_changed_by_a_plan(cache):
+    view = cache._ws[:8].view(torch.int32)
+    before = view._version
+    call(cache, "plan", None)
+    assert view._version > before
