@@ -482,9 +482,9 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
 
 /* Attention of the last plan's rows over the pages of one layer: out row r (of entry b, head h) =
  * softmax over the positions t <= row_pos[r] of slot seq_ids[b] of scale q[r][h] . k[t][h / group]
- * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim). lse (or NULL): fp32
- * [rows][n_heads], the natural log of the sum of exponentials of the scaled scores. out may be q with
- * q's stride. Statistics, products and sums in fp32, the output rounded once. Few rows (at most 64 / group
+ * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim), others are
+ * up to 2.35e38 in size. lse (or NULL): fp32 [rows][n_heads], the natural log of the sum of exponentials of
+ * the scaled scores. out may be q with q's stride. Statistics, products and sums in fp32, the output rounded once. Few rows (at most 64 / group
  * new tokens: with group 1 every block length of the library's decoding, with group 4 blocks of up to 16)
  * and fp32: bf16 probabilities are two bf16 planes, and a row's bits depend on its queries, its position and
  * the keys and values up to it alone, not on the chunk, the other requests, the pages or the bounds: a block

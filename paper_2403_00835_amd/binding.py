@@ -566,8 +566,8 @@ class PagedCache:
         """cllm_paged_attn: rows q [.., n_heads, head_dim] over the pools into out (of q's shape); lse: a
         contiguous float32 [.., n_heads]. scale None: 1 / sqrt(head_dim)."""
         self._on_stream()
-        if scale is not None and not scale:
-            raise ValueError("scale must not be 0")
+        if scale is not None and not _f32(scale).value:
+            raise ValueError(f"scale {scale} is 0 in float32")
         if lse is not None:
             if lse.dtype != self._float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
                     not lse.is_contiguous() or lse.device != self.device:
@@ -575,7 +575,7 @@ class PagedCache:
             if lse.requires_grad:
                 self._no_backward("lse")
         self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
-                                           self._pool(v_pages, "v_pages"), scale or 0.0, *self._rows(out, self.n_heads, "out"),
+                                           self._pool(v_pages, "v_pages"), 0.0 if scale is None else scale, *self._rows(out, self.n_heads, "out"),
                                            None if lse is None else lse.data_ptr()))
         if lse is None:
             _changed(out)

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -366,7 +367,8 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     if (!c->planned) return fail(c, CLLM_ERR_STATE, "attention before a plan");
     if (c->rows == 0) return CLLM_OK;
     const cllm_paged_config &f = c->cfg;
-    if (!std::isfinite(scale)) return fail(c, CLLM_ERR_ARG, "scale is not finite");
+    const double scale_log2 = 1.4426950408889634 * (scale == 0.0f ? 1.0 / std::sqrt((double)f.head_dim) : (double)scale);
+    if (!(std::fabs(scale_log2) <= FLT_MAX)) return fail(c, CLLM_ERR_ARG, "scale %g: not finite, or above 2.35e38", (double)scale);
     DeviceGuard dev(f.device);
     if (!dev.ok) return fail(c, CLLM_ERR_DEVICE, "the cache's device cannot be made current");
     if ((s = check_rows(c, "q", q, q_stride, f.n_heads)) || (s = check_rows(c, "out", out, out_stride, f.n_heads)) ||
@@ -395,8 +397,7 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     p.hd = f.head_dim;
     p.group = c->group;
     p.group_inv = ((1u << 24) + c->group - 1) / c->group;
-    const double sc = scale == 0.0f ? 1.0 / std::sqrt((double)f.head_dim) : (double)scale;
-    p.scale_log2 = (float)(1.4426950408889634 * sc);
+    p.scale_log2 = (float)scale_log2;
     // bounds of the launch
     auto pieces = [&](int64_t most, int rows) {  // of requests of at most `most` rows each
         return std::min(c->n * ((most + rows - 1) / rows), (int64_t)c->rows * c->group / rows + c->n);

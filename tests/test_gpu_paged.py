@@ -172,6 +172,30 @@ def test_calls_are_refused_before_the_device(binding):
         c.attn(q, *pools, q)
 
 
+def test_scales_at_the_ends_of_their_range(binding):
+    """A scale whose product with log2(e) is above fp32's range is refused; the smallest gives equal weights, and not
+    those of the default."""
+    c = make(binding, page=16, n_pages=4, max_seqs=1, max_ctx=40, max_rows=2, heads=2, kv=1, hd=32)
+    books = ref.Books(16, 4, 1)
+    books.plan([0], [30], [2])
+    c.plan(ints([0]), ints([30]), ints([2]), rows=2)
+    kp, vp = fill(c, books, [0], [32], seed=9)
+    q, out = torch.randn(2, 2, 32, device="cuda").bfloat16(), torch.full((2, 2, 32), 5.0, device="cuda").bfloat16()
+    for bad in (3e38, -3.4e38, 2.4e38, 1e39, float("nan")):
+        with pytest.raises(binding.CllmError, match="ERR_ARG.*scale"):
+            c.attn(q, kp, vp, out, scale=bad)
+    for bad in (1e-46, 0.0):
+        with pytest.raises(ValueError, match="scale"):
+            c.attn(q, kp, vp, out, scale=bad)
+    assert (out == 5).all()
+    v = ref.gather(host(vp), books.table[0], 32)[0]
+    for scale in (1e-45, -1e-45, 1e-38):  # scores of at most 2^-100: every weight is 1
+        c.attn(q, kp, vp, out, scale=scale)
+        for i in range(2):
+            want = v[:31 + i].mean(0)
+            assert (np.abs(host(out[i]) - want) <= 2.0**-8 * np.abs(want) + 2.0**-17).all()
+
+
 # ---------------------------------------------------------------------------------------- append
 @pytest.mark.parametrize("dtype,heads,kv,hd,page,ctx,new,base", [
     ("bf16", 4, 4, 128, 64, [0, 63, 100], [1, 2, 70], 10000.0), ("bf16", 14, 2, 64, 16, [5], [33], 10000.0),

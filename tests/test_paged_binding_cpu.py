@@ -82,3 +82,15 @@ def test_the_books_count_as_changed_by_a_plan(cache):
     before = view._version
     call(cache, "plan", None)
     assert view._version > before
+
+
+@pytest.mark.parametrize("scale", [0, 0.0, -0.0, 1e-46, -1e-50])
+def test_a_scale_of_0_in_fp32_is_refused(cache, scale):
+    """The library takes 0 for the default scale: what rounds to it must not."""
+    a = arrays()
+    with pytest.raises(ValueError, match="scale"):
+        cache.attn(a["q"], a["kp"], a["vp"], a["out"], scale=scale)
+    assert cache.calls == []
+    for good in (None, 1e-45, -0.5, 1.0, 3e38):
+        cache.attn(a["q"], a["kp"], a["vp"], a["out"], scale=good)
+    assert [x[1][5] for x in cache.calls] == [0.0, 1e-45, -0.5, 1.0, 3e38]
