@@ -26,7 +26,10 @@ constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >
 // token of 64 requests at 1000 to 8000 keys takes 229 us in spans, 284 whole (4 tokens at 4000: 232 and 199).
 constexpr int kPagedWaveRows = 16;
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
-constexpr int kPagedUnits = 16384;    // workgroups that the spans of a plan's row blocks make, about
+// Workgroups that the spans of a plan's row blocks make, about: above, one takes several spans. It bounds the unit
+// list. 256 tokens at 1000 to 8000 keys (32 over 8 heads of 128): 960 us, 981 of 8192 workgroups, 920 of one a span;
+// 64 blocks of 16 at 2000 to 9000 keys (32 heads of 64): 755, 764 and 773.
+constexpr int kPagedUnits = 16384;
 constexpr int kAllSpans = 1 << 30;
 constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cache: 1024 requests' sums fit 31 bits
 constexpr int kPagedTileGroups = 512;   // workgroups that fill the device (two a CU): tiles of few requests are split into

@@ -588,6 +588,51 @@ def test_a_longer_block_of_grouped_heads_in_steps(binding, heads, kv, hd, m):
     assert (run(m, 0).float() - want.float()).abs().max() <= 2.0**-8 * 3 * 6
 
 
+@pytest.mark.parametrize("dtype,heads,kv,hd,page,n,hi,lo_ctx,hi_ctx,far", [
+    ("bf16", 32, 32, 32, 64, 64, 16, 1000, 4000, 0), ("bf16", 64, 32, 32, 16, 48, 8, 200, 9000, 0),
+    ("bf16", 32, 32, 32, 64, 101, 60, 800, 2500, 9000), ("bf16", 16, 16, 128, 64, 96, 1, 3000, 5000, 0),
+    ("f32", 32, 32, 16, 32, 99, 40, 500, 2500, 9000)])
+def test_full_plans_give_a_workgroup_several_spans(binding, dtype, heads, kv, hd, page, n, hi, lo_ctx, hi_ctx, far):
+    """Row blocks whose spans of all key heads are above 16384: a workgroup takes several, one after another, the last
+    one of a request fewer. The formula for some requests, and the bits of a plan of its own."""
+    rng = random.Random(hd + n)
+    new = [rng.randint(1, hi) for _ in range(n)]
+    ctx = [rng.randint(lo_ctx, hi_ctx) for _ in range(n)]
+    if far:  # a request of more than twice the mean keys, so that none is taken whole
+        ctx[5], new[5] = far, hi
+    total = [a + b for a, b in zip(ctx, new)]
+    n_pages = sum(-(-t // page) for t in total)
+    c = make(binding, page=page, n_pages=n_pages, max_seqs=n, max_ctx=max(total), max_rows=sum(new), heads=heads, kv=kv, hd=hd,
+             dtype=dtype)
+    rows = 16 if hd * (2 if dtype == "bf16" else 4) >= 512 else 32
+    blocks = [-(-m * heads // kv // rows) for m in new]
+    spans = [(t - 1) // 256 + 1 for t in total]
+    units = sum(b * s for b, s in zip(blocks, spans))
+    per = -(-units * kv // 16384)
+    assert per > 1 and units * kv % 16384 and any(s % per for s in spans)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    kp, vp = (torch.randn(c.pool_shape, generator=g, device="cuda").to(c.dtype) for _ in range(2))
+    q = (torch.randn(sum(new), heads, hd, generator=g, device="cuda") * 1.5).to(c.dtype)
+    out, lse = torch.empty_like(q), torch.empty(sum(new), heads, device="cuda")
+    c.plan(ints(list(range(n))), ints(ctx), ints(new), rows=sum(new))
+    took = int(c._ws[:64].view(torch.int32)[4])  # the plan's units: a word of the status block
+    assert took == sum(b * -(-s // per) for b, s in zip(blocks, spans))
+    c.attn(q, kp, vp, out, lse=lse)
+    start = np.concatenate([[0], np.cumsum(new)])
+    for s in (0, 5, n // 2, n - 1):
+        c.plan(ints([s]), ints([ctx[s]]), ints([new[s]]), rows=new[s])
+        qs, o, ls = q[start[s]:start[s + 1]], torch.empty_like(q[:new[s]]), torch.empty_like(lse[:new[s]])
+        c.attn(qs, kp, vp, o, lse=ls)
+        assert torch.equal(o, out[start[s]:start[s + 1]]) and torch.equal(ls, lse[start[s]:start[s + 1]])
+        pages = c.block_table[s, :-(-total[s] // page)].long()
+        k, v = (ref.gather(host(p[pages]), range(len(pages)), total[s]) for p in (kp, vp))
+        for i in {0, new[s] - 1}:
+            t = ctx[s] + i + 1
+            want, wl, mag = ref.attend(host(qs[i:i + 1]), k[:, :t], v[:, :t], t - 1, hd ** -0.5)
+            tol, tl = tolerance(c, host(qs[i:i + 1]), k[:, :t], want, wl, mag, hd ** -0.5, t)
+            assert (np.abs(host(o[i]) - want[0]) <= tol[0]).all() and (np.abs(host(ls[i]) - wl[0]) <= tl[0]).all()
+
+
 @pytest.mark.parametrize("new", [1, 130], ids=["token", "chunk"])
 def test_offsets_past_32_bits(binding, new):
     """A request in the last pages of pools of more than 2^31 elements."""
