@@ -448,7 +448,8 @@ cllm_status cllm_paged_workspace_bytes(const cllm_paged_config *cfg, size_t *byt
 /* An empty cache. Synchronous. Errors: ERR_ARG (shape, workspace), ERR_CAPACITY (workspace too small),
  * ERR_OOM, ERR_DEVICE. */
 cllm_status cllm_paged_create(const cllm_paged_config *cfg, cllm_paged **out);
-/* The caller has waited for the cache's stream before it frees the cache or a workspace of its own. */
+/* Without a workspace of the caller's: waits for the device. With one: makes no device call, and work in flight goes
+ * on; the caller has waited for the cache's stream before it frees the workspace. */
 void cllm_paged_free(cllm_paged *c);
 /* Errors: ERR_ARG. */
 cllm_status cllm_paged_views_get(cllm_paged *c, cllm_paged_views *views);

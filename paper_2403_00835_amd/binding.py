@@ -461,6 +461,7 @@ class PagedCache:
         self._ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
         if self.stream != cur.cuda_stream:
             cur.synchronize()  # the memory's last user in the allocator's order
+            self._ws.record_stream(torch.cuda.ExternalStream(self.stream, device=self.device))
         cfg.stream, cfg.workspace, cfg.workspace_bytes = self.stream, self._ws.data_ptr(), n.value
         h = _vp()
         st = self.L.cllm_paged_create(ctypes.byref(cfg), ctypes.byref(h))
@@ -482,9 +483,9 @@ class PagedCache:
         self.row_pos = view(v.row_pos, max_rows)
 
     def close(self):
+        """Ends the cache. Waits for nothing (a graph may be in capture): work in flight has the books until PyTorch's
+        allocator gives their memory to another user, in the stream's order."""
         if getattr(self, "h", None):
-            import torch
-            torch.cuda.synchronize(self.device)  # work in flight still reads the books
             self.L.cllm_paged_free(self.h)
             self.h = None
 

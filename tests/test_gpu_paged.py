@@ -897,3 +897,52 @@ def test_two_caches_side_by_side(binding):
         for c, *_ in caches:
             c.close()
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_a_cache_made_for_a_stream_that_is_not_current(binding):
+    """stream= at creation: the calls are made with that stream current, and refused with any other."""
+    side, got = torch.cuda.Stream(), []
+    for stream in (None, side.cuda_stream):
+        c = make(binding, page=16, n_pages=30, max_seqs=2, max_ctx=200, max_rows=8, heads=4, kv=2, hd=64, rope_base=10000.0,
+                 stream=stream)
+        if stream is not None:
+            with pytest.raises(ValueError, match="stream"):
+                c.plan(ints([0]), ints([0]), ints([1]), rows=1)
+        with torch.cuda.stream(side) if stream else torch.cuda.stream(torch.cuda.current_stream()):
+            g = torch.Generator(device="cuda").manual_seed(4)
+            pools = [torch.randn(c.pool_shape, generator=g, device="cuda").bfloat16() for _ in range(2)]
+            x, out = torch.randn(8, 8, 64, generator=g, device="cuda").bfloat16(), torch.empty(8, 4, 64, device="cuda").bfloat16()
+            c.plan(ints([1, 0]), ints([150, 20]), ints([3, 5]), rows=8)
+            c.append(x[:, :4], x[:, 4:6], x[:, 6:], x[:, :4], *pools)
+            c.attn(x[:, :4], *pools, out)
+            assert c.status() == (8, 30 - 10 - 2)
+            got.append(out.clone())
+            torch.cuda.current_stream().synchronize()
+        c.close()
+    assert torch.equal(*got)
+
+
+def test_a_cache_that_ends_while_a_graph_is_captured(binding):
+    """Closing a cache, or dropping it, waits for nothing: another cache's step can be in capture meanwhile."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        kw = dict(page=16, n_pages=30, max_seqs=2, max_ctx=200, max_rows=8, heads=4, kv=2, hd=64)
+        c, old = make(binding, **kw), [make(binding, **kw) for _ in range(2)]
+        pools = [torch.randn(c.pool_shape, device="cuda").bfloat16() for _ in range(2)]
+        q = torch.randn(8, 4, 64, device="cuda").bfloat16()
+        want, out = torch.empty_like(q), torch.empty_like(q)
+        for x in [c] + old:
+            x.plan(ints([0, 1]), ints([150, 20]), ints([3, 5]), rows=8)
+            x.attn(q, *pools, want)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            old.pop().close()
+            c.attn(q, *pools, out)
+            old.pop()
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(out, want)
+        del graph
