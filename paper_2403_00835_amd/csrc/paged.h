@@ -12,8 +12,8 @@ constexpr int kPagedMaxSeqs = 1024;   // one plan thread per request
 // them with one query head per key head, blocks of up to 64 / group tokens with grouped ones. Larger ones in spans, by
 // tokens in place of rows, would take longer: 32 over 8 heads of 128, one block of 64 tokens at 2304 keys 26.5 us
 // in place of 19.1, 16 of 17 at 1000 45.8 in place of 29.7, 64 of 32 at 2000 190 in place of 129, and the partials of a
-// 1.2 GB workspace. Tiles of 33 rows at 600 keys take 16.3 us in place of 14.7 (32 heads of 128), 16 requests of 64
-// rows at 1000 keys 65 in place of 72.
+// 1.2 GB workspace. Tiles from 33 rows on (32 heads of 128): 33 rows at 600 keys 16.6 us in place of 14.8, 64 at 2304 24
+// in place of 28, 16 requests of 64 at 1000 64 in place of 69.
 constexpr int kPagedFewRows = 64;
 constexpr int kPagedTileRows = 128;
 constexpr int kPagedItemRows = 32;    // rows that are joined together
@@ -21,9 +21,9 @@ constexpr int kPagedItemRows = 32;    // rows that are joined together
 constexpr int paged_block_rows(bool bf16, int hd) { return hd * (bf16 ? 2 : 4) >= 512 ? 16 : 32; }
 // Where bf16 requests of few, but more than kPagedWaveRows rows make kPagedTileGroups workgroups or more, a
 // workgroup takes a whole request: its keys once for all rows, no partial states. 64 requests of 36 rows at 4000
-// keys (8 key heads of 128): 400 us in spans, 205 whole; 16 of 64 rows at 1000 keys (32 heads): 144 and 72; of
-// 32 rows: 85 and 61. Up to 16 rows spans read the keys once too, and do not wait for the longest request: a
-// token of 64 requests at 1000 to 8000 keys takes 229 us in spans, 284 whole (4 tokens at 4000: 232 and 199).
+// keys (8 key heads of 128): 433 us in spans, 205 whole; 16 of 64 rows at 1000 keys (32 heads): 153 and 69; of
+// 32 rows: 90 and 58. Up to 16 rows spans read the keys once too, and do not wait for the longest request: a
+// token of 64 requests at 1000 to 8000 keys takes 241 us in spans, 282 whole (4 tokens at 4000: 227 and 193).
 constexpr int kPagedWaveRows = 16;
 constexpr int kPagedSpanKeys = 256;   // keys of a span, at absolute positions
 // Workgroups that the spans of a plan's row blocks make, about: above, one takes several spans. It bounds the unit

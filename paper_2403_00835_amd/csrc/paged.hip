@@ -110,8 +110,8 @@ __global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64
 // (bad slot or length, more rows than the bound, too few pages) leaves the books as they were and has
 // no rows.
 // Bound: one CU's latency: four barriers and sums, then a round trip per dependent read (lengths, pages owned,
-// table). 16 requests: 3.5 to 4.9 us; 512 requests of 1 to 64 tokens: 26 us, of which the rows'
-// slots are most.
+// table). 16 requests of 32 tokens: 6.6 us, giving their pages back 3.4; 512 of 1 to 64: 26 and 8.7, of which the
+// rows' slots are most: work that one CU does here for a step of 16,000 rows.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParams p) {
     __shared__ int s_wave[8][kPlanWaves], s_wave2[5][kPlanWaves];
     __shared__ int s_rows[kPlanThreads + 1], s_give[kPlanThreads + 1], s_take[kPlanThreads + 1];
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
 // Rows of the step: queries and keys turned by their positions (rotate-half: (a c - b s, b c + a s) of
 // a head's halves a, b), in fp32 and rounded once; keys and values into their slots. A thread takes
 // 16 bytes of each half of one head of one row.
-// Bound: memory: 197 MB (5 prompts, 8000 rows of 32 and 8 heads of 128) in 31 us, 6.3 TB/s; 512 rows 6.1 us, 8
-// rows 2.1.
+// Bound: memory: 197 MB (5 prompts, 8000 rows of 32 and 8 heads of 128) in 31 us, 6.3 TB/s (some of it in the
+// last-level cache); 512 rows 6.0 us, 8 rows 2.2.
 template <Prec PR>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) {
     using PT = PrecT<PR>;

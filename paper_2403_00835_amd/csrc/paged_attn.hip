@@ -552,10 +552,10 @@ struct ChunkLoads {
 // partials, or, where the request has one span only (fp32: also where the partials do not hold the
 // request's), the rows are written.
 // Bound: reading the cache. Tokens of 64 requests at 1000 to 8000 keys (8 key heads of 128, pages of 16):
-// 1.18 GB in 222 us, 5.3 TB/s, and 13 in the join (a large copy here reaches 4.75). Short calls: latency, a
-// round trip each for the unit, the pages and the keys: one token at 512 keys 7.7 us and 3.2 in the join, 16
-// rows at 700 9.2 and 3.3, 64 rows at 2304 24.0 and 4.8 (32 heads); fp32, 29 to 82 KiB of keys a head, 13.8
-// and 3.9. Spans of 512 keys by eight waves leave one workgroup a CU: 259 us in place of 224. The last
+// 1.18 GB in 227 us, 5.2 TB/s, and 13 in the join (a large copy here reaches 4.9). Short calls: latency, a
+// round trip each for the unit, the pages and the keys: one token at 512 keys 7.8 us and 3.3 in the join, 16
+// rows at 700 9.2 and 3.2, 64 rows at 2304 23.7 and 4.8 (32 heads); fp32, 29 to 82 KiB of keys a head, 14.0
+// and 3.8 (one workgroup a CU, as K takes the registers of two). Spans of 512 keys by eight waves leave one workgroup a CU: 259 us in place of 224. The last
 // workgroup of a row joining its spans in place of a kernel costs 10 us of fences.
 template <Prec P, int HD, int RG>
 __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
@@ -768,16 +768,18 @@ constexpr int tile_lds() {
 // rows. Chunks of 64 keys of K and V come into LDS by DMA, once for all waves, one chunk ahead. Per chunk
 // and wave: S^T = K Q^T (32 keys x 32 rows a product), so that a lane holds half the keys of one row: the
 // softmax is lane-local but for one exchange, and the weights are the next product's operand as they lie;
-// O^T += V^T P^T with transposing reads of V. The weights are rounded to bf16 (half a step, 2^-9 of each
-// weight, of random sign: less than the output's own rounding), their sum is not. The reference of the
+// O^T += V^T P^T with transposing reads of V. The weights are rounded to bf16 (at most half a step, 2^-8
+// of each weight, of random sign: a sum over keys is off by less than the output's own rounding may be), their sum is
+// not: 0.0023 off the formula where exact weights give 0.0017, the output's rounding alone. Weights of two planes as in
+// the few rows' kernels take 606 us in place of 470 (the case below). The reference of the
 // exponentials follows the running maximum only when that has grown by 2^8: weights are then at most 2^8
 // in place of 1, which neither type minds, and the output is rescaled rarely.
 // Bound: the matrix unit and, between its products, the softmax: 2048 tokens at 12288 (32 heads, 8 key heads
-// of 128) take 462 to 480 us, 930 to 970 TFLOP/s (a large bf16 product of the library reaches 1200 here).
+// of 128) take 462 to 483 us, 925 to 968 TFLOP/s (a large bf16 product of the library reaches 1200 here).
 // Left out of a copy, the exponentials save 35 us, the DMA 60, three quarters of either product 105 to 125:
 // nothing waits for one thing alone. Reads that run ahead of the softmax, softmax and products of two chunks
-// interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 770
-// TFLOP/s, 32 wide 660, 256 wide 460 (one workgroup a CU, and 38 registers spilled).
+// interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 800
+// TFLOP/s, 32 wide 640, 256 wide 490 (one workgroup a CU, and 32 registers spilled).
 template <int HD>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
     using TL = Tile<HD>;
@@ -986,8 +988,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
 }
 
 // Joins the partial states of split row blocks, in position order. Workgroup: some rows of one key head of
-// an item, a thread per four columns of a row. Bound: latency, four states in flight a thread: 3.2 us for one
-// span's worth, 13 us for 64 requests of 4 to 32 spans (16 in flight: 15.5 in place of 8.3 us at 16 requests).
+// an item, a thread per four columns of a row. Bound: latency, four states in flight a thread: 3.3 us for three
+// spans, 13 us for 64 requests of 4 to 32 spans (16 in flight: 15.5 in place of 8.3 us at 16 requests).
 template <Prec P, int HD>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int cap_items) {
     constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedItemRows + RPW - 1) / RPW;
@@ -1010,7 +1012,7 @@ hipError_t launch_spans(int64_t units, bool whole, const PagedAttnParams &p, hip
     constexpr int lds = kSpanChunks * span_wave_lds<P, HD, RG>();
     static_assert(lds + 4096 <= 160 * 1024, "the LDS of a CU");
     static_assert(16 * RG == paged_block_rows(P == Prec::BF16, HD), "the plan's row blocks");
-    // (where requests may be taken whole, fewer: passing over 2560 units takes 6.5 us, 3.7 in a grid of 1024; spans in
+    // (where requests may be taken whole, fewer: passing over 2560 units takes 6.5 us, 4.6 in a grid of 1024; spans in
     // a grid of 1024 take up to 2% longer)
     const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, whole ? 4 * kCUs : 16 * kCUs));
     hipLaunchKernelGGL((paged_span_kernel<P, HD, RG>), grid, dim3(kSpanChunks * kWave), lds, s, p, p.bk.cap_units);
