@@ -461,7 +461,9 @@ class PagedCache:
         self._ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
         if self.stream != cur.cuda_stream:
             cur.synchronize()  # the memory's last user in the allocator's order
-            self._ws.record_stream(torch.cuda.ExternalStream(self.stream, device=self.device))
+            # (an ExternalStream of address 0 would be a new stream)
+            self._ws.record_stream(torch.cuda.ExternalStream(self.stream, device=self.device) if self.stream else
+                                   torch.cuda.default_stream(self.device))
         cfg.stream, cfg.workspace, cfg.workspace_bytes = self.stream, self._ws.data_ptr(), n.value
         h = _vp()
         st = self.L.cllm_paged_create(ctypes.byref(cfg), ctypes.byref(h))
@@ -576,7 +578,8 @@ class PagedCache:
             if lse.requires_grad:
                 self._no_backward("lse")
         self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
-                                           self._pool(v_pages, "v_pages"), 0.0 if scale is None else scale, *self._rows(out, self.n_heads, "out"),
+                                           self._pool(v_pages, "v_pages"), 0.0 if scale is None else scale,
+                                           *self._rows(out, self.n_heads, "out"),
                                            None if lse is None else lse.data_ptr()))
         if lse is None:
             _changed(out)

@@ -900,15 +900,20 @@ def test_two_caches_side_by_side(binding):
 
 
 def test_a_cache_made_for_a_stream_that_is_not_current(binding):
-    """stream= at creation: the calls are made with that stream current, and refused with any other."""
-    side, got = torch.cuda.Stream(), []
-    for stream in (None, side.cuda_stream):
-        c = make(binding, page=16, n_pages=30, max_seqs=2, max_ctx=200, max_rows=8, heads=4, kv=2, hd=64, rope_base=10000.0,
-                 stream=stream)
-        if stream is not None:
-            with pytest.raises(ValueError, match="stream"):
-                c.plan(ints([0]), ints([0]), ints([1]), rows=1)
-        with torch.cuda.stream(side) if stream else torch.cuda.stream(torch.cuda.current_stream()):
+    """stream= at creation: the calls are made with that stream current, and refused with any other. The memory of the
+    books is told of that stream and no other (the default one has the address 0)."""
+    side, default, got = torch.cuda.Stream(), torch.cuda.default_stream(), []
+    for now, stream in ((default, None), (default, side), (side, default)):
+        told, record = [], torch.Tensor.record_stream
+        with torch.cuda.stream(now), pytest.MonkeyPatch.context() as patch:
+            patch.setattr(torch.Tensor, "record_stream", lambda x, s: (told.append(s.cuda_stream), record(x, s)))
+            c = make(binding, page=16, n_pages=30, max_seqs=2, max_ctx=200, max_rows=8, heads=4, kv=2, hd=64, rope_base=10000.0,
+                     stream=None if stream is None else stream.cuda_stream)
+            assert told == ([] if stream is None else [stream.cuda_stream])
+            if stream is not None:
+                with pytest.raises(ValueError, match="stream"):
+                    c.plan(ints([0]), ints([0]), ints([1]), rows=1)
+        with torch.cuda.stream(stream or default):
             g = torch.Generator(device="cuda").manual_seed(4)
             pools = [torch.randn(c.pool_shape, generator=g, device="cuda").bfloat16() for _ in range(2)]
             x, out = torch.randn(8, 8, 64, generator=g, device="cuda").bfloat16(), torch.empty(8, 4, 64, device="cuda").bfloat16()
@@ -919,7 +924,7 @@ def test_a_cache_made_for_a_stream_that_is_not_current(binding):
             got.append(out.clone())
             torch.cuda.current_stream().synchronize()
         c.close()
-    assert torch.equal(*got)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
 
 
 def test_a_cache_that_ends_while_a_graph_is_captured(binding):
