@@ -483,17 +483,17 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
 
 /* Attention of the last plan's rows over the pages of one layer: out row r (of entry b, head h) =
  * softmax over the positions t <= row_pos[r] of slot seq_ids[b] of scale q[r][h] . k[t][h / group]
- * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim), others are
- * up to 2.35e38 in size. lse (or NULL): fp32 [rows][n_heads], the natural log of the sum of exponentials of
- * the scaled scores. out may be q with q's stride. Statistics, products and sums in fp32, the output rounded once. Few rows (at most 64 / group
- * new tokens: with group 1 every block length of the library's decoding, with group 4 blocks of up to 16)
- * and fp32: bf16 probabilities are two bf16 planes, and a row's bits depend on its queries, its position and
+ * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim), others are up to 2.35e38
+ * in size. lse (or NULL): fp32 [rows][n_heads], the natural log of the sum of exponentials of the scaled
+ * scores. out may be q with q's stride. Statistics, products and sums in fp32, the output rounded once. Few
+ * rows (at most 64 / group new tokens: with group 1 every block length of the library's decoding, with group
+ * 4 blocks of up to 16) and fp32: bf16 probabilities are two bf16 planes, and a row's bits depend on its queries, its position and
  * the keys and values up to it alone, not on the chunk, the other requests, the pages or the bounds: a block
  * of one token and a block of many give the same row. A longer block of grouped heads has its tokens' bits
  * when it is run in steps of 64 / group. Longer bf16 chunks (where group is above 64, all of them):
  * probabilities are rounded to bf16 for their product with the values, and how the keys are split into ranges
- * depends on the plan (rounding differences only; the same plan gives the same bits). What a page holds past a row's position (another request's remains, rejected tokens,
- * NaN) does not reach the row.
+ * depends on the plan (rounding differences only; the same plan gives the same bits). What a page holds past a
+ * row's position (another request's remains, rejected tokens, NaN) does not reach the row.
  * Errors: ERR_ARG, ERR_STATE (no plan yet), ERR_DEVICE. */
 cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
                             float scale, void *out, int64_t out_stride, float *lse);

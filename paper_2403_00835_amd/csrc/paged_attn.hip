@@ -555,8 +555,9 @@ struct ChunkLoads {
 // 1.18 GB in 227 us, 5.2 TB/s, and 13 in the join (a large copy here reaches 4.9). Short calls: latency, a
 // round trip each for the unit, the pages and the keys: one token at 512 keys 7.8 us and 3.3 in the join, 16
 // rows at 700 9.2 and 3.2, 64 rows at 2304 23.7 and 4.8 (32 heads); fp32, 29 to 82 KiB of keys a head, 14.0
-// and 3.8 (one workgroup a CU, as K takes the registers of two). Spans of 512 keys by eight waves leave one workgroup a CU: 259 us in place of 224. The last
-// workgroup of a row joining its spans in place of a kernel costs 10 us of fences.
+// and 3.8 (one workgroup a CU, as K takes the registers of two). Spans of 512 keys by eight waves leave one
+// workgroup a CU: 259 us in place of 224. The last workgroup of a row joining its spans in place of a kernel costs
+// 10 us of fences.
 template <Prec P, int HD, int RG>
 __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
                                                                                                   int cap_units) {
