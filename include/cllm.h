@@ -481,6 +481,40 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
 cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                               int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages);
 
+/* Another form of the rotation, for later appends to a cache created with rope_base > 0 (which starts as
+ * halves of the whole head, unscaled). The first dim elements of a head (0: all) are turned in pairs, HALVES:
+ * (j, j + dim / 2), NEIGHBOURS: (2j, 2j + 1), by t * theta_j; the others are left as they are. theta_j =
+ * base^(-2j / dim) (PLAIN); theta_j / factor (LINEAR); theta_j (g + (1 - g) / factor) with g = (orig_ctx theta_j /
+ * 2 pi - low) / (high - low) within [0, 1] (BY_PARTS: pairs of more than `high` turns over the original context
+ * keep their angle, those of fewer than `low` are stretched). freqs (host, dim / 2 doubles, or NULL) gives the
+ * theta_j themselves in place of base and scaling. Sines and cosines are formed in double, times magnitude (0
+ * means 1), and rounded once to fp32. The factors are made again on the cache's stream; a captured append keeps the
+ * layout and dim that it was captured with, so capture it again behind this call.
+ * Errors: ERR_ARG, ERR_STATE (rope_base 0), ERR_DEVICE. */
+#define CLLM_ROTARY_HALVES 0
+#define CLLM_ROTARY_NEIGHBOURS 1
+#define CLLM_ROTARY_PLAIN 0
+#define CLLM_ROTARY_LINEAR 1
+#define CLLM_ROTARY_BY_PARTS 2
+typedef struct cllm_paged_rotary_spec {
+    int32_t layout, dim, scaling;
+    float base, factor, orig_ctx, low, high, magnitude;
+    const double *freqs;
+} cllm_paged_rotary_spec;
+cllm_status cllm_paged_rotary(cllm_paged *c, const cllm_paged_rotary_spec *spec);
+/* The theta_j of a spec for heads of head_dim elements: dim / 2 doubles to the host array freqs. No device call.
+ * Errors: ERR_ARG. */
+cllm_status cllm_paged_rotary_freqs(const cllm_paged_rotary_spec *spec, int32_t head_dim, double *freqs);
+
+/* cllm_paged_append with an RMS norm of every query and key head before the rotation, in the same pass: x / sqrt(mean
+ * (x^2) + eps) * gain over the head's elements, in fp32 and rounded once behind the rotation. q_gain, k_gain: device
+ * fp32 [head_dim], one for all heads, or NULL: no norm (q_gain with q only). eps: finite, at least FLT_MIN. A head
+ * that holds an infinity or a NaN gets NaN where the formula does.
+ * Errors: those of cllm_paged_append. */
+cllm_status cllm_paged_append_norm(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                   int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages,
+                                   const float *q_gain, const float *k_gain, float eps);
+
 /* Attention of the last plan's rows over the pages of one layer: out row r (of entry b, head h) =
  * softmax over the positions t <= row_pos[r] of slot seq_ids[b] of scale q[r][h] . k[t][h / group]
  * (group = n_heads / n_kv_heads), times v[t]; scale 0 means 1 / sqrt(head_dim), others are up to 2.35e38

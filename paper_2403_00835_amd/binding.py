@@ -63,6 +63,11 @@ class cllm_paged_views(ctypes.Structure):
                 ("row_pos", _vp), ("max_pages", _i32)]
 
 
+class cllm_paged_rotary_spec(ctypes.Structure):
+    _fields_ = [("layout", _i32), ("dim", _i32), ("scaling", _i32), ("base", _f32), ("factor", _f32), ("orig_ctx", _f32),
+                ("low", _f32), ("high", _f32), ("magnitude", _f32), ("freqs", ctypes.POINTER(_dbl))]
+
+
 TRACE_STRIDE = 5 + 2 * 64  # CLLM_TRACE_STRIDE
 
 EXPORTS = ["cllm_model_create", "cllm_model_set_weights", "cllm_model_init_random", "cllm_model_load", "cllm_model_free", "cllm_prefill",
@@ -70,7 +75,7 @@ EXPORTS = ["cllm_model_create", "cllm_model_set_weights", "cllm_model_init_rando
            "cllm_jacobi_decode_batch", "cllm_reset", "cllm_debug_logits", "cllm_trace_enable", "cllm_trace_read",
            "cllm_trace_count", "cllm_collect_states", "cllm_loss_head", "cllm_loss_head_device", "cllm_hidden_rows", "cllm_hidden_rows_noalloc", "cllm_seq_state", "cllm_timing_enable", "cllm_timing_read",
            "cllm_paged_workspace_bytes", "cllm_paged_create", "cllm_paged_free", "cllm_paged_views_get", "cllm_paged_plan",
-           "cllm_paged_append", "cllm_paged_attn", "cllm_paged_status", "cllm_paged_last_error",
+           "cllm_paged_append", "cllm_paged_rotary", "cllm_paged_rotary_freqs", "cllm_paged_append_norm", "cllm_paged_attn", "cllm_paged_status", "cllm_paged_last_error",
            "cllm_streamed_weight_bytes", "cllm_workspace_bytes", "cllm_status_string", "cllm_last_error"]
 
 _lib = None
@@ -132,6 +137,9 @@ def lib():
         L.cllm_paged_views_get.argtypes = [_vp, P(cllm_paged_views)]
         L.cllm_paged_plan.argtypes = [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32]
         L.cllm_paged_append.argtypes = [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+        L.cllm_paged_rotary.argtypes = [_vp, P(cllm_paged_rotary_spec)]
+        L.cllm_paged_rotary_freqs.argtypes = [P(cllm_paged_rotary_spec), _i32, _vp]
+        L.cllm_paged_append_norm.argtypes = [*L.cllm_paged_append.argtypes, _vp, _vp, _f32]
         L.cllm_paged_attn.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]
         L.cllm_paged_status.argtypes = [_vp, P(_i32), P(_i32)]
         L.cllm_paged_last_error.argtypes = [_vp]
@@ -539,6 +547,16 @@ class PagedCache:
             self._no_backward(name)
         return x.data_ptr()
 
+    def _gain(self, x, name):
+        if x is None:
+            return None
+        if x.dtype != self._float32 or x.shape != (self.head_dim,) or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"{name}: a contiguous float32 tensor of {self.head_dim} on {self.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        if x.requires_grad:
+            self._no_backward(name)
+        return x.data_ptr()
+
     def plan(self, seq_ids, ctx_lens, new_lens, rows, max_new=0, max_len=0):
         """cllm_paged_plan: int32 tensors of one size; rows, max_new, max_len: the host's bounds."""
         self._on_stream()
@@ -548,18 +566,43 @@ class PagedCache:
         self.rows = rows
         _changed(self._ws)
 
-    def append(self, q, k, v, q_out, k_pages, v_pages):
+    def rotary(self, layout="half", dim=0, base=10000.0, scaling=None, factor=0.0, orig_ctx=0.0, low=0.0, high=0.0, magnitude=1.0,
+               freqs=None):
+        """cllm_paged_rotary: the form of the rotation in later appends. layout "half" or "interleaved"; dim: the
+        elements of a head that are turned (0: all); scaling None, "linear" (factor) or "parts" (factor, orig_ctx, low,
+        high); freqs: the angles a position themselves, dim / 2 numbers, in place of base and scaling."""
+        self._on_stream()
+        if layout not in ("half", "interleaved"):
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        if scaling not in (None, "linear", "parts"):
+            raise ValueError("scaling must be None, 'linear' or 'parts'")
+        if not _f32(magnitude).value:  # 0 is the library's default
+            raise ValueError(f"magnitude {magnitude} is 0 in float32")
+        if freqs is not None:
+            if scaling is not None or len(freqs) != (dim or self.head_dim) // 2:
+                raise ValueError(f"freqs: {(dim or self.head_dim) // 2} numbers, and no scaling")
+            freqs = (_dbl * max(len(freqs), 1))(*[float(x) for x in freqs])
+        spec = cllm_paged_rotary_spec(("half", "interleaved").index(layout), dim, (None, "linear", "parts").index(scaling), base,
+                                      factor, orig_ctx, low, high, magnitude, freqs)
+        self._check(self.L.cllm_paged_rotary(self.h, ctypes.byref(spec)))
+        _changed(self._ws)
+
+    def append(self, q, k, v, q_out, k_pages, v_pages, q_gain=None, k_gain=None, eps=1e-6):
         """cllm_paged_append: rows q [.., n_heads, head_dim] (or None, with q_out), k and v
-        [.., n_kv_heads, head_dim], of any row stride, into pools of pool_shape."""
+        [.., n_kv_heads, head_dim], of any row stride, into pools of pool_shape. With q_gain or k_gain (contiguous
+        float32 [head_dim]) cllm_paged_append_norm: those heads are normalised before they are turned."""
         self._on_stream()
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
         none = (None, 0)
         qa = none if q is None else self._rows(q, self.n_heads, "q")
         qo = none if q_out is None else self._rows(q_out, self.n_heads, "q_out")
-        self._check(self.L.cllm_paged_append(self.h, *qa, *self._rows(k, self.n_kv_heads, "k"),
-                                             *self._rows(v, self.n_kv_heads, "v"), *qo, self._pool(k_pages, "k_pages"),
-                                             self._pool(v_pages, "v_pages")))
+        args = (self.h, *qa, *self._rows(k, self.n_kv_heads, "k"), *self._rows(v, self.n_kv_heads, "v"), *qo,
+                self._pool(k_pages, "k_pages"), self._pool(v_pages, "v_pages"))
+        if q_gain is None and k_gain is None:
+            self._check(self.L.cllm_paged_append(*args))
+        else:
+            self._check(self.L.cllm_paged_append_norm(*args, self._gain(q_gain, "q_gain"), self._gain(k_gain, "k_gain"), eps))
         if q_out is None:
             _changed(k_pages, v_pages)
         else:

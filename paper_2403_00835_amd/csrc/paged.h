@@ -97,8 +97,18 @@ struct PagedAppendParams {
     const void *q, *k, *v;       // rows of q_stride (k_stride, v_stride) elements
     void *q_out, *k_pages, *v_pages;
     int64_t q_stride, k_stride, v_stride, q_out_stride;
-    const float *rcos, *rsin;    // [max_ctx][hd / 2], or null: no rotation
+    const float *rcos, *rsin;    // [max_ctx][rot], or null: no rotation
     int n_heads, n_kv, hd;
+    int rot;                     // pairs of a head that are turned (0: none)
+    bool inter;                  // pairs (2 j, 2 j + 1) in place of (j, j + rot)
+    const float *q_gain, *k_gain;  // [hd], or null: no norm
+    float eps;
+};
+
+// Angles of a position's pairs, by value to the kernel that makes the rotary factors.
+constexpr int kMaxRot = 128;
+struct PagedFreqs {
+    double f[kMaxRot];
 };
 
 struct PagedAttnParams {
@@ -128,7 +138,10 @@ __device__ __forceinline__ int bounded_rows(const PagedBooks &bk, int rows, int 
 hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int hd,
                              double rope_base, hipStream_t s);
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s);
+hipError_t launch_paged_rotary(float *rcos, float *rsin, int max_ctx, int rot, double magnitude, const PagedFreqs &f, hipStream_t s);
 hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_t s);
+// The same with norms of the heads, and with any part of the head turned in either layout.
+hipError_t launch_paged_append_forms(bool bf16, const PagedAppendParams &p, hipStream_t s);
 // Upper bounds of the plan's units and tiles; join: some may be split.
 hipError_t launch_paged_attn(bool bf16, int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s);
 

@@ -355,6 +355,231 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
     }
 }
 
+// Factors of one pair j at every position: cos and sin of t * f[j] in double, times the magnitude, rounded once.
+__global__ __launch_bounds__(256) void paged_rotary_kernel(float *rcos, float *rsin, int max_ctx, int rot, double magnitude,
+                                                           PagedFreqs f) {
+    const int t = (int)blockIdx.x * 256 + threadIdx.x, j = blockIdx.y;
+    if (t >= max_ctx) return;
+    const double ang = (double)t * f.f[j];
+    rcos[(size_t)t * rot + j] = (float)(cos(ang) * magnitude);
+    rsin[(size_t)t * rot + j] = (float)(sin(ang) * magnitude);
+}
+
+namespace {
+
+// Sum over the nv (2, 4, 8 or 16) neighbouring lanes of a head, in every one of them.
+__device__ __forceinline__ float head_sum(float x, int nv) {
+    auto add = [](float a, int moved) { return a + __int_as_float(moved); };
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, true));                // lane ^ 1
+    if (nv >= 4) x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, true));   // lane ^ 2
+    if (nv >= 8) x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, 0xf, 0xf, true));  // 8 lanes mirrored
+    if (nv >= 16) x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, 0xf, 0xf, true)); // 16 lanes mirrored
+    return x;
+}
+
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));  // a vector of floats at any float's address
+
+template <int N>
+__device__ __forceinline__ void load_floats(float (&x)[N], const float *src) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4_a4 *>(src + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+    }
+}
+
+// How a head's elements lie in its threads: thread l takes the pairs l VEC .. (l + 1) VEC - 1. Pair j of the turned
+// ones is (j, j + rot) or (2 j, 2 j + 1); behind them pair j is the elements (2 j, 2 j + 1), left as they are.
+enum Pairs {
+    HALVES,       // rot a multiple of VEC: two vectors rot apart, or next to each other
+    NEIGHBOURS,   // interleaved: two vectors next to each other
+    SCATTERED,    // halves of other widths: element by element
+};
+
+}  // namespace
+
+// paged_append_kernel with a norm of each query and key head before the rotation, and every form of the rotation:
+// y = x / sqrt(mean(x^2) + eps) * gain in fp32, then the turned pairs, rounded once. A thread takes U heads of one
+// row, whose rotary factors and gains it loads once.
+template <Prec PR, Pairs F, int U>
+__global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendParams p, int per_row, uint32_t per_row_inv, int rpb) {
+    using PT = PrecT<PR>;
+    using T = typename PT::T;
+    constexpr int VEC = PT::VEC;
+    const int R = bounded_rows(p.bk, p.rows, p.max_new, p.max_len);
+    const int nv = p.hd / 2 / VEC, nv_shift = 31 - __clz(nv);
+    const int q_segs = p.q ? (p.n_heads + U - 1) / U : 0, kv_segs = (p.n_kv + U - 1) / U;
+    for (int row0 = blockIdx.x * rpb; row0 < R; row0 += gridDim.x * rpb) {
+        const int items = min(rpb, R - row0) * per_row;
+        for (int i = threadIdx.x; i < items; i += 256) {
+            const int dr = (int)__umulhi((uint32_t)i, per_row_inv), w = i - dr * per_row, r = row0 + dr;
+            const int l = w & (nv - 1), pair = l * VEC;
+            int seg = w >> nv_shift;
+            const bool isq = seg < q_segs, isk = !isq && seg < q_segs + kv_segs;
+            seg -= isq ? 0 : isk ? q_segs : q_segs + kv_segs;
+            const int heads = isq ? p.n_heads : p.n_kv, h0 = seg * U;
+            const T *src = isq ? (const T *)p.q + (size_t)r * p.q_stride : isk ? (const T *)p.k + (size_t)r * p.k_stride
+                                                                             : (const T *)p.v + (size_t)r * p.v_stride;
+            T *dst;
+            size_t head_step = p.hd;
+            if (isq) {
+                dst = (T *)p.q_out + (size_t)r * p.q_out_stride;
+            } else {
+                const int slot = p.bk.row_slot[r], page = slot >> p.bk.page_shift, off = slot & ((1 << p.bk.page_shift) - 1);
+                head_step = (size_t)p.hd << p.bk.page_shift;
+                dst = (T *)(isk ? p.k_pages : p.v_pages) + (size_t)page * p.n_kv * head_step + (size_t)off * p.hd;
+            }
+            const bool whole = F == HALVES && pair < p.rot;  // of its vectors, the first members and the second ones
+            const int o0 = whole ? pair : 2 * pair, o1 = whole ? pair + p.rot : 2 * pair + VEC;
+            auto at = [&](int i) {  // SCATTERED: element of member i % 2 of pair i / 2
+                const int j = pair + i / 2;
+                return j < p.rot ? j + (i & 1) * p.rot : 2 * j + (i & 1);
+            };
+            if (!isq && !isk) {  // values: as they are
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (h0 + u >= heads) break;
+                    const u32x4 *s = reinterpret_cast<const u32x4 *>(src + (h0 + u) * p.hd + 2 * pair);
+                    u32x4 *d = reinterpret_cast<u32x4 *>(dst + (h0 + u) * head_step + 2 * pair);
+                    const u32x4 a = s[0], b = s[1];
+                    d[0] = a;
+                    d[1] = b;
+                }
+                continue;
+            }
+            alignas(16) T x[U][2 * VEC];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const T *s = src + min(h0 + u, heads - 1) * p.hd;
+                if constexpr (F == SCATTERED) {
+#pragma unroll
+                    for (int i = 0; i < 2 * VEC; ++i) x[u][i] = s[at(i)];
+                } else {
+                    *reinterpret_cast<u32x4 *>(x[u]) = *reinterpret_cast<const u32x4 *>(s + o0);
+                    *reinterpret_cast<u32x4 *>(x[u] + VEC) = *reinterpret_cast<const u32x4 *>(s + o1);
+                }
+            }
+            const float *gain = isq ? p.q_gain : p.k_gain;
+            float g[2 * VEC], c[VEC], s[VEC];
+            if (gain) {
+                if constexpr (F == SCATTERED) {
+#pragma unroll
+                    for (int i = 0; i < 2 * VEC; ++i) g[i] = gain[at(i)];
+                } else {
+                    float a[VEC], b[VEC];
+                    load_floats(a, gain + o0);
+                    load_floats(b, gain + o1);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[i] = a[i], g[VEC + i] = b[i];
+                }
+            }
+            if (pair < p.rot) {
+                const size_t t = (size_t)p.bk.row_pos[r] * p.rot + pair;
+                if (pair + VEC <= p.rot) {
+                    load_floats(c, p.rcos + t);
+                    load_floats(s, p.rsin + t);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        const bool turned = pair + i < p.rot;
+                        c[i] = turned ? p.rcos[t + (turned ? i : 0)] : 1.f;
+                        s[i] = turned ? p.rsin[t + (turned ? i : 0)] : 0.f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float y[2 * VEC];
+#pragma unroll
+                for (int i = 0; i < 2 * VEC; ++i) y[i] = from_elem<PR>(x[u][i]);
+                if (gain) {
+                    auto squares = [&]() {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 2 * VEC; ++i) ss += y[i] * y[i];
+                        return head_sum(ss, nv) / (float)p.hd;
+                    };
+                    float ms = squares(), eps = p.eps;
+                    if (!(ms <= 3.4e38f)) {  // squares past fp32: of 2^-80 of the values, beside which eps is nothing
+#pragma unroll
+                        for (int i = 0; i < 2 * VEC; ++i) y[i] *= 0x1p-80f;
+                        ms = squares();
+                        eps = 0.f;
+                    }
+                    const float f = 1.0f / sqrtf(ms + eps);
+#pragma unroll
+                    for (int i = 0; i < 2 * VEC; ++i) y[i] = y[i] * f * g[i];
+                }
+                if (pair < p.rot) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        constexpr int D = F == HALVES ? VEC : 1, S = F == HALVES ? 1 : 2;
+                        if (F != HALVES && pair + i >= p.rot) continue;  // (0 * inf)
+                        const float a = y[S * i], b = y[S * i + D];
+                        y[S * i] = a * c[i] - b * s[i];
+                        y[S * i + D] = b * c[i] + a * s[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2 * VEC; ++i)
+                    x[u][i] = to_elem<PR>(y[i]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (h0 + u >= heads) break;
+                T *d = dst + (h0 + u) * head_step;
+                if constexpr (F == SCATTERED) {
+#pragma unroll
+                    for (int i = 0; i < 2 * VEC; ++i) d[at(i)] = x[u][i];
+                } else {
+                    *reinterpret_cast<u32x4 *>(d + o0) = *reinterpret_cast<const u32x4 *>(x[u]);
+                    *reinterpret_cast<u32x4 *>(d + o1) = *reinterpret_cast<const u32x4 *>(x[u] + VEC);
+                }
+            }
+        }
+    }
+}
+
+hipError_t launch_paged_rotary(float *rcos, float *rsin, int max_ctx, int rot, double magnitude, const PagedFreqs &f, hipStream_t s) {
+    if (!rcos || !rsin || rot < 1 || rot > kMaxRot || max_ctx < 1) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(paged_rotary_kernel, dim3((unsigned)((max_ctx + 255) / 256), (unsigned)rot), dim3(256), 0, s, rcos, rsin,
+                       max_ctx, rot, magnitude, f);
+    return hipGetLastError();
+}
+
+namespace {
+
+template <Prec PR, Pairs F, int U>
+hipError_t launch_forms(const PagedAppendParams &p, hipStream_t s) {
+    const int nv = p.hd / 2 / PrecT<PR>::VEC;
+    const int per_row = ((p.q ? (p.n_heads + U - 1) / U : 0) + 2 * ((p.n_kv + U - 1) / U)) * nv;
+    const int rpb = std::max(1, 256 / per_row);
+    // (item * per_row is below 2^32: at most 512 items of several rows, or one row's 3 * 1024 * 16)
+    const uint32_t inv = (uint32_t)(((1ull << 32) + per_row - 1) / per_row);
+    const dim3 grid((unsigned)std::min<int64_t>((p.rows + rpb - 1) / rpb, 16 * kCUs));
+    hipLaunchKernelGGL((paged_append_forms_kernel<PR, F, U>), grid, dim3(256), 0, s, p, per_row, inv, rpb);
+    return hipGetLastError();
+}
+
+template <Prec PR>
+hipError_t launch_forms(const PagedAppendParams &p, hipStream_t s) {
+    if (p.inter || p.rot == 0) return launch_forms<PR, NEIGHBOURS, 1>(p, s);
+    if (p.rot % PrecT<PR>::VEC == 0) return launch_forms<PR, HALVES, 1>(p, s);
+    return launch_forms<PR, SCATTERED, 1>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_append_forms(bool bf16, const PagedAppendParams &p, hipStream_t s) {
+    const int vec = bf16 ? 8 : 4, nv = p.hd / 2 / vec;
+    if (p.hd % (2 * vec) != 0 || nv < 2 || nv > 16 || (nv & (nv - 1)) != 0 || p.rows < 0 || p.rot < 0 || 2 * p.rot > p.hd ||
+        (p.rot > 0 && !p.rcos))
+        return hipErrorInvalidValue;
+    if (p.rows == 0) return hipSuccess;
+    return bf16 ? launch_forms<Prec::BF16>(p, s) : launch_forms<Prec::F32>(p, s);
+}
+
 hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int hd, double rope_base,
                              hipStream_t s) {
     const int64_t n_rot = rcos ? (int64_t)max_ctx * (hd / 2) : 0;

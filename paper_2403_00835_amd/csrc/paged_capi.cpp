@@ -22,6 +22,8 @@ struct cllm_paged {
     int elem = 2, group = 1;
     PagedBooks bk{};
     float *rcos = nullptr, *rsin = nullptr;  // null without rotation
+    int rot = 0;                             // pairs of a head that are turned
+    bool inter = false;                      // neighbours in place of halves
     float *part_o = nullptr, *part_m = nullptr, *part_l = nullptr;
     bool tiled = false;  // long chunks take tiles
     int block_rows = 32, cap_part = 0, cap_tile_part = 0;
@@ -249,6 +251,7 @@ cllm_status cllm_paged_create(const cllm_paged_config *cfg, cllm_paged **out) {
         *b.p = base;
         base += round_up(b.bytes);
     }
+    c->rot = c->rcos ? cfg->head_dim / 2 : 0;
     if (launch_paged_init(c->bk, c->rcos, c->rsin, cfg->max_ctx, cfg->head_dim, (double)cfg->rope_base, c->stream) != hipSuccess ||
         hipStreamSynchronize(c->stream) != hipSuccess)
         return bail(CLLM_ERR_DEVICE);
@@ -318,15 +321,70 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
     return CLLM_OK;
 }
 
-cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
-                              int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages) {
+cllm_status cllm_paged_rotary_freqs(const cllm_paged_rotary_spec *spec, int32_t head_dim, double *freqs) {
+    if (!spec || !freqs || head_dim < 2 || head_dim > 2 * kMaxRot || head_dim % 2 != 0) return CLLM_ERR_ARG;
+    const int dim = spec->dim == 0 ? head_dim : spec->dim;
+    if (dim < 2 || dim > head_dim || dim % 2 != 0) return CLLM_ERR_ARG;
+    if (spec->layout != CLLM_ROTARY_HALVES && spec->layout != CLLM_ROTARY_NEIGHBOURS) return CLLM_ERR_ARG;
+    if (!std::isfinite(spec->magnitude)) return CLLM_ERR_ARG;
+    auto positive = [](float x) { return x > 0.0f && std::isfinite(x); };
+    if (!spec->freqs) {
+        if (spec->scaling < CLLM_ROTARY_PLAIN || spec->scaling > CLLM_ROTARY_BY_PARTS || !positive(spec->base)) return CLLM_ERR_ARG;
+        if (spec->scaling != CLLM_ROTARY_PLAIN && !positive(spec->factor)) return CLLM_ERR_ARG;
+        if (spec->scaling == CLLM_ROTARY_BY_PARTS &&
+            !(positive(spec->orig_ctx) && std::isfinite(spec->low) && std::isfinite(spec->high) && spec->low < spec->high))
+            return CLLM_ERR_ARG;
+    }
+    double w[kMaxRot];
+    for (int j = 0; j < dim / 2; ++j) {
+        w[j] = spec->freqs ? spec->freqs[j] : std::pow((double)spec->base, -2.0 * j / (double)dim);
+        if (!spec->freqs && spec->scaling == CLLM_ROTARY_LINEAR) w[j] /= (double)spec->factor;
+        if (!spec->freqs && spec->scaling == CLLM_ROTARY_BY_PARTS) {
+            const double turns = (double)spec->orig_ctx * w[j] / 6.283185307179586, low = spec->low, high = spec->high;
+            const double keep = std::min(std::max((turns - low) / (high - low), 0.0), 1.0);
+            w[j] *= keep + (1.0 - keep) / (double)spec->factor;
+        }
+        if (!(std::fabs(w[j]) <= 1e300)) return CLLM_ERR_ARG;  // (and times a position it is finite)
+    }
+    std::copy(w, w + dim / 2, freqs);
+    return CLLM_OK;
+}
+
+cllm_status cllm_paged_rotary(cllm_paged *c, const cllm_paged_rotary_spec *spec) {
     if (!c) return CLLM_ERR_ARG;
+    cllm_status s;
+    if ((s = check(c))) return s;
+    const cllm_paged_config &f = c->cfg;
+    if (!c->rcos) return fail(c, CLLM_ERR_STATE, "the cache was created without rotation (rope_base 0)");
+    PagedFreqs fr{};
+    if (cllm_paged_rotary_freqs(spec, f.head_dim, fr.f) != CLLM_OK)
+        return fail(c, CLLM_ERR_ARG, "rotary spec: dim even and up to head_dim, a known layout and scaling, base, factor and "
+                                     "orig_ctx positive, low below high, all finite");
+    const int rot = (spec->dim == 0 ? f.head_dim : spec->dim) / 2;
+    DeviceGuard dev(f.device);
+    if (!dev.ok) return fail(c, CLLM_ERR_DEVICE, "the cache's device cannot be made current");
+    HIPCHK(c, launch_paged_rotary(c->rcos, c->rsin, f.max_ctx, rot, spec->magnitude == 0.0f ? 1.0 : (double)spec->magnitude, fr,
+                                  c->stream));
+    c->rot = rot;
+    c->inter = spec->layout == CLLM_ROTARY_NEIGHBOURS;
+    return CLLM_OK;
+}
+
+namespace {
+
+cllm_status append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                   void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages, const float *q_gain, const float *k_gain,
+                   float eps) {
     cllm_status s;
     if ((s = check(c))) return s;
     if (!c->planned) return fail(c, CLLM_ERR_STATE, "append before a plan");
     if (c->rows == 0) return CLLM_OK;
     const cllm_paged_config &f = c->cfg;
     if (!q != !q_out) return fail(c, CLLM_ERR_ARG, "q and q_out go together");
+    if (q_gain && !q) return fail(c, CLLM_ERR_ARG, "q_gain without q");
+    // (below fp32's normal range the squares of small values, which underflow, would count beside it)
+    if ((q_gain || k_gain) && !(eps >= FLT_MIN && std::isfinite(eps)))
+        return fail(c, CLLM_ERR_ARG, "eps %g: finite, at least 1.18e-38", (double)eps);
     DeviceGuard dev(f.device);
     if (!dev.ok) return fail(c, CLLM_ERR_DEVICE, "the cache's device cannot be made current");
     if (q && ((s = check_rows(c, "q", q, q_stride, f.n_heads)) || (s = check_rows(c, "q_out", q_out, q_out_stride, f.n_heads))))
@@ -335,6 +393,9 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
     if ((s = check_rows(c, "k", k, k_stride, f.n_kv_heads)) || (s = check_rows(c, "v", v, v_stride, f.n_kv_heads)) ||
         (s = check_pool(c, "k_pages", k_pages)) || (s = check_pool(c, "v_pages", v_pages)))
         return s;
+    for (const float *g : {q_gain, k_gain})
+        if (g && (reinterpret_cast<uintptr_t>(g) % 4 != 0 || !accessible(c, g)))
+            return fail(c, CLLM_ERR_ARG, "gains: an array is not device memory of the cache's GPU");
     PagedAppendParams p{};
     p.bk = c->bk;
     p.rows = c->rows;
@@ -355,8 +416,32 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
     p.n_heads = f.n_heads;
     p.n_kv = f.n_kv_heads;
     p.hd = f.head_dim;
-    HIPCHK(c, launch_paged_append(c->bf16, p, c->stream));
+    p.rot = c->rot;
+    p.inter = c->inter;
+    p.q_gain = q_gain;
+    p.k_gain = k_gain;
+    p.eps = eps;
+    const bool whole = !c->rcos || (!c->inter && 2 * c->rot == f.head_dim);
+    if (whole && !q_gain && !k_gain)
+        HIPCHK(c, launch_paged_append(c->bf16, p, c->stream));
+    else
+        HIPCHK(c, launch_paged_append_forms(c->bf16, p, c->stream));
     return CLLM_OK;
+}
+
+}  // namespace
+
+cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                              int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages) {
+    if (!c) return CLLM_ERR_ARG;
+    return append(c, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, k_pages, v_pages, nullptr, nullptr, 0.0f);
+}
+
+cllm_status cllm_paged_append_norm(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                   int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages,
+                                   const float *q_gain, const float *k_gain, float eps) {
+    if (!c) return CLLM_ERR_ARG;
+    return append(c, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, k_pages, v_pages, q_gain, k_gain, eps);
 }
 
 cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
