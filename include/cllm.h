@@ -532,6 +532,16 @@ cllm_status cllm_paged_append_norm(cllm_paged *c, const void *q, int64_t q_strid
 cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
                             float scale, void *out, int64_t out_stride, float *lse);
 
+/* cllm_paged_attn behind a window: the row at position p sees the positions t <= p with t > p - window (its own is one
+ * of them) or t < sinks. window >= 1, sinks >= 0; a window of max_len (of the plan) or more is cllm_paged_attn's call.
+ * Everything else as there: a row's bits do not depend on the chunk, the other requests, the pages or the bounds where
+ * they do not there, and with a window that holds its whole past they are those without one. Keys and values of the
+ * window's spans only are read (a span is 256 positions; of longer bf16 chunks, a run of 64), and what pages hold at
+ * positions that a row does not see (NaN, infinities) does not reach it.
+ * Errors: those of cllm_paged_attn. */
+cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                                   float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse);
+
 /* Waits for the stream and says how the last plan went: its rows and the free pages (either may be
  * NULL). Errors: ERR_ARG or ERR_CAPACITY (the plan was refused), ERR_STATE (append or attention of a
  * replayed graph ran behind a plan with other bounds than its own and did nothing; or the stream is

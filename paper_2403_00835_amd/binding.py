@@ -75,7 +75,7 @@ EXPORTS = ["cllm_model_create", "cllm_model_set_weights", "cllm_model_init_rando
            "cllm_jacobi_decode_batch", "cllm_reset", "cllm_debug_logits", "cllm_trace_enable", "cllm_trace_read",
            "cllm_trace_count", "cllm_collect_states", "cllm_loss_head", "cllm_loss_head_device", "cllm_hidden_rows", "cllm_hidden_rows_noalloc", "cllm_seq_state", "cllm_timing_enable", "cllm_timing_read",
            "cllm_paged_workspace_bytes", "cllm_paged_create", "cllm_paged_free", "cllm_paged_views_get", "cllm_paged_plan",
-           "cllm_paged_append", "cllm_paged_rotary", "cllm_paged_rotary_freqs", "cllm_paged_append_norm", "cllm_paged_attn", "cllm_paged_status", "cllm_paged_last_error",
+           "cllm_paged_append", "cllm_paged_rotary", "cllm_paged_rotary_freqs", "cllm_paged_append_norm", "cllm_paged_attn", "cllm_paged_attn_window", "cllm_paged_status", "cllm_paged_last_error",
            "cllm_streamed_weight_bytes", "cllm_workspace_bytes", "cllm_status_string", "cllm_last_error"]
 
 _lib = None
@@ -141,6 +141,7 @@ def lib():
         L.cllm_paged_rotary_freqs.argtypes = [P(cllm_paged_rotary_spec), _i32, _vp]
         L.cllm_paged_append_norm.argtypes = [*L.cllm_paged_append.argtypes, _vp, _vp, _f32]
         L.cllm_paged_attn.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]
+        L.cllm_paged_attn_window.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _i32, _i32, _vp, _i64, _vp]
         L.cllm_paged_status.argtypes = [_vp, P(_i32), P(_i32)]
         L.cllm_paged_last_error.argtypes = [_vp]
         L.cllm_paged_last_error.restype = ctypes.c_char_p
@@ -608,22 +609,31 @@ class PagedCache:
         else:
             _changed(q_out, k_pages, v_pages)
 
-    def attn(self, q, k_pages, v_pages, out, scale=None, lse=None):
+    def attn(self, q, k_pages, v_pages, out, scale=None, lse=None, window=None, sinks=0):
         """cllm_paged_attn: rows q [.., n_heads, head_dim] over the pools into out (of q's shape); lse: a
-        contiguous float32 [.., n_heads]. scale None: 1 / sqrt(head_dim)."""
+        contiguous float32 [.., n_heads]. scale None: 1 / sqrt(head_dim). With a window cllm_paged_attn_window: each row
+        over its last `window` tokens and the first `sinks`."""
         self._on_stream()
         if scale is not None and not _f32(scale).value:
             raise ValueError(f"scale {scale} is 0 in float32")
+        if window is None:
+            if sinks != 0:
+                raise ValueError("sinks go with a window")
+        elif not 0 < window < 1 << 31 or not 0 <= sinks < 1 << 31:
+            raise ValueError(f"window {window} (at least 1), sinks {sinks} (at least 0)")
         if lse is not None:
             if lse.dtype != self._float32 or lse.dim() != 2 or lse.shape[1] != self.n_heads or lse.shape[0] < self.rows or \
                     not lse.is_contiguous() or lse.device != self.device:
                 raise ValueError(f"lse: a contiguous float32 tensor of at least {self.rows} x {self.n_heads} on {self.device}")
             if lse.requires_grad:
                 self._no_backward("lse")
-        self._check(self.L.cllm_paged_attn(self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"),
-                                           self._pool(v_pages, "v_pages"), 0.0 if scale is None else scale,
-                                           *self._rows(out, self.n_heads, "out"),
-                                           None if lse is None else lse.data_ptr()))
+        args = (self.h, *self._rows(q, self.n_heads, "q"), self._pool(k_pages, "k_pages"), self._pool(v_pages, "v_pages"),
+                0.0 if scale is None else scale)
+        end = (*self._rows(out, self.n_heads, "out"), None if lse is None else lse.data_ptr())
+        if window is None:
+            self._check(self.L.cllm_paged_attn(*args, *end))
+        else:
+            self._check(self.L.cllm_paged_attn_window(*args, window, sinks, *end))
         if lse is None:
             _changed(out)
         else:

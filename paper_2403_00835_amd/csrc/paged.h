@@ -58,6 +58,15 @@ struct alignas(16) PagedUnit {
                            // and keys; tiles: chunks [k0, k1)
     int part;              // partial row of the first row (row blocks: in span k0), or -1: none, the output is written
 };
+// A request of the plan. Attention with a window takes its blocks and spans from here: which spans a block sees is the
+// call's, not the plan's.
+struct alignas(16) PagedEntry {
+    int slot, ctx, m, r0;
+    int part;    // partial row of the first row in the first span that its block sees, or -1
+    int kind;    // PE_*
+    int pad[2];
+};
+enum PagedEntryKind { PE_BLOCKS = 0, PE_WHOLE = 1, PE_TILED = 2 };
 struct alignas(16) PagedItem {
     int ctx, m, r0, row;
     int part;    // partial row of the first row in the first span or range
@@ -77,6 +86,7 @@ struct PagedBooks {
     int32_t *row_pos;    // [max_rows]
     PagedUnit *units, *tiles;
     PagedItem *items;
+    PagedEntry *entries;  // [max_seqs]
     int cap_units, cap_tiles, cap_items;  // entries of the three
     int max_seqs, max_pages, n_pages, page_shift;
 };
@@ -122,6 +132,8 @@ struct PagedAttnParams {
     int n_heads, n_kv, hd, group;
     uint32_t group_inv;           // 2^24 / group, rounded up
     float scale_log2;
+    int window, sinks;            // of the calls with a window: a row sees its last `window` tokens and the first `sinks`
+    int spans, blocks;            // the most spans that a row block of such a call sees, the most row blocks of a request
 };
 
 // Rows of the last plan, or none when it was made for other bounds than the call's (a replayed graph
@@ -144,5 +156,9 @@ hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_
 hipError_t launch_paged_append_forms(bool bf16, const PagedAppendParams &p, hipStream_t s);
 // Upper bounds of the plan's units and tiles; join: some may be split.
 hipError_t launch_paged_attn(bool bf16, int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s);
+
+// The same behind a window of p.window tokens. n: requests; most: rows of a request, at most.
+hipError_t launch_paged_attn_window(bool bf16, int n, int64_t most, bool whole, int64_t tiles, bool join, const PagedAttnParams &p,
+                                    hipStream_t s);
 
 }  // namespace cllm

@@ -255,6 +255,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
     if (b < n) {
         bk.seq_pages[seq] = need;
         bk.row_start[b] = v[0];
+        bk.entries[b] = PagedEntry{seq, ctx, m, v[0], dparts ? place : -1, whole ? PE_WHOLE : tiled ? PE_TILED : PE_BLOCKS, {0, 0}};
     }
     if (b == 0) bk.row_start[n] = R;
     if (U > 0)

@@ -97,16 +97,47 @@ __device__ __forceinline__ void merge_weights(float &M, float Ms, float &w, floa
 }
 __device__ __forceinline__ float merge_value(float x, float xs, float w, float ws) { return __builtin_fmaf(xs, ws, x * w); }
 
-// Scores to probabilities: keys past qpos (relative to the chunk's first key) are out. mx: the row's
+// What a call's rows see: every position up to their own, or of those the last `window` and the first `sinks`.
+template <bool WIN>
+struct Sight {
+    int window, sinks;
+    __device__ explicit Sight(const PagedAttnParams &p) : window(p.window), sinks(p.sinks) {}
+    // The row at pos sees the key; it sees some key of [k, k + n), k <= pos.
+    __device__ bool key(int pos, int k) const { return k <= pos && (!WIN || k > pos - window || k < sinks); }
+    __device__ bool some(int pos, int k, int n) const { return !WIN || k + n - 1 > pos - window || k < sinks; }
+    // Some row of the positions up to `last` does not see some key of [k, k + n) that is behind it.
+    __device__ bool cuts(int last, int k, int n) const { return WIN && max(k, sinks) <= min(k + n - 1, last - window); }
+};
+
+// The pieces of N keys that rows at positions first .. last see, in order: those of the sinks, then those from the first
+// row's window on.
+template <bool WIN, int N>
+struct Visible {
+    int sink_end, from, count;
+    __device__ Visible(const Sight<WIN> &see, int first, int last) : sink_end(0), from(0), count(last / N + 1) {
+        if constexpr (WIN) {
+            sink_end = (min(see.sinks, last + 1) + N - 1) / N;
+            from = max(max(first - see.window + 1, 0) / N, sink_end);
+            count = sink_end + (last / N + 1 - from);
+        }
+    }
+    __device__ int piece(int j) const { return WIN && j >= sink_end ? j - sink_end + from : j; }
+};
+
+// Scores to probabilities: keys past qpos (relative to the chunk's first key, key0) are out. mx: the row's
 // maximum (-inf: it sees no key), l: its sum.
-__device__ __forceinline__ void chunk_softmax(f32x4 (&st)[4], int qpos, float scale_log2, int lane, float &mx, float &l) {
+template <bool WIN>
+__device__ __forceinline__ void chunk_softmax(f32x4 (&st)[4], int qpos, const Sight<WIN> &see, int key0, float scale_log2, int lane,
+                                              float &mx, float &l) {
     const int g = lane >> 4;
     mx = -INFINITY;
+    const int under = qpos - see.window, sinks = see.sinks - key0;  // keys above `under` or below `sinks`
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const float sc = 16 * kt + 4 * g + v <= qpos ? st[kt][v] * scale_log2 : -INFINITY;
+            const int k = 16 * kt + 4 * g + v;
+            const float sc = k <= qpos && (!WIN || k > under || k < sinks) ? st[kt][v] * scale_log2 : -INFINITY;
             st[kt][v] = sc;
             mx = fmaxf(mx, sc);
         }
@@ -240,16 +271,79 @@ __device__ __forceinline__ bool next_unit(const PagedAttnParams &p, int i, int c
     return R > 0 && i < n;
 }
 
+// A request of the plan, likewise.
+__device__ __forceinline__ bool next_entry(const PagedAttnParams &p, int i, PagedEntry &e, int &count) {
+    const int32_t *st = p.bk.status;
+    const int R = st[PS_ROWS], n = st[PS_ENTRIES], br = st[PS_BOUND_ROWS], bn = st[PS_BOUND_NEW], bl = st[PS_BOUND_LEN];
+    e = p.bk.entries[min(i, p.bk.max_seqs - 1)];
+    request_together(R, n, br, bn, bl, e.slot, e.ctx, e.m, e.r0, e.part, e.kind);
+    if (R > 0 && (br != p.rows || bn != p.max_new || bl != p.max_len)) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.bk.status[PS_LATE] = 1;
+        return false;
+    }
+    count = n;
+    return R > 0 && i < n;
+}
+
+// What a workgroup of the span kernel takes, one after another: the plan's units; behind a window, of block x of every
+// gridDim.z-th request the y-th span that the block sees (all of them where the request has no partial states).
+template <int ROWS, bool WIN>
+struct SpanUnits {
+    int idx = blockIdx.x, z = blockIdx.z, count = 0;
+    __device__ __forceinline__ bool next(const PagedAttnParams &p, int cap, PagedUnit &u, int &h) {
+        if constexpr (!WIN) {
+            const bool more = next_unit<false>(p, idx / p.n_kv, cap, u, count);
+            h = idx % p.n_kv;
+            idx += gridDim.x;
+            return more;
+        }
+        for (; idx < p.blocks * p.n_kv; idx += gridDim.x, z = blockIdx.z) {
+            PagedEntry e;
+            while (next_entry(p, z, e, count)) {
+                z += gridDim.z;
+                const int j = blockIdx.y, row = idx / p.n_kv * ROWS;
+                if (e.kind != PE_BLOCKS || row >= e.m * p.group || (e.part < 0 && j > 0)) continue;
+                u = PagedUnit{e.slot, e.ctx, e.m, e.r0, row, j, e.part < 0 ? kAllSpans : j + 1,
+                              e.part < 0 ? -1 : e.part + j * e.m * p.group + row};
+                h = idx % p.n_kv;
+                return true;
+            }
+            if (count == 0) break;
+        }
+        return false;
+    }
+};
+
+// What a workgroup of the request kernel takes, where u.k0 < 0.
+template <bool WIN>
+__device__ __forceinline__ bool next_request(const PagedAttnParams &p, int i, int cap, PagedUnit &u, int &count) {
+    if constexpr (!WIN) return next_unit<false>(p, i, cap, u, count);
+    PagedEntry e;
+    const bool more = next_entry(p, i, e, count);
+    u = PagedUnit{e.slot, e.ctx, e.m, e.r0, 0, e.kind == PE_WHOLE ? -1 : 0, kAllSpans, -1};
+    return more;
+}
+
 }  // namespace
 
 namespace {
 
-// Four columns of one row of an item: the states of its spans (those up to the row's position) or ranges.
-template <Prec P, int HD>
+// Four columns of one row of an item: the states of its spans (those up to the row's position; behind a window those of
+// its block that it sees) or ranges.
+template <Prec P, int HD, bool WIN>
 __device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedItem &it, int h, int row, int col) {
     if (row >= min(kPagedItemRows, it.m * p.group - it.row)) return;
     const RowMap map(p, it.row);
-    const int count = it.count > 0 ? it.count : (it.ctx + map.token(row)) / kPagedSpanKeys + 1;
+    const Sight<WIN> see(p);
+    const int pos = it.ctx + map.token(row);
+    int count = it.count > 0 ? it.count : pos / kPagedSpanKeys + 1;
+    Visible<WIN, kPagedSpanKeys> spans(see, pos, pos);
+    if (WIN && it.count == 0) {
+        constexpr int BR = paged_block_rows(P == Prec::BF16, HD);
+        const int first = row / BR * BR, last = min(first + BR, it.m * p.group - it.row) - 1;  // (an item begins with a block)
+        spans = Visible<WIN, kPagedSpanKeys>(see, it.ctx + map.token(first), it.ctx + map.token(last));
+        count = spans.count;
+    }
     float M = -INFINITY, l = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr int U = 4;  // states in flight (of short rows, more repeat the last one's loads)
@@ -265,7 +359,11 @@ __device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedIt
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const bool use = s0 + i < count;  // a select: a branch would sink the loads behind it
+            bool use = s0 + i < count;  // a select: a branch would sink the loads behind it
+            if (WIN && it.count == 0) {
+                const int k = spans.piece(s0 + i) * kPagedSpanKeys;
+                use = use && k <= pos && see.some(pos, k, kPagedSpanKeys);
+            }
             float Mn = M, w0, w1;
             merge_weights(Mn, Ms[i], w0, w1);
             const float ln = merge_value(l, ls[i], w0, w1);
@@ -297,8 +395,8 @@ constexpr int class_words(int hd) { return (hd + kWave - 1) / kWave; }
 // memory, at[]: the first elements of its four tiles of 16 keys). valid: keys of the chunk that the request
 // has (behind them a page holds whatever it did before), kKeys where the others have been cleared; qpos: the lane's rows' positions in the chunk. Says
 // whether the classes cls are to be added to the result.
-template <Prec P, int HD, int NRG, int N, int NPL>
-__device__ __forceinline__ bool chunk_values(const PagedAttnParams &p, const uint8_t *V, const size_t (&at)[4], int valid,
+template <Prec P, int HD, bool WIN, int NRG, int N, int NPL>
+__device__ __forceinline__ bool chunk_values(const PagedAttnParams &p, const uint8_t *V, const size_t (&at)[4], int valid, int key0,
                                              const u32x4 (&pb)[NRG][NPL][N], const int (&qpos)[NRG], f32x4 (&oc)[NRG][HD / 16],
                                              uint64_t (&cls)[class_words(HD)]) {
     constexpr bool B = P == Prec::BF16;
@@ -379,9 +477,10 @@ __device__ __forceinline__ bool chunk_values(const PagedAttnParams &p, const uin
             int key = 0;
 #pragma unroll 1
             for (int r = 0; r < 16 * NRG; ++r) {  // the rows' positions do not fall
-                const int last = min(__builtin_amdgcn_readlane(r < 16 ? qpos[0] : qpos[NRG - 1], r & 15), kKeys - 1);
+                const int pos = __builtin_amdgcn_readlane(r < 16 ? qpos[0] : qpos[NRG - 1], r & 15), last = min(pos, kKeys - 1);
+                if (WIN) key = 0, acc = 0.f;  // behind a window, row by row
                 for (; key <= last; ++key) {
-                    if (col >= HD) continue;
+                    if (col >= HD || !Sight<WIN>(p).key(key0 + pos, key0 + key)) continue;
                     uint32_t x;
                     if constexpr (B) {
                         using TL = Tile<HD>;
@@ -406,7 +505,7 @@ __device__ __forceinline__ float class_value(uint32_t c) { return (c & 3) == 1 ?
 
 // One chunk of the span kernel, by one wave: the states of its NRG groups of 16 rows into s_mine ([row][column])
 // and s_m, s_l (this wave's rows). last_key: the request's last token; pages: its table.
-template <Prec P, int HD, int NRG>
+template <Prec P, int HD, bool WIN, int NRG>
 __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const PagedUnit &u, const RowMap &map, int h, int rows, int key0,
                                            int last_key, const int32_t *table, uint8_t *s_mine, float *s_m, float *s_l) {
     using PT = PrecT<P>;
@@ -463,7 +562,7 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) st[kt] = mfma_kstep<P>(kf[kt][kk], q[rg][kk], st[kt]);
         }
-        chunk_softmax(st, qpos[rg], p.scale_log2, lane, mx[rg], lc[rg]);
+        chunk_softmax<WIN>(st, qpos[rg], Sight<WIN>(p), key0, p.scale_log2, lane, mx[rg], lc[rg]);
         weight_operand<P>(st, pb[rg]);
     }
     if constexpr (B) {
@@ -474,7 +573,7 @@ __device__ __forceinline__ void span_chunk(const PagedAttnParams &p, const Paged
     }
     f32x4 oc[NRG][NDT];
     uint64_t cls[class_words(HD)];
-    const bool taken = chunk_values<P, HD>(p, s_mine, at, B ? kKeys : valid, pb, qpos, oc, cls);
+    const bool taken = chunk_values<P, HD, WIN>(p, s_mine, at, B ? kKeys : valid, key0, pb, qpos, oc, cls);
     // V has been read: the states in its place
 #pragma unroll
     for (int rg = 0; rg < NRG; ++rg) {
@@ -558,7 +657,9 @@ struct ChunkLoads {
 // and 3.8 (one workgroup a CU, as K takes the registers of two). Spans of 512 keys by eight waves leave one
 // workgroup a CU: 259 us in place of 224. The last workgroup of a row joining its spans in place of a kernel costs
 // 10 us of fences.
-template <Prec P, int HD, int RG>
+// Behind a window (WIN) the grid is (blocks x key heads, spans that a block sees, requests): the plan's units are all spans
+// up to a row's position.
+template <Prec P, int HD, int RG, bool WIN>
 __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
                                                                                                   int cap_units) {
     constexpr bool WHOLE = P == Prec::F32;  // several spans without partials
@@ -569,16 +670,17 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];  // the chunks' statistics
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     uint8_t *s_mine = s_all + (size_t)w * REGION;
-    int count = 0;
+    int h;
     PagedUnit u;
-    for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
-        const int h = idx % p.n_kv;
-        if (u.k0 < 0) continue;  // a whole request's (uniform)
+    for (SpanUnits<ROWS, WIN> units; units.next(p, cap_units, u, h);) {
+        if (!WIN && u.k0 < 0) continue;  // a whole request's (uniform)
         const int rows = min(ROWS, u.m * p.group - u.row);
         const RowMap map(p, u.row);
         const int blast = u.ctx + map.token(rows - 1);  // the block's last position
         const int last_key = u.ctx + u.m - 1;
-        const int s0 = u.k0, s1 = min(u.k1, blast / kPagedSpanKeys + 1);
+        const Sight<WIN> see(p);
+        const Visible<WIN, kPagedSpanKeys> spans(see, WIN ? u.ctx + map.token(0) : 0, blast);
+        const int s0 = u.k0, s1 = min(u.k1, spans.count);
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
         // states of this thread's (row, four columns) items over the spans
         float Mr[WHOLE ? ITEMS : 1], lr[WHOLE ? ITEMS : 1];
@@ -588,12 +690,13 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
             for (int i = 0; i < ITEMS; ++i) Mr[i] = -INFINITY, lr[i] = 0.f, orow[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         for (int s = s0; s < s1; ++s) {
-            const int c0 = s * kSpanChunks, key0 = (c0 + w) * kKeys;
-            if (key0 <= blast) {  // uniform over the wave
+            const int c0 = spans.piece(s) * kSpanChunks, key0 = (c0 + w) * kKeys;
+            // uniform over the wave; a chunk that no row of the block sees is left out (the first row's window begins first)
+            if (key0 <= blast && see.some(u.ctx + map.token(0), key0, kKeys)) {
                 if (RG == 1 || rows <= 16)
-                    span_chunk<P, HD, 1>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                    span_chunk<P, HD, WIN, 1>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
                 else
-                    span_chunk<P, HD, RG>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                    span_chunk<P, HD, WIN, RG>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
             }
             __syncthreads();
 #pragma unroll
@@ -606,6 +709,7 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
 #pragma unroll
                 for (int k = 0; k < NW; ++k) {
                     if ((c0 + k) * kKeys > pos) break;  // chunks that the row does not see
+                    if (!see.some(pos, (c0 + k) * kKeys, kKeys)) continue;
                     const f32x4 oc = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(s_all + (size_t)k * REGION) +
                                                                       row * SROW + col);
                     float wo, wc;
@@ -625,7 +729,7 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
                 }
                 float Mo = -INFINITY, v, vc;
                 if constexpr (WHOLE) {
-                    if (c0 * kKeys <= pos) {
+                    if (c0 * kKeys <= pos && see.some(pos, c0 * kKeys, kPagedSpanKeys)) {
                         merge_weights(Mr[i], M, v, vc);
                         lr[i] = merge_value(lr[i], l, v, vc);
 #pragma unroll
@@ -654,7 +758,8 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
 // Bound: reading the cache, one chunk of 32 KiB a workgroup (head_dim 128, two a CU) ahead. 64 requests of 36
 // rows at 4000 keys, 8 key heads: 205 us, 5.1 TB/s. 16 ragged requests of 32 rows at 256 to 1280 keys, 32
 // heads: 218 MB in 49 us. The unit list is the span kernel's, and each passes over the other's units.
-template <int HD>
+// Behind a window (WIN) it walks the plan's requests.
+template <int HD, bool WIN>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_kernel(PagedAttnParams p, int cap_units) {
     constexpr Prec P = Prec::BF16;
     using TL = Tile<HD>;
@@ -665,20 +770,22 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_ke
     const int lane = loads.lane, w = loads.w, g = lane >> 4, r16 = lane & 15;
     int count = 0;
     PagedUnit u;
-    for (int idx = blockIdx.x; next_unit<false>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
+    for (int idx = blockIdx.x; next_request<WIN>(p, idx / p.n_kv, cap_units, u, count); idx += gridDim.x) {
         if (u.k0 >= 0) continue;  // the span kernel's (uniform)
         const int h = idx % p.n_kv, rows = u.m * p.group;
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
         const RowMap map(p, 0);
         const int last_key = u.ctx + u.m - 1, last_tile = last_key >> 4;
         const int blast = u.ctx + map.token(rows - 1), wlast = u.ctx + map.token(min(16 * w + 15, rows - 1));
-        const int c1 = blast / kKeys + 1;
+        const Sight<WIN> see(p);
+        const Visible<WIN, kKeys> chunks(see, u.ctx, blast);
+        const int c1 = chunks.count, wfirst = WIN ? u.ctx + map.token(min(16 * w, rows - 1)) : 0;
         const bool live = 16 * w < rows;  // uniform over the wave
         const int row = min(16 * w + r16, rows - 1), token = map.token(row), head = h * p.group + map.head(row);
-        int pg = loads.pages(p, table, 0, last_tile);
+        int pg = loads.pages(p, table, chunks.piece(0), last_tile);
         __syncthreads();  // the unit before is done with the buffers
-        loads.issue(p, h, 0, last_tile, pg, s_kv);
-        pg = loads.pages(p, table, 1, last_tile);
+        loads.issue(p, h, chunks.piece(0), last_tile, pg, s_kv);
+        pg = loads.pages(p, table, chunks.piece(1), last_tile);
         u32x4 q[NKK];
         const uint16_t *qrow = reinterpret_cast<const uint16_t *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + g * 8;
 #pragma unroll
@@ -688,14 +795,14 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_ke
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o[dt] = orow[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int c = 0; c < c1; ++c) {
-            const int key0 = c * kKeys;
+            const int chunk = chunks.piece(c), key0 = chunk * kKeys;
             const uint8_t *K = s_kv + (size_t)(c & 1) * 2 * TL::BYTES, *V = K + TL::BYTES;
             wait_vm_lds<0>();
             barrier_no_fence();  // every wave's pieces of the chunk have landed, and the other buffer has been read
-            if (c + 1 < c1) loads.issue(p, h, c + 1, last_tile, pg, s_kv + (size_t)((c + 1) & 1) * 2 * TL::BYTES);
-            pg = loads.pages(p, table, c + 2, last_tile);
+            if (c + 1 < c1) loads.issue(p, h, chunks.piece(c + 1), last_tile, pg, s_kv + (size_t)((c + 1) & 1) * 2 * TL::BYTES);
+            pg = loads.pages(p, table, chunks.piece(c + 2), last_tile);
             if (!live) continue;
-            if (key0 <= wlast) {  // uniform over the wave
+            if (key0 <= wlast && see.some(wfirst, key0, kKeys)) {  // uniform over the wave
                 f32x4 st[4];
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt) {
@@ -709,12 +816,12 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_ke
                 const int qpos[1] = {u.ctx + token - key0};
                 float mx, lc;
                 u32x4 pb[1][2][2];
-                chunk_softmax(st, qpos[0], p.scale_log2, lane, mx, lc);
+                chunk_softmax<WIN>(st, qpos[0], see, key0, p.scale_log2, lane, mx, lc);
                 weight_operand<P>(st, pb[0]);
                 f32x4 oc[1][NDT];
                 uint64_t cls[class_words(HD)];
                 const size_t at[4] = {};
-                if (chunk_values<P, HD>(p, V, at, last_key - key0 + 1, pb, qpos, oc, cls)) {
+                if (chunk_values<P, HD, WIN>(p, V, at, last_key - key0 + 1, key0, pb, qpos, oc, cls)) {
 #pragma unroll
                     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -723,7 +830,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_ke
                             if (k) oc[0][dt][e] += class_value(k);
                         }
                 }
-                if (qpos[0] >= 0) {
+                if (qpos[0] >= 0 && see.some(u.ctx + token, key0, kKeys)) {
                     float wo, wc;
                     merge_weights(M, mx, wo, wc);
                     l = merge_value(l, lc, wo, wc);
@@ -733,8 +840,11 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_ke
                         for (int e = 0; e < 4; ++e) o[dt][e] = merge_value(o[dt][e], oc[0][dt][e], wo, wc);
                 }
             }
-            if (c % kSpanChunks + 1 < kSpanChunks && c + 1 < c1) continue;
-            if (c / kSpanChunks * kPagedSpanKeys <= u.ctx + token) {
+            if (WIN ? c + 1 < c1 && chunks.piece(c + 1) / kSpanChunks == chunk / kSpanChunks
+                    : c % kSpanChunks + 1 < kSpanChunks && c + 1 < c1)
+                continue;
+            const int span0 = chunk / kSpanChunks * kPagedSpanKeys;
+            if (span0 <= u.ctx + token && see.some(u.ctx + token, span0, kPagedSpanKeys)) {
                 float v, vc;
                 merge_weights(Mr, M, v, vc);
                 lr = merge_value(lr, l, v, vc);
@@ -781,7 +891,8 @@ constexpr int tile_lds() {
 // nothing waits for one thing alone. Reads that run ahead of the softmax, softmax and products of two chunks
 // interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 800
 // TFLOP/s, 32 wide 640, 256 wide 490 (one workgroup a CU, and 32 registers spilled).
-template <int HD>
+// Behind a window (WIN) a tile walks the chunks that its rows see; a range of the plan's is that share of them.
+template <int HD, bool WIN>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
     using TL = Tile<HD>;
     constexpr int NKK = HD / 16, NDT = HD / 32;
@@ -803,14 +914,21 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
         const RowMap map(p, u.row);
         const int tfirst = u.ctx + map.token(0), tlast = u.ctx + map.token(rows - 1);
         const int wfirst = u.ctx + map.token(min(32 * w, rows - 1)), wlast = u.ctx + map.token(min(32 * w + 31, rows - 1));
-        const int c0 = u.k0, c1 = min(u.k1, tlast / kKeys + 1);
+        const Sight<WIN> see(p);
+        const Visible<WIN, kKeys> chunks(see, tfirst, tlast);
+        int c0 = u.k0, c1 = min(u.k1, tlast / kKeys + 1);
+        if (WIN && chunks.count <= tlast / kKeys) {  // (a tile that sees every chunk: as without a window, with the same bits)
+            const int all = (kvlen + kKeys - 1) / kKeys;
+            c0 = (int)((int64_t)min(u.k0, all) * chunks.count / all);
+            c1 = (int)((int64_t)min(u.k1, all) * chunks.count / all);
+        }
         const bool live = 32 * w < rows;  // uniform over the wave
         const int rr = min(32 * w + r32, rows - 1), token = map.token(rr), head = h * p.group + map.head(rr);
         const int qpos = u.ctx + token;
-        int pg = loads.pages(p, table, c0, last_tile);
+        int pg = loads.pages(p, table, chunks.piece(c0), last_tile);
         __syncthreads();  // the unit before is done with the buffers
-        if (c0 < c1) loads.issue(p, h, c0, last_tile, pg, s_kv);
-        pg = loads.pages(p, table, c0 + 1, last_tile);
+        if (c0 < c1) loads.issue(p, h, chunks.piece(c0), last_tile, pg, s_kv);
+        pg = loads.pages(p, table, chunks.piece(c0 + 1), last_tile);
         u32x4 q[NKK];
         const uint16_t *qrow = reinterpret_cast<const uint16_t *>(p.q) + (size_t)(u.r0 + token) * p.q_stride + head * HD + hb * 8;
 #pragma unroll
@@ -822,14 +940,14 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
         for (int c = c0; c < c1; ++c) {
-            const int buf = (c - c0) & 1, key0 = c * kKeys;
+            const int buf = (c - c0) & 1, key0 = chunks.piece(c) * kKeys;
             wait_vm_lds<0>();
             barrier_no_fence();  // every wave's pieces of the chunk have landed, and the other buffer has been read
-            if (c + 1 < c1) loads.issue(p, h, c + 1, last_tile, pg, s_kv + (size_t)(buf ^ 1) * 2 * TL::BYTES);
-            pg = loads.pages(p, table, c + 2, last_tile);
+            if (c + 1 < c1) loads.issue(p, h, chunks.piece(c + 1), last_tile, pg, s_kv + (size_t)(buf ^ 1) * 2 * TL::BYTES);
+            pg = loads.pages(p, table, chunks.piece(c + 2), last_tile);
             const uint8_t *K = s_kv + (size_t)buf * 2 * TL::BYTES;
             uint8_t *V = s_kv + (size_t)buf * 2 * TL::BYTES + TL::BYTES;
-            if (key0 + kKeys - 1 > tfirst) {  // uniform: keys that some row does not see
+            if (key0 + kKeys - 1 > tfirst || see.cuts(tlast, key0, kKeys)) {  // uniform: keys that some row does not see
                 // A weight of 0 does not silence a NaN or an infinity in the product. Values behind the
                 // request's last token are cleared, whatever the page holds there; others that are not
                 // finite (rare) are taken out, and what the rows that see them get from them is added to
@@ -851,20 +969,33 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                     for (int col = tid; col < HD; col += 256) {
                         float acc = 0.f;
                         int key = 0;
+                        uint64_t odd[3] = {};  // WIN: keys of +inf, -inf, NaN
                         auto next = [&]() {
                             uint16_t *v = reinterpret_cast<uint16_t *>(V + key * TL::ROWB + ((col / 8) ^ TL::vswz(key)) * 16) + col % 8;
                             const uint32_t x = (uint32_t)*v << 16;
                             if ((x & 0x7f800000u) == 0x7f800000u) {
                                 acc += __uint_as_float(x);
+                                if (WIN) odd[x == 0x7f800000u ? 0 : x == 0xff800000u ? 1 : 2] |= 1ull << key;
                                 *v = 0;
                             }
                             ++key;
                         };
+                        if (WIN)
+                            while (key < kKeys) next();
                         for (int r0 = 0; r0 < kPagedTileRows; r0 += 16) {
                             uint32_t bits = 0;
                             for (int r = r0; r < r0 + 16; ++r) {
-                                const int last = min(u.ctx + map.token(min(r, rows - 1)) - key0, kKeys - 1);
-                                while (key <= last) next();
+                                const int pos = u.ctx + map.token(min(r, rows - 1)), last = min(pos - key0, kKeys - 1);
+                                if constexpr (WIN) {
+                                    // bits [0, n) of the chunk
+                                    auto below = [](int n) { return n <= 0 ? 0ull : n >= kKeys ? ~0ull : (1ull << n) - 1; };
+                                    const uint64_t seen =
+                                        below(last + 1) & (~below(pos - see.window + 1 - key0) | below(see.sinks - key0));
+                                    const bool plus = odd[0] & seen, minus = odd[1] & seen;
+                                    acc = (odd[2] & seen) || (plus && minus) ? NAN : plus ? INFINITY : minus ? -INFINITY : 0.f;
+                                } else {
+                                    while (key <= last) next();
+                                }
                                 bits |= (acc != acc ? 3u : acc == INFINITY ? 1u : acc == -INFINITY ? 2u : 0u) << (2 * (r - r0));
                             }
                             s_cls[col * (kPagedTileRows / 16) + r0 / 16] = bits;
@@ -884,7 +1015,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                     __syncthreads();  // the classes have been read
                 }
             }
-            if (!live || key0 > wlast) continue;
+            if (!live || key0 > wlast || !see.some(wfirst, key0, kKeys)) continue;
             // Reads run ahead of the products that take them (the scheduler would put each next to its
             // product, behind a wait for it alone).
             u32x4 kf[NKK][2];
@@ -917,12 +1048,12 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
             read_v(0);
             __builtin_amdgcn_sched_barrier(0);
             // st[kt][i] = S^T[key 32 kt + 8 (i / 4) + 4 hb + i % 4][row r32]
-            if (key0 + kKeys - 1 > wfirst) {
+            if (key0 + kKeys - 1 > wfirst || see.cuts(wlast, key0, kKeys)) {
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (key0 + 32 * kt + 8 * (i / 4) + 4 * hb + i % 4 > qpos) st[kt][i] = -INFINITY;
+                        if (!see.key(qpos, key0 + 32 * kt + 8 * (i / 4) + 4 * hb + i % 4)) st[kt][i] = -INFINITY;
             }
             float mx = -INFINITY;
 #pragma unroll
@@ -991,7 +1122,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
 // Joins the partial states of split row blocks, in position order. Workgroup: some rows of one key head of
 // an item, a thread per four columns of a row. Bound: latency, four states in flight a thread: 3.3 us for three
 // spans, 13 us for 64 requests of 4 to 32 spans (16 in flight: 15.5 in place of 8.3 us at 16 requests).
-template <Prec P, int HD>
+template <Prec P, int HD, bool WIN>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int cap_items) {
     constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedItemRows + RPW - 1) / RPW;
     const int32_t *st = p.bk.status;
@@ -1002,7 +1133,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int 
     const int work = n * p.n_kv * NG;
     for (int idx = blockIdx.x; idx < work; idx += gridDim.x) {
         if (idx != (int)blockIdx.x) it = p.bk.items[idx / (p.n_kv * NG)];
-        join_row<P, HD>(p, it, idx % p.n_kv, idx / p.n_kv % NG * RPW + threadIdx.x / LPR, threadIdx.x % LPR * 4);
+        join_row<P, HD, WIN>(p, it, idx % p.n_kv, idx / p.n_kv % NG * RPW + threadIdx.x / LPR, threadIdx.x % LPR * 4);
     }
 }
 
@@ -1016,48 +1147,104 @@ hipError_t launch_spans(int64_t units, bool whole, const PagedAttnParams &p, hip
     // (where requests may be taken whole, fewer: passing over 2560 units takes 6.5 us, 4.6 in a grid of 1024; spans in
     // a grid of 1024 take up to 2% longer)
     const dim3 grid((unsigned)std::min<int64_t>(units * p.n_kv, whole ? 4 * kCUs : 16 * kCUs));
-    hipLaunchKernelGGL((paged_span_kernel<P, HD, RG>), grid, dim3(kSpanChunks * kWave), lds, s, p, p.bk.cap_units);
+    hipLaunchKernelGGL((paged_span_kernel<P, HD, RG, false>), grid, dim3(kSpanChunks * kWave), lds, s, p, p.bk.cap_units);
+    return hipGetLastError();
+}
+
+template <Prec P, int HD, bool WIN>
+hipError_t launch_join(int64_t units, int64_t tiles, const PagedAttnParams &p, hipStream_t s) {
+    const int64_t groups = (kPagedItemRows + 1024 / HD - 1) / (1024 / HD);
+    const int64_t work = std::min<int64_t>(units + 4 * tiles, p.bk.cap_items) * p.n_kv * groups;
+    hipLaunchKernelGGL((paged_join_kernel<P, HD, WIN>), dim3((unsigned)std::min<int64_t>(work, 8 * kCUs)), dim3(256), 0, s, p,
+                       p.bk.cap_items);
+    return hipGetLastError();
+}
+
+template <int HD, bool WIN>
+hipError_t launch_tiles(int64_t tiles, const PagedAttnParams &p, hipStream_t s) {
+    hipLaunchKernelGGL((paged_tile_kernel<HD, WIN>), dim3((unsigned)std::min<int64_t>(tiles * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
+                       tile_lds<HD>(), s, p, p.bk.cap_tiles);
     return hipGetLastError();
 }
 
 template <Prec P, int HD, int RG>
-hipError_t launch_shape(int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
-    hipError_t e = launch_spans<P, HD, RG>(units, whole, p, s);
-    if (e != hipSuccess) return e;
-    if constexpr (P == Prec::BF16) {
-        if (whole > 0)
-            hipLaunchKernelGGL((paged_request_kernel<HD>), dim3((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
-                               4 * Tile<HD>::BYTES, s, p, p.bk.cap_units);
-        if (tiles > 0)
-            hipLaunchKernelGGL((paged_tile_kernel<HD>), dim3((unsigned)std::min<int64_t>(tiles * p.n_kv, 16 * kCUs)),
-                               dim3(4 * kWave), tile_lds<HD>(), s, p, p.bk.cap_tiles);
+struct FullCall {
+    int64_t units;
+    bool whole;
+    int64_t tiles;
+    bool join;
+    hipError_t operator()(const PagedAttnParams &p, hipStream_t s) const {
+        hipError_t e = launch_spans<P, HD, RG>(units, whole, p, s);
+        if constexpr (P == Prec::BF16) {
+            if (e == hipSuccess && whole) {
+                hipLaunchKernelGGL((paged_request_kernel<HD, false>), dim3((unsigned)std::min<int64_t>(units * p.n_kv, 16 * kCUs)),
+                                   dim3(4 * kWave), 4 * Tile<HD>::BYTES, s, p, p.bk.cap_units);
+                e = hipGetLastError();
+            }
+            if (e == hipSuccess && tiles > 0) e = launch_tiles<HD, false>(tiles, p, s);
+        }
+        return e == hipSuccess && join ? launch_join<P, HD, false>(units, tiles, p, s) : e;
     }
-    if (join) {
-        const int64_t groups = (kPagedItemRows + 1024 / HD - 1) / (1024 / HD);
-        const int64_t work = std::min<int64_t>(units + 4 * tiles, p.bk.cap_items) * p.n_kv * groups;
-        hipLaunchKernelGGL((paged_join_kernel<P, HD>), dim3((unsigned)std::min<int64_t>(work, 8 * kCUs)), dim3(256), 0, s, p,
-                           p.bk.cap_items);
+};
+
+template <Prec P, int HD, int RG>
+struct WindowCall {
+    int n;
+    int64_t most;
+    bool whole;
+    int64_t tiles;
+    bool join;
+    hipError_t operator()(const PagedAttnParams &call, hipStream_t s) const {
+        constexpr int ROWS = 16 * RG;
+        PagedAttnParams p = call;
+        p.blocks = (int)((std::min<int64_t>(most, P == Prec::BF16 ? kPagedFewRows : most) + ROWS - 1) / ROWS);
+        const dim3 grid((unsigned)std::min(p.blocks * p.n_kv, 1 << 20), (unsigned)p.spans, (unsigned)n);
+        hipLaunchKernelGGL((paged_span_kernel<P, HD, RG, true>), grid, dim3(kSpanChunks * kWave),
+                           kSpanChunks * (span_wave_lds<P, HD, RG>()), s, p, 0);
+        hipError_t e = hipGetLastError();
+        if constexpr (P == Prec::BF16) {
+            if (e == hipSuccess && whole) {
+                hipLaunchKernelGGL((paged_request_kernel<HD, true>), dim3((unsigned)std::min(n * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
+                                   4 * Tile<HD>::BYTES, s, p, 0);
+                e = hipGetLastError();
+            }
+            if (e == hipSuccess && tiles > 0) e = launch_tiles<HD, true>(tiles, p, s);
+        }
+        return e == hipSuccess && join ? launch_join<P, HD, true>((int64_t)n * p.blocks, tiles, p, s) : e;
     }
-    return hipGetLastError();
+};
+
+// The call of the shape.
+template <template <Prec, int, int> class Call, class... A>
+hipError_t launch_shape(bool bf16, const PagedAttnParams &p, hipStream_t s, A... a) {
+    if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group) return hipErrorInvalidValue;
+    if (bf16) {
+        if (p.hd == 32) return Call<Prec::BF16, 32, 2>{a...}(p, s);
+        if (p.hd == 64) return Call<Prec::BF16, 64, 2>{a...}(p, s);
+        if (p.hd == 128) return Call<Prec::BF16, 128, 2>{a...}(p, s);
+        if (p.hd == 256) return Call<Prec::BF16, 256, 1>{a...}(p, s);
+    } else {
+        if (p.hd == 16) return Call<Prec::F32, 16, 2>{a...}(p, s);
+        if (p.hd == 32) return Call<Prec::F32, 32, 2>{a...}(p, s);
+        if (p.hd == 64) return Call<Prec::F32, 64, 2>{a...}(p, s);
+        if (p.hd == 128) return Call<Prec::F32, 128, 1>{a...}(p, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 hipError_t launch_paged_attn(bool bf16, int64_t units, bool whole, int64_t tiles, bool join, const PagedAttnParams &p, hipStream_t s) {
-    if (p.n_kv < 1 || p.group < 1 || p.n_heads != p.n_kv * p.group || units < 0 || tiles < 0) return hipErrorInvalidValue;
+    if (units < 0 || tiles < 0) return hipErrorInvalidValue;
     if (units + tiles == 0 || p.rows == 0) return hipSuccess;
-    if (bf16) {
-        if (p.hd == 32) return launch_shape<Prec::BF16, 32, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::BF16, 64, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::BF16, 128, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 256) return launch_shape<Prec::BF16, 256, 1>(units, whole, tiles, join, p, s);
-    } else {
-        if (p.hd == 16) return launch_shape<Prec::F32, 16, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 32) return launch_shape<Prec::F32, 32, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 64) return launch_shape<Prec::F32, 64, 2>(units, whole, tiles, join, p, s);
-        if (p.hd == 128) return launch_shape<Prec::F32, 128, 1>(units, whole, tiles, join, p, s);
-    }
-    return hipErrorInvalidValue;
+    return launch_shape<FullCall>(bf16, p, s, units, whole, tiles, join);
+}
+
+hipError_t launch_paged_attn_window(bool bf16, int n, int64_t most, bool whole, int64_t tiles, bool join, const PagedAttnParams &p,
+                                    hipStream_t s) {
+    if (n < 1 || most < 0 || tiles < 0 || p.window < 1 || p.sinks < 0 || p.spans < 1) return hipErrorInvalidValue;
+    if (most == 0 || p.rows == 0) return hipSuccess;
+    return launch_shape<WindowCall>(bf16, p, s, n, most, whole, tiles, join);
 }
 
 }  // namespace cllm

@@ -142,6 +142,7 @@ Bufs buffers(cllm_paged *c) {
             Buf{P(&bk.units), (size_t)bk.cap_units * sizeof(PagedUnit)},
             Buf{P(&bk.tiles), (size_t)bk.cap_tiles * sizeof(PagedUnit)},
             Buf{P(&bk.items), (size_t)bk.cap_items * sizeof(PagedItem)},
+            Buf{P(&bk.entries), (size_t)f.max_seqs * sizeof(PagedEntry)},
             Buf{P(&c->part_o), part * f.head_dim * 4},
             Buf{P(&c->part_m), part * 4},
             Buf{P(&c->part_l), part * 4}})
@@ -444,9 +445,11 @@ cllm_status cllm_paged_append_norm(cllm_paged *c, const void *q, int64_t q_strid
     return append(c, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, k_pages, v_pages, q_gain, k_gain, eps);
 }
 
-cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
-                            float scale, void *out, int64_t out_stride, float *lse) {
-    if (!c) return CLLM_ERR_ARG;
+namespace {
+
+// window 0: none
+cllm_status attend(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages, float scale,
+                   int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse) {
     cllm_status s;
     if ((s = check(c))) return s;
     if (!c->planned) return fail(c, CLLM_ERR_STATE, "attention before a plan");
@@ -496,9 +499,37 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
     // more requests
     const int64_t blocks = std::min<int64_t>(f.max_seqs, (int64_t)c->rows * c->group / (kPagedWaveRows + 1));
     const bool whole = c->tiled && most > kPagedWaveRows && blocks * f.n_kv_heads >= kPagedTileGroups;
-    HIPCHK(c, launch_paged_attn(c->bf16, units, whole, tiles, spans > 1, p, c->stream));
+    if (window == 0 || window >= c->max_len) {  // (a window that holds every token: what the call without one does)
+        HIPCHK(c, launch_paged_attn(c->bf16, units, whole, tiles, spans > 1, p, c->stream));
+        return CLLM_OK;
+    }
+    p.window = window;
+    p.sinks = std::min(sinks, c->max_len);
+    // a block's tokens end in at most block_rows positions; the window of the first begins anywhere in a span
+    const int64_t reach = (int64_t)window + std::min(c->max_new, c->block_rows) - 1;
+    const int64_t sink_spans = (p.sinks + kPagedSpanKeys - 1) / kPagedSpanKeys;
+    p.spans = (int)std::min(spans, (reach + kPagedSpanKeys - 1) / kPagedSpanKeys + 1 + sink_spans);
+    HIPCHK(c, launch_paged_attn_window(c->bf16, c->n, most, whole, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
 }
+
+}  // namespace
+
+cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                            float scale, void *out, int64_t out_stride, float *lse) {
+    if (!c) return CLLM_ERR_ARG;
+    return attend(c, q, q_stride, k_pages, v_pages, scale, 0, 0, out, out_stride, lse);
+}
+
+cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
+                                   float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse) {
+    if (!c) return CLLM_ERR_ARG;
+    cllm_status s;
+    if ((s = check(c))) return s;
+    if (window < 1 || sinks < 0) return fail(c, CLLM_ERR_ARG, "window=%d (at least 1), sinks=%d (at least 0)", window, sinks);
+    return attend(c, q, q_stride, k_pages, v_pages, scale, window, sinks, out, out_stride, lse);
+}
+
 
 cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages) {
     if (!c) return CLLM_ERR_ARG;
