@@ -542,6 +542,34 @@ cllm_status cllm_paged_attn(cllm_paged *c, const void *q, int64_t q_stride, cons
 cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_stride, const void *k_pages, const void *v_pages,
                                    float scale, int32_t window, int32_t sinks, void *out, int64_t out_stride, float *lse);
 
+/* Verification of drafted tokens (any block of a plan: a pending token and guesses behind it, with or without a draft
+ * model): how many of a request's tokens stand against the target's distribution, and the token that follows them. The
+ * accepted counts are on the device, as the lengths of the next plan are.
+ *
+ * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device; row_start NULL:
+ * those of the last plan; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
+ * and element's alignment) are the target's behind tokens[r]; tokens[r + 1] is its draft. With p = softmax(logits /
+ * temperature[b]) and q the softmax of the draft's logits at the same temperature (draft_logits NULL, or a row of them
+ * without a distribution: a point mass on the draft), the draft x stands where accept_u[r] q(x) < p(x). At the first row
+ * whose draft does not stand, the next token is drawn from max(p - q, 0) (where that is 0 everywhere, from p), behind the last
+ * row from p; so a request of one row just draws. Drawn is the lowest index whose running sum is above sample_u[b] times the
+ * sum. Temperature 0 is greedy: p and q are 1 at the largest logit (ties: the lowest index): the acceptance of a Jacobi
+ * block (cllm_jacobi_step). Weights and sums are in 64 bits.
+ * accepted[b] (1 .. the request's rows): its rows that stand, the first one always; next_token[b]. A request of no rows, or
+ * whose rows are not within [0, rows], has 0 and -1. Where a row that is to be decided on has no distribution (a NaN or +inf logit, all
+ * -inf; a temperature that is negative or not finite) the rows up to it are accepted and next_token is -1. A draft outside
+ * [0, vocab) does not stand and takes nothing from p. A number outside [0, 1) counts as the nearest in it in the draw.
+ * workspace: device memory of at least cllm_paged_verify_bytes() bytes (draft: whether there are draft logits), 256-byte aligned, used
+ * during the call: one for every stream that such calls run on at once. No allocation, no wait.
+ * Errors: ERR_ARG (n outside [1, max_seqs], sizes, strides, NULL or inaccessible arrays), ERR_STATE (row_start NULL before
+ * a plan), ERR_CAPACITY (workspace too small, rows x vocab above 2^41), ERR_DEVICE. */
+cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start, int32_t rows, const int32_t *tokens, int32_t dtype,
+                              int32_t vocab, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride,
+                              const float *temperature, const double *accept_u, const double *sample_u, int32_t *accepted,
+                              int32_t *next_token, void *workspace, size_t workspace_bytes);
+/* No device call. Errors: ERR_ARG, ERR_CAPACITY. */
+cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, size_t *bytes);
+
 /* Waits for the stream and says how the last plan went: its rows and the free pages (either may be
  * NULL). Errors: ERR_ARG or ERR_CAPACITY (the plan was refused), ERR_STATE (append or attention of a
  * replayed graph ran behind a plan with other bounds than its own and did nothing; or the stream is

@@ -75,7 +75,7 @@ EXPORTS = ["cllm_model_create", "cllm_model_set_weights", "cllm_model_init_rando
            "cllm_jacobi_decode_batch", "cllm_reset", "cllm_debug_logits", "cllm_trace_enable", "cllm_trace_read",
            "cllm_trace_count", "cllm_collect_states", "cllm_loss_head", "cllm_loss_head_device", "cllm_hidden_rows", "cllm_hidden_rows_noalloc", "cllm_seq_state", "cllm_timing_enable", "cllm_timing_read",
            "cllm_paged_workspace_bytes", "cllm_paged_create", "cllm_paged_free", "cllm_paged_views_get", "cllm_paged_plan",
-           "cllm_paged_append", "cllm_paged_rotary", "cllm_paged_rotary_freqs", "cllm_paged_append_norm", "cllm_paged_attn", "cllm_paged_attn_window", "cllm_paged_status", "cllm_paged_last_error",
+           "cllm_paged_append", "cllm_paged_rotary", "cllm_paged_rotary_freqs", "cllm_paged_append_norm", "cllm_paged_attn", "cllm_paged_attn_window", "cllm_paged_verify", "cllm_paged_verify_bytes", "cllm_paged_status", "cllm_paged_last_error",
            "cllm_streamed_weight_bytes", "cllm_workspace_bytes", "cllm_status_string", "cllm_last_error"]
 
 _lib = None
@@ -142,6 +142,9 @@ def lib():
         L.cllm_paged_append_norm.argtypes = [*L.cllm_paged_append.argtypes, _vp, _vp, _f32]
         L.cllm_paged_attn.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]
         L.cllm_paged_attn_window.argtypes = [_vp, _vp, _i64, _vp, _vp, _f32, _i32, _i32, _vp, _i64, _vp]
+        L.cllm_paged_verify.argtypes = [_vp, _i32, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                        ctypes.c_size_t]
+        L.cllm_paged_verify_bytes.argtypes = [_i32, _i32, _i32, P(ctypes.c_size_t)]
         L.cllm_paged_status.argtypes = [_vp, P(_i32), P(_i32)]
         L.cllm_paged_last_error.argtypes = [_vp]
         L.cllm_paged_last_error.restype = ctypes.c_char_p
@@ -454,6 +457,8 @@ class PagedCache:
         self.max_rows, self.rows = max_rows, 0
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self._int32, self._float32 = torch.int32, torch.float32
+        self._logits = {torch.bfloat16: 1, torch.float32: 0}
+        self._float64 = torch.float64
         self.pool_shape = (n_pages, n_kv_heads, page_size, head_dim)
         cfg = cllm_paged_config(n_heads, n_kv_heads, head_dim, 1 if dtype == "bf16" else 0, page_size, n_pages, max_seqs,
                                 max_ctx, max_rows, rope_base, device, None, None, 0)
@@ -638,6 +643,60 @@ class PagedCache:
             _changed(out)
         else:
             _changed(out, lse)
+
+    @staticmethod
+    def verify_workspace_bytes(rows, vocab, draft):
+        """cllm_paged_verify_bytes: bytes of the workspace of verify on so many rows, with draft logits or without."""
+        n = ctypes.c_size_t(0)
+        st = lib().cllm_paged_verify_bytes(rows, vocab, 1 if draft else 0, ctypes.byref(n))
+        if st != CLLM_OK:
+            raise CllmError(st, "cllm_paged_verify_bytes failed")
+        return int(n.value)
+
+    def _vector(self, x, dtype, count, name):
+        if x.dtype != dtype or x.dim() != 1 or x.numel() < count or not x.is_contiguous() or x.device != self.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {count} on {self.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        if x.requires_grad:
+            self._no_backward(name)
+        return x.data_ptr()
+
+    def _logit_rows(self, x, shape, dtype, name):
+        if x.shape != shape or x.dtype != dtype or x.device != self.device or x.stride(1) != 1 and shape[1] > 1:
+            raise ValueError(f"{name}: a {dtype} tensor {tuple(shape)} with contiguous rows on {self.device}, got {x.dtype} "
+                             f"{tuple(x.shape)} strides {x.stride()} on {x.device}")
+        if x.requires_grad:
+            self._no_backward(name)
+        return x.data_ptr(), (x.stride(0) if shape[0] > 1 else shape[1])
+
+    def verify(self, tokens, logits, accepted, next_token, temperature, accept_u, sample_u, row_start=None, draft_logits=None,
+               workspace=None):
+        """cllm_paged_verify: tokens int32 [rows] and logits [rows, vocab] (bfloat16 or float32, contiguous rows of any
+        stride) of the n requests that accepted and next_token (int32 [n]) are for; temperature float32 [n]; accept_u
+        float64 [rows], sample_u float64 [n], uniform in [0, 1); row_start int32 [n + 1] (None: the last plan's);
+        draft_logits as logits, or None. workspace: a uint8 tensor of verify_workspace_bytes (None: one from PyTorch's
+        allocator)."""
+        self._on_stream()
+        if logits.dim() != 2 or logits.dtype not in self._logits:
+            raise ValueError(f"logits: bfloat16 or float32 [rows, vocab], got {logits.dtype} {tuple(logits.shape)}")
+        shape, n = logits.shape, accepted.numel()
+        rows, vocab = shape
+        i32, f64 = self._int32, self._float64
+        lg = self._logit_rows(logits, shape, logits.dtype, "logits")
+        dl = (None, 0) if draft_logits is None else self._logit_rows(draft_logits, shape, logits.dtype, "draft_logits")
+        need = self.verify_workspace_bytes(rows, vocab, draft_logits is not None)
+        if workspace is None:
+            import torch
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        elif workspace.device != self.device or not workspace.is_contiguous() or workspace.element_size() != 1:
+            raise ValueError(f"workspace: a contiguous uint8 tensor on {self.device}")
+        self._check(self.L.cllm_paged_verify(
+            self.h, n, None if row_start is None else self._vector(row_start, i32, n + 1, "row_start"), rows,
+            self._vector(tokens, i32, rows, "tokens"), self._logits[logits.dtype], vocab, *lg, *dl,
+            self._vector(temperature, self._float32, n, "temperature"), self._vector(accept_u, f64, rows, "accept_u"),
+            self._vector(sample_u, f64, n, "sample_u"), self._vector(accepted, i32, n, "accepted"),
+            self._vector(next_token, i32, n, "next_token"), workspace.data_ptr(), workspace.numel()))
+        _changed(accepted, next_token, workspace)
 
     def status(self):
         """cllm_paged_status: (rows of the last plan, free pages); raises when it was refused."""

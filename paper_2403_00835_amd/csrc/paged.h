@@ -136,6 +136,26 @@ struct PagedAttnParams {
     int spans, blocks;            // the most spans that a row block of such a call sees, the most row blocks of a request
 };
 
+constexpr int kVerifyChunk = 4096;  // logits whose statistics one workgroup takes
+struct alignas(16) VerifyStat {
+    double sum;  // of the weights, relative to max
+    float max;   // NaN where a logit is
+    int top;     // its lowest index
+};
+
+struct VerifyParams {
+    const int32_t *row_start, *tokens;  // [n + 1], [rows]
+    const int32_t *status;              // of the plan whose row_start it is, or null
+    int n, rows, vocab, chunks;         // chunks of a row
+    const void *logits, *draft;         // [rows][vocab] of stride elements; draft may be null
+    int64_t stride, draft_stride;
+    const float *temperature;           // [n]
+    const double *accept_u, *sample_u;  // [rows], [n]
+    int32_t *accepted, *next_token;     // [n]
+    VerifyStat *stats;                  // [rows (twice with a draft)][chunks]
+    double *rest;                       // [rows][chunks], with a draft
+};
+
 // Rows of the last plan, or none when it was made for other bounds than the call's (a replayed graph
 // after another plan): the call's arrays may be smaller then, and its launches fewer.
 __device__ __forceinline__ int bounded_rows(const PagedBooks &bk, int rows, int max_new, int max_len) {
@@ -150,6 +170,7 @@ __device__ __forceinline__ int bounded_rows(const PagedBooks &bk, int rows, int 
 hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int hd,
                              double rope_base, hipStream_t s);
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s);
+hipError_t launch_paged_verify(bool bf16, const VerifyParams &p, hipStream_t s);
 hipError_t launch_paged_rotary(float *rcos, float *rsin, int max_ctx, int rot, double magnitude, const PagedFreqs &f, hipStream_t s);
 hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_t s);
 // The same with norms of the heads, and with any part of the head turned in either layout.

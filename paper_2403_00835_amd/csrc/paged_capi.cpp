@@ -531,6 +531,75 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
 }
 
 
+cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, size_t *bytes) {
+    if (!bytes) return CLLM_ERR_ARG;
+    *bytes = 0;
+    if (rows < 0 || vocab < 1) return CLLM_ERR_ARG;
+    const int64_t parts = (int64_t)rows * ((vocab - 1) / kVerifyChunk + 1);
+    if (2 * parts > INT32_MAX) return CLLM_ERR_CAPACITY;
+    *bytes = round_up((size_t)parts * (draft ? 2 * sizeof(VerifyStat) + sizeof(double) : sizeof(VerifyStat)));
+    return CLLM_OK;
+}
+
+cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start, int32_t rows, const int32_t *tokens, int32_t dtype,
+                              int32_t vocab, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride,
+                              const float *temperature, const double *accept_u, const double *sample_u, int32_t *accepted,
+                              int32_t *next_token, void *workspace, size_t workspace_bytes) {
+    if (!c) return CLLM_ERR_ARG;
+    cllm_status s;
+    if ((s = check(c))) return s;
+    const cllm_paged_config &f = c->cfg;
+    if (n < 1 || n > f.max_seqs) return fail(c, CLLM_ERR_ARG, "n=%d outside [1, max_seqs]", n);
+    if (dtype != CLLM_DTYPE_BF16 && dtype != CLLM_DTYPE_F32) return fail(c, CLLM_ERR_ARG, "unknown dtype %d", dtype);
+    if (!row_start && !c->planned) return fail(c, CLLM_ERR_STATE, "row_start NULL before a plan");
+    size_t need = 0;
+    if ((s = cllm_paged_verify_bytes(rows, vocab, draft_logits != nullptr, &need)))
+        return fail(c, s, "rows=%d (at least 0), vocab=%d (at least 1): too many, or out of range", rows, vocab);
+    DeviceGuard dev(f.device);
+    if (!dev.ok) return fail(c, CLLM_ERR_DEVICE, "the cache's device cannot be made current");
+    // a name, what each element's address is a multiple of, and whether the call may do without the array
+    const size_t elem = dtype == CLLM_DTYPE_BF16 ? 2 : 4;
+    const struct {
+        const char *name;
+        const void *p;
+        size_t align;
+        bool none;
+    } arrays[] = {{"row_start", row_start, 4, true},       {"temperature", temperature, 4, false}, {"sample_u", sample_u, 8, false},
+                  {"accepted", accepted, 4, false},        {"next_token", next_token, 4, false},   {"tokens", tokens, 4, rows == 0},
+                  {"logits", logits, elem, rows == 0},     {"draft_logits", draft_logits, elem, true},
+                  {"accept_u", accept_u, 8, rows == 0},    {"workspace", workspace, kAlign, rows == 0}};
+    for (const auto &a : arrays) {
+        if (!a.p && a.none) continue;
+        if (!a.p || reinterpret_cast<uintptr_t>(a.p) % a.align != 0 || !accessible(c, a.p))
+            return fail(c, CLLM_ERR_ARG, "%s: NULL, misaligned, or not device memory of the cache's GPU", a.name);
+    }
+    for (int64_t x : {stride, draft_logits ? draft_stride : stride})
+        if (x < vocab || x > (int64_t)1 << 40) return fail(c, CLLM_ERR_ARG, "row stride %lld (at least vocab, at most 2^40)", (long long)x);
+    if (workspace_bytes < need) return fail(c, CLLM_ERR_CAPACITY, "workspace of %zu bytes: %zu are needed", workspace_bytes, need);
+    VerifyParams p{};
+    p.row_start = row_start ? row_start : c->bk.row_start;
+    p.status = row_start ? nullptr : c->bk.status;
+    p.tokens = tokens;
+    p.n = n;
+    p.rows = rows;
+    p.vocab = vocab;
+    p.chunks = (vocab - 1) / kVerifyChunk + 1;
+    p.logits = logits;
+    p.draft = draft_logits;
+    p.stride = stride;
+    p.draft_stride = draft_stride;
+    p.temperature = temperature;
+    p.accept_u = accept_u;
+    p.sample_u = sample_u;
+    p.accepted = accepted;
+    p.next_token = next_token;
+    p.stats = static_cast<VerifyStat *>(workspace);
+    const size_t parts = (size_t)rows * p.chunks;
+    p.rest = draft_logits && rows > 0 ? reinterpret_cast<double *>(p.stats + 2 * parts) : nullptr;
+    HIPCHK(c, launch_paged_verify(dtype == CLLM_DTYPE_BF16, p, c->stream));
+    return CLLM_OK;
+}
+
 cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages) {
     if (!c) return CLLM_ERR_ARG;
     cllm_status s;
