@@ -546,8 +546,8 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * model): how many of a request's tokens stand against the target's distribution, and the token that follows them. The
  * accepted counts are on the device, as the lengths of the next plan are.
  *
- * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device; row_start NULL:
- * those of the last plan; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
+ * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device, ascending;
+ * row_start NULL: those of the last plan; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
  * and element's alignment) are the target's behind tokens[r]; tokens[r + 1] is its draft. With p = softmax(logits /
  * temperature[b]) and q the softmax of the draft's logits at the same temperature (draft_logits NULL, or a row of them
  * without a distribution: a point mass on the draft), the draft x stands where accept_u[r] q(x) < p(x). At the first row

@@ -136,11 +136,25 @@ struct PagedAttnParams {
     int spans, blocks;            // the most spans that a row block of such a call sees, the most row blocks of a request
 };
 
-constexpr int kVerifyChunk = 4096;  // logits whose statistics one workgroup takes
+constexpr int kVerifyChunk = 2048;  // logits whose statistics one wave takes
 struct alignas(16) VerifyStat {
     double sum;  // of the weights, relative to max
-    float max;   // NaN where a logit is
-    int top;     // its lowest index
+    float max;   // a logit (greedy requests: the largest); NaN where one is, or +inf
+    int top;     // greedy requests: its lowest index
+};
+// Where a request stops, and the distributions there.
+struct alignas(16) VerifyStop {
+    double p_norm, q_norm;  // 1 / the sums of the row's weights
+    float p_max, q_max;     // what they are relative to
+    int first, row;       // the request's first row, the one it stops at; row -1: the request has none
+    int draft;            // a refused draft that is a token, or -1
+    int kind;             // VS_*
+    int top;
+};
+enum VerifyStopKind {
+    VS_REFUSED = 1,  // the row's draft does not stand (else it is the last row)
+    VS_LAW = 2,      // the row has a distribution
+    VS_REST = 4,     // and so has the draft's, of a refused draft
 };
 
 struct VerifyParams {
@@ -153,7 +167,9 @@ struct VerifyParams {
     const double *accept_u, *sample_u;  // [rows], [n]
     int32_t *accepted, *next_token;     // [n]
     VerifyStat *stats;                  // [rows (twice with a draft)][chunks]
-    double *rest;                       // [rows][chunks], with a draft
+    float *picked;                      // [rows (twice with a draft)]: logits of the drafts
+    double *rest;                       // [rows][chunks], at a request's first row, with a draft
+    VerifyStop *stops;                  // [rows], at a request's first row, with a draft
 };
 
 // Rows of the last plan, or none when it was made for other bounds than the call's (a replayed graph

@@ -537,7 +537,9 @@ cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, 
     if (rows < 0 || vocab < 1) return CLLM_ERR_ARG;
     const int64_t parts = (int64_t)rows * ((vocab - 1) / kVerifyChunk + 1);
     if (2 * parts > INT32_MAX) return CLLM_ERR_CAPACITY;
-    *bytes = round_up((size_t)parts * (draft ? 2 * sizeof(VerifyStat) + sizeof(double) : sizeof(VerifyStat)));
+    const size_t n = rows;
+    *bytes = round_up(draft ? parts * (2 * sizeof(VerifyStat) + sizeof(double)) + n * (sizeof(VerifyStop) + 2 * sizeof(float))
+                            : parts * sizeof(VerifyStat) + n * sizeof(float));
     return CLLM_OK;
 }
 
@@ -595,7 +597,13 @@ cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start
     p.next_token = next_token;
     p.stats = static_cast<VerifyStat *>(workspace);
     const size_t parts = (size_t)rows * p.chunks;
-    p.rest = draft_logits && rows > 0 ? reinterpret_cast<double *>(p.stats + 2 * parts) : nullptr;
+    if (draft_logits) {
+        p.stops = reinterpret_cast<VerifyStop *>(p.stats + 2 * parts);
+        p.rest = reinterpret_cast<double *>(p.stops + rows);
+        p.picked = reinterpret_cast<float *>(p.rest + parts);
+    } else {
+        p.picked = reinterpret_cast<float *>(p.stats + parts);
+    }
     HIPCHK(c, launch_paged_verify(dtype == CLLM_DTYPE_BF16, p, c->stream));
     return CLLM_OK;
 }

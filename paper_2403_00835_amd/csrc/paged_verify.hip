@@ -6,7 +6,7 @@
 // row whose draft does not stand, the next token is drawn from max(p - q, 0); behind the last row, from p: the tokens
 // then have the target's distribution. A token is drawn as the lowest index whose running sum is above u times the sum.
 //
-// Every weight 2^((l - max) log2(e) / T) and every sum is in 64 bits: a draw among V tokens picks the neighbour with a
+// Every weight 2^((l - max) log2(e) / T) and every sum is in 64 bits: a draw among V tokens picks a neighbour with a
 // probability of about V times the sums' relative error, which in 32 bits is one in some hundred draws.
 #include <algorithm>
 
@@ -17,377 +17,551 @@ namespace cllm {
 
 namespace {
 
-constexpr int kThreads = 256, kPer = kVerifyChunk / kThreads;  // of the statistics' workgroups; logits a thread
-constexpr int kDecide = 512;                                   // threads of the workgroups that decide
+constexpr int kThreads = 256;                        // of the statistics' workgroups: a chunk a wave
+constexpr int kPart = 8 * kWave, kParts = kVerifyChunk / kPart;  // logits that a wave takes by eights, of a chunk
+constexpr int kRest = 512, kToken = 1024;           // of the two kernels that decide where a request stops: a row a wave at once
 
-// 2^(j / 32)
-__constant__ double kExpTable[32] = {
-    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
-    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
-    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
-    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
-    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
-    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
-    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+constexpr int kExpSteps = 256;
+// 2^(j / 256), by its Taylor series to z^17 / 17! (z = ln 2 j / 256: 1e-18 is left out): no load to wait for.
+__device__ __forceinline__ double exp_step(int j) {
+    const double z = 0x1.62e42fefa39efp-9 * j;
+    double y = 1.0;
+#pragma unroll
+    for (int k = 17; k >= 1; --k) y = __builtin_fma(y, z * (1.0 / k), 1.0);
+    return y;
+}
+// A barrier for what is in LDS: loads in flight are not waited for, as __syncthreads() would.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
+    barrier_no_fence();
+}
+// The table, in LDS, by the first kExpSteps threads.
+__device__ __forceinline__ void make_table(double (&table)[kExpSteps]) {
+    if (threadIdx.x < kExpSteps) table[threadIdx.x] = exp_step(threadIdx.x);
+    lds_barrier();
+}
 
-// 2^d for d <= 0 (below 2^-1000: 0): 2^(k / 32) from the table (LDS) times 2^r, |r| <= 1 / 64, by its Taylor polynomial,
-// whose first term left out is 2e-18 of it.
-__device__ __forceinline__ double exp2_wide(double d, const double *table) {
-    constexpr double kRound = 0x1.8p47;  // its last place is 1 / 32
-    const double dc = fmax(d, -1000.0), t = dc + kRound, r = dc - (t - kRound);
-    const int k = (int)__builtin_bit_cast(uint64_t, t);  // 32 dc, rounded
-    double y = 0x1.430912f86c787p-13;
-    y = __builtin_fma(y, r, 0x1.5d87fe78a6731p-10);
-    y = __builtin_fma(y, r, 0x1.3b2ab6fba4e77p-7);
-    y = __builtin_fma(y, r, 0x1.c6b08d704a0c0p-5);
+// 1 / t: the instruction's guess and two steps of Newton's.
+__device__ __forceinline__ double inverse(double t) {
+    double y = __builtin_amdgcn_rcp(t);
+    y = __builtin_fma(y, __builtin_fma(-t, y, 1.0), y);
+    return __builtin_fma(y, __builtin_fma(-t, y, 1.0), y);
+}
+
+// The weights' exponent: scale = log2(e) / T. 0: the greedy choice; -1: not a temperature.
+__device__ __forceinline__ double weight_scale(float temperature) {
+    const double y = inverse(temperature);
+    return temperature == 0.0f ? 0.0 : temperature > 0.0f && temperature < INFINITY ? 1.4426950408889634 * y : -1.0;
+}
+
+// -1000 / scale (of a temperature).
+__device__ __forceinline__ double weight_floor(float temperature) { return -693.14718055994531 * (double)temperature; }
+
+// 2^(d scale), d scale within +-1000, as f 2^r: f = 2^(k / 256) from the table (LDS) with k / 256's whole part added to its
+// exponent, 2^r, |r| <= 1 / 512, by its Taylor polynomial, whose first term left out is 2^-42 of it. The product d scale is not
+// rounded on its own.
+struct Weight {
+    double f, r2;
+};
+__device__ __forceinline__ Weight weight_parts(double d, double scale, const double *table) {
+    constexpr double kRound = 0x1.8p44;  // its last place is 1 / 256
+    const double t = __builtin_fma(d, scale, kRound), r = __builtin_fma(d, scale, kRound - t);
+    const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, t);  // 256 d scale, rounded
+    double y = 0x1.c6b08d704a0c0p-5;
+    asm("" : "+v"(y));  // (kept in registers: the product takes one constant from elsewhere)
     y = __builtin_fma(y, r, 0x1.ebfbdff82c58fp-3);
     y = __builtin_fma(y, r, 0x1.62e42fefa39efp-1);
     y = __builtin_fma(y, r, 1.0);
-    const uint64_t w = __builtin_bit_cast(uint64_t, y * table[k & 31]) + ((uint64_t)(uint32_t)(k >> 5) << 52);
-    return d < -1000.0 ? 0.0 : __builtin_bit_cast(double, w);
+    const u32x2 e = __builtin_bit_cast(u32x2, table[k & (kExpSteps - 1)]);
+    uint32_t high;
+    asm("v_lshl_add_u32 %0, %1, 12, %2" : "=v"(high) : "v"(k & ~(kExpSteps - 1u)), "v"(e[1]));  // (the compiler makes three of it)
+    return {__builtin_bit_cast(double, u32x2{e[0], high}), y};
+}
+// Below 2^-1000: about 2^-1000, which no sum that holds a weight above 2^-900 minds; floor = -1000 / scale.
+__device__ __forceinline__ double weight(double d, double scale, double floor, const double *table) {
+    const Weight w = weight_parts(fmax(d, floor), scale, table);
+    return w.f * w.r2;
+}
+// Of the logit l beside m: 0 below 2^-1000.
+__device__ __forceinline__ double weight_of(float l, float m, double scale, double floor, const double *table) {
+    const double d = (double)l - (double)m;
+    return d >= floor ? weight(d, scale, floor, table) : 0.0;
 }
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-// N logits from any element's address; past the row's end -inf.
-template <Prec PR, int N>
-__device__ __forceinline__ void load_logits(float (&x)[N], const typename PrecT<PR>::T *row, int i, int vocab) {
+// The logits i .. i + 7 of a row, at any element's address, as eight neighbours from `from` on; those of them that are before i
+// or past the row's end are -inf.
+template <Prec PR>
+struct Eight {
     using T = typename PrecT<PR>::T;
-    constexpr int VEC = PrecT<PR>::VEC;
-    static_assert(N % VEC == 0, "whole vectors");
+    static constexpr int VEC = PrecT<PR>::VEC, NV = 8 / VEC;
+    u32x4 raw[NV];  // (words, not elements: of those the compiler would make a register each)
+    int from;
+    __device__ __forceinline__ void load_whole(const T *row, int i) {
+        from = i;
 #pragma unroll
-    for (int v = 0; v < N; v += VEC) {
-        alignas(16) T e[VEC];
-        if (i + v + VEC <= vocab) {
-            *reinterpret_cast<u32x4 *>(e) = *reinterpret_cast<const u32x4_any *>(row + i + v);
+        for (int v = 0; v < NV; ++v) raw[v] = *reinterpret_cast<const u32x4_any *>(row + i + v * VEC);
+    }
+    __device__ __forceinline__ void load(const T *row, int i, int vocab) {
+        if (vocab >= 8) {
+            load_whole(row, min(i, vocab - 8));
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[v + k] = from_elem<PR>(e[k]);
+            for (int k = 0; k < 8; ++k) put(k, from + k >= i ? (*this)[k] : -INFINITY);
         } else {
+            from = i;
+            asm volatile("" : "+v"(i));  // (or the eight addresses are formed before every caller's loop)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[v + k] = i + v + k < vocab ? from_elem<PR>(row[i + v + k]) : -INFINITY;
+            for (int k = 0; k < 8; ++k) put(k, i + k < vocab ? from_elem<PR>(row[i + k]) : -INFINITY);
         }
     }
-}
+    __device__ __forceinline__ float operator[](int k) const {
+        if constexpr (PR == Prec::BF16) return __uint_as_float(k % 2 ? raw[0][k / 2] & 0xffff0000u : raw[0][k / 2] << 16);
+        return __uint_as_float(raw[k / VEC][k % VEC]);
+    }
+    __device__ __forceinline__ void put(int k, float x) {  // (a value of T)
+        uint32_t &w = reinterpret_cast<uint32_t *>(raw)[PR == Prec::BF16 ? k / 2 : k];
+        const uint32_t b = __float_as_uint(x);
+        if constexpr (PR == Prec::BF16)
+            w = k % 2 ? (w & 0xffffu) | (b & 0xffff0000u) : (w & 0xffff0000u) | b >> 16;
+        else
+            w = b;
+    }
+    // What has been made of the words is not kept beside them for later uses.
+    __device__ __forceinline__ void keep() {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) asm volatile("" : "+v"(raw[v]));
+    }
+};
 
 // The request of a row: the last one that starts at or before it (a wave's two reads; n up to 1024).
 __device__ __forceinline__ int request_of(const int32_t *row_start, int n, int row) {
     const int lane = threadIdx.x & 63;
+    if (n <= kWave) return max((int)__popcll(__ballot(lane < n && row_start[min(lane, n)] <= row)) - 1, 0);
     const uint64_t far = __ballot(16 * lane < n && row_start[min(16 * lane, n)] <= row);
     const int c = 16 * max((int)__popcll(far) - 1, 0);  // (a row before the first request is counted to that)
     const uint64_t near = __ballot(lane < 16 && c + lane < n && row_start[min(c + lane, n)] <= row);
     return min(c + max((int)__popcll(near) - 1, 0), n - 1);
 }
 
-// Weights are 2^((l - max) scale); 0: the greedy choice. Not a temperature: -1.
-__device__ __forceinline__ double weight_scale(float temperature) {
-    return temperature == 0.0f ? 0.0 : temperature > 0.0f && temperature < INFINITY ? 1.4426950408889634 / (double)temperature : -1.0;
+// Lane moves in the ALU. A step: 16 lanes by shifts, then across them; lane 63 ends with all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float x, float none) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, ROWS, 0xf, false));
 }
-
-// The larger value, of equal ones the lower index. (A NaN is kept apart.)
-__device__ __forceinline__ void take_larger(float &m, int &at, float m2, int at2) {
-    const bool other = m2 > m || (m2 == m && at2 < at);
-    m = other ? m2 : m;
-    at = other ? at2 : at;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x, double none) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x), o = __builtin_bit_cast(uint64_t, none);
+    const uint32_t lo = __builtin_amdgcn_update_dpp((int)(uint32_t)o, (int)(uint32_t)b, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp((int)(o >> 32), (int)(b >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
-
-__device__ __forceinline__ double wave_sum(double x) {
+__device__ __forceinline__ float of_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+__device__ __forceinline__ double of_lane(double x, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <class T, class F>
+__device__ __forceinline__ T wave_scan(T x, T none, F f) {  // inclusive, from lane 0 on
+    x = f(x, moved<0x111, 0xf>(x, none));
+    x = f(x, moved<0x112, 0xf>(x, none));
+    x = f(x, moved<0x114, 0xf>(x, none));
+    x = f(x, moved<0x118, 0xf>(x, none));
+    x = f(x, moved<0x142, 0xa>(x, none));
+    return f(x, moved<0x143, 0xc>(x, none));
+}
+__device__ __forceinline__ double scan_sum(double x) {
+    return wave_scan(x, 0.0, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_sum(double x) { return of_lane(scan_sum(x), 63); }
+__device__ __forceinline__ float wave_max(float x) {
+    return of_lane(wave_scan(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); }), 63);
+}
+__device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
+    for (int off = 32; off >= 1; off >>= 1) x = min(x, __shfl_xor(x, off));
     return x;
 }
 
-// Sum over the workgroup, the same in every thread, in a fixed order. s: one word a wave.
-__device__ __forceinline__ double block_sum(double x, double *s) {
-    x = wave_sum(x);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-    __syncthreads();
-    double t = 0.0;
-    for (int w = 0; w < (int)blockDim.x / kWave; ++w) t += s[w];
-    return t;
-}
-
-__device__ __forceinline__ void load_table(double *table) {
-    if (threadIdx.x < 32) table[threadIdx.x] = kExpTable[threadIdx.x];
-    __syncthreads();
-}
-
-// A row's distribution from the statistics of its chunks, by one wave: the same in every lane.
+// A row's distribution from the statistics of its chunks, by one wave.
 struct Law {
-    float max;
-    double sum;  // of the weights
-    int top;     // the largest logit's lowest index
-    bool ok;     // neither NaN nor +inf among the logits, nor all -inf
+    float max;    // what weights are relative to: the largest of its chunks' (greedy requests: the largest logit)
+    double norm;  // 1 / the sum of the weights
+    int top;      // greedy requests: the largest logit's lowest index
+    bool ok;      // neither NaN nor +inf among the logits, nor all -inf
 };
-__device__ __forceinline__ Law row_law(const VerifyStat *st, int chunks, double scale, const double *table) {
+__device__ __forceinline__ Law row_law(const VerifyStat *st, int chunks, double scale, double floor, const double *table) {
     const int lane = threadIdx.x & 63;
-    Law w{-INFINITY, 0.0, 0x7fffffff, true};
-    bool bad = false;
-    for (int c = lane; c < chunks; c += kWave) {
-        const VerifyStat s = st[c];
-        bad |= s.max != s.max;
-        take_larger(w.max, w.top, s.max, s.top);
+    constexpr VerifyStat kNone{0.0, -INFINITY, 0x7fffffff};
+    const VerifyStat mine = lane < chunks ? st[lane] : kNone;  // (the first 64 chunks: most vocabularies' all)
+    float m = mine.max;
+    bool bad = m != m;
+    for (int c = lane + kWave; c < chunks; c += kWave) {
+        const float x = st[c].max;
+        bad |= x != x;
+        m = fmaxf(m, x);
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) take_larger(w.max, w.top, __shfl_xor(w.max, off), __shfl_xor(w.top, off));
+    Law w{wave_max(m), 0.0, 0x7fffffff, false};
     w.ok = !__any(bad) && w.max > -INFINITY && w.max < INFINITY;
-    if (!w.ok || scale <= 0.0) return w;
-    double sum = 0.0;
-    for (int c = lane; c < chunks; c += kWave) {
-        const VerifyStat s = st[c];
-        sum += s.sum * exp2_wide(((double)s.max - (double)w.max) * scale, table);
+    if (!w.ok) return w;
+    if (scale > 0.0) {
+        double sum = mine.sum * weight((double)mine.max - (double)w.max, scale, floor, table);
+        for (int c = lane + kWave; c < chunks; c += kWave)
+            sum += st[c].sum * weight((double)st[c].max - (double)w.max, scale, floor, table);
+        w.norm = inverse(wave_sum(sum));
+    } else {
+        int top = mine.max == w.max ? mine.top : 0x7fffffff;
+        for (int c = lane + kWave; c < chunks; c += kWave)
+            if (st[c].max == w.max) top = min(top, st[c].top);
+        w.top = wave_min(top);
     }
-    w.sum = wave_sum(sum);
     return w;
 }
 
-// Where a request stops: its row, and whether that row's draft was refused.
-struct Stop {
-    int first, last;  // its rows
-    int row;
-    bool refused;
-    int draft;        // the refused token where it is one of the vocabulary, or -1
-    double scale;
-    Law p, q;         // of the row; q with draft logits and a refused draft
+// A request: its rows (first >= end: none, or not within the call's), and its temperature.
+struct Request {
+    int first, end;
+    double scale, floor;
 };
-
-// By the whole workgroup. False where the request has no rows.
-template <Prec PR>
-__device__ __forceinline__ bool decide(const VerifyParams &p, int b, const double *table, int *s_stop, Stop &d) {
-    using T = typename PrecT<PR>::T;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / kWave;
-    int first = p.row_start[b], end = p.row_start[b + 1];
-    if (p.status && (p.status[PS_ROWS] == 0 || b >= p.status[PS_ENTRIES])) first = end = 0;  // a refused plan
-    if (first < 0 || end > p.rows || first >= end) return false;  // uniform
-    d.first = first;
-    d.last = end - 1;
-    d.scale = weight_scale(p.temperature[b]);
-    const int chunks = p.chunks;
-    if (threadIdx.x == 0) *s_stop = end - 1;
-    __syncthreads();
-    for (int r0 = first; r0 < end - 1; r0 += waves) {
-        const int r = r0 + w;
-        if (r < end - 1) {
-            const int x = p.tokens[r + 1];
-            const bool known = x >= 0 && x < p.vocab;
-            const double u = p.accept_u[r];
-            const float lp = known ? from_elem<PR>(((const T *)p.logits)[(size_t)r * p.stride + x]) : -INFINITY;
-            const float lq = known && p.draft ? from_elem<PR>(((const T *)p.draft)[(size_t)r * p.draft_stride + x]) : 0.f;
-            const Law law = row_law(p.stats + (size_t)r * chunks, chunks, d.scale, table);
-            bool stands = false;
-            if (law.ok && d.scale == 0.0) {
-                stands = x == law.top;
-            } else if (law.ok && d.scale > 0.0 && known) {
-                const double px = exp2_wide(((double)lp - (double)law.max) * d.scale, table) / law.sum;
-                double qx = 1.0;
-                if (p.draft) {
-                    const Law lawq = row_law(p.stats + (size_t)(p.rows + r) * chunks, chunks, d.scale, table);
-                    qx = lawq.ok ? exp2_wide(((double)lq - (double)lawq.max) * d.scale, table) / lawq.sum : 1.0;
-                }
-                stands = u * qx < px;
-            }
-            if (!stands && (threadIdx.x & 63) == 0) atomicMin(s_stop, r);
-        }
-        __syncthreads();
-        if (*s_stop < r0 + waves) break;  // uniform
-    }
-    __syncthreads();
-    d.row = __builtin_amdgcn_readfirstlane(*s_stop);
-    d.refused = d.row < d.last;
-    d.p = row_law(p.stats + (size_t)d.row * chunks, chunks, d.scale, table);
-    d.q = Law{0.f, 0.0, 0, false};
-    d.draft = -1;
-    if (d.refused) {
-        const int x = p.tokens[d.row + 1];
-        d.draft = x >= 0 && x < p.vocab ? x : -1;
-        if (p.draft) d.q = row_law(p.stats + (size_t)(p.rows + d.row) * chunks, chunks, d.scale, table);
-    }
-    return true;
+// The request of a workgroup, and the table; what they read is on its way at once.
+__device__ __forceinline__ Request begin(const VerifyParams &p, int b, double (&table)[kExpSteps]) {
+    const float temperature = p.temperature[b];
+    Request q;
+    q.first = p.row_start[b];
+    q.end = p.row_start[b + 1];
+    if (p.status && (p.status[PS_ROWS] == 0 || b >= p.status[PS_ENTRIES])) q.end = q.first;  // a refused plan
+    if (q.first < 0 || q.end > p.rows) q.end = q.first;
+    q.scale = weight_scale(temperature);
+    q.floor = weight_floor(temperature);
+    make_table(table);
+    return q;
 }
 
-// The weights of N neighbouring tokens: p's (but for `without`), or max(p - q, 0) where the draft's are given.
-template <Prec PR, int N>
-__device__ __forceinline__ void row_weights(const VerifyParams &p, const Stop &d, bool rest, int without, int i, const double *table,
-                                            double (&w)[N]) {
-    using T = typename PrecT<PR>::T;
-    float x[N];
-    load_logits<PR>(x, (const T *)p.logits + (size_t)d.row * p.stride, i, p.vocab);
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        w[k] = exp2_wide(((double)x[k] - (double)d.p.max) * d.scale, table);
-        if (i + k == without) w[k] = 0.0;
+struct Decide {  // LDS
+    VerifyStop at[kToken / kWave];
+    int stop;
+};
+
+// Where a request stops, by the whole workgroup: a row a wave.
+__device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Request &q, const double *table, Decide &s) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / kWave, first = q.first, end = q.end;
+    const double scale = q.scale, floor = q.floor;
+    if (first >= end) {  // uniform
+        VerifyStop none{};
+        none.row = -1;
+        return none;
     }
-    if (rest) {
-        load_logits<PR>(x, (const T *)p.draft + (size_t)d.row * p.draft_stride, i, p.vocab);
-        const double ip = 1.0 / d.p.sum, iq = 1.0 / d.q.sum;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-#pragma clang fp contract(off)  // the same p and q leave exactly nothing: both products are rounded
-            const double pk = w[k] * ip, qk = exp2_wide(((double)x[k] - (double)d.q.max) * d.scale, table) * iq;
-            w[k] = fmax(pk - qk, 0.0);
+    if (threadIdx.x == 0) s.stop = end;
+    __syncthreads();
+    for (int r0 = first; r0 < end; r0 += waves) {
+        const int r = r0 + w;
+        if (r < end) {
+            const bool drafted = r + 1 < end;
+            const VerifyStat *st = p.stats + (size_t)r * p.chunks, *sq = p.stats + (size_t)(p.rows + r) * p.chunks;
+            const int x = drafted ? p.tokens[r + 1] : -1;
+            const bool known = x >= 0 && x < p.vocab;
+            const double u = drafted ? p.accept_u[r] : 0.0;
+            const float lp = p.picked[r], lq = p.draft ? p.picked[p.rows + r] : 0.f;  // the draft's, where it is a token
+            const Law law = row_law(st, p.chunks, scale, floor, table);
+            Law lawq{0.f, 0.0, 0, false};
+            if (p.draft && drafted && scale > 0.0) lawq = row_law(sq, p.chunks, scale, floor, table);
+            bool stands = false;
+            if (law.ok && drafted && known) {
+                if (scale == 0.0) {
+                    stands = x == law.top;
+                } else if (scale > 0.0) {
+                    const double px = weight_of(lp, law.max, scale, floor, table) * law.norm;
+                    const double qx = lawq.ok ? weight_of(lq, lawq.max, scale, floor, table) * lawq.norm : 1.0;
+                    stands = u * qx < px;
+                }
+            }
+            if (!stands && (threadIdx.x & 63) == 0) {
+                VerifyStop &at = s.at[w];
+                at.p_norm = law.norm;
+                at.q_norm = lawq.norm;
+                at.p_max = law.max;
+                at.q_max = lawq.max;
+                at.first = first;
+                at.row = r;
+                at.draft = known ? x : -1;
+                at.kind = (drafted ? VS_REFUSED : 0) | (law.ok && scale >= 0.0 ? VS_LAW : 0) | (law.ok && lawq.ok ? VS_REST : 0);
+                at.top = law.top;
+                atomicMin(&s.stop, r);
+            }
         }
+        __syncthreads();
+        if (s.stop < r0 + waves) return s.at[s.stop - r0];  // uniform: the last row at the latest
+    }
+    return VerifyStop{};  // (not reached)
+}
+
+// max(p - q, 0) of a token of logits l and lq.
+__device__ __forceinline__ double left_weight(float l, float lq, const VerifyStop &at, const Request &q, const double *table) {
+#pragma clang fp contract(off)  // the same p and q leave exactly nothing: both products are rounded
+    const double px = weight_of(l, at.p_max, q.scale, q.floor, table) * at.p_norm;
+    const double qx = weight_of(lq, at.q_max, q.scale, q.floor, table) * at.q_norm;
+    return fmax(px - qx, 0.0);
+}
+
+// The weights of N neighbouring tokens: p's (but for `without`), or max(p - q, 0).
+template <Prec PR, int N>
+__device__ __forceinline__ void row_weights(const VerifyParams &p, const VerifyStop &at, bool rest, int without, int i, const Request &q,
+                                            const double *table, double (&w)[N]) {
+    using T = typename PrecT<PR>::T;
+    const T *row = (const T *)p.logits + (size_t)at.row * p.stride, *drow = (const T *)p.draft + (size_t)at.row * p.draft_stride;
+    float x[N], y[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = i + k < p.vocab ? from_elem<PR>(row[i + k]) : -INFINITY;
+    if (rest) {  // uniform
+#pragma unroll
+        for (int k = 0; k < N; ++k) y[k] = i + k < p.vocab ? from_elem<PR>(drow[i + k]) : -INFINITY;
+#pragma unroll
+        for (int k = 0; k < N; ++k) w[k] = left_weight(x[k], y[k], at, q, table);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) w[k] = i + k == without ? 0.0 : weight_of(x[k], at.p_max, q.scale, q.floor, table);
     }
 }
 
 }  // namespace
 
-// Largest logit, its lowest index and the sum of weights relative to it, of chunks of 4096 logits of the target's rows and then of
-// the draft's. Workgroup: a chunk; its logits stay in registers between the two passes over them.
+// The sum of weights of chunks of 2048 logits of the target's rows and then of the draft's, and the logit that they are relative
+// to: 0 where 64 bits hold every weight, which saves a difference and a bound for each (such chunks are most), or the largest
+// one. Of greedy requests the largest logit and its index instead. A chunk a wave, its logits in registers as they came, which
+// leaves room for eight waves a SIMD.
 template <Prec PR>
-__global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p) {
+__global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, int row0) {
     using T = typename PrecT<PR>::T;
-    constexpr int VEC = PrecT<PR>::VEC;
-    __shared__ double s_sum[kThreads / kWave], table[32];
-    __shared__ float s_max[kThreads / kWave];
-    __shared__ int s_top[kThreads / kWave], s_bad[kThreads / kWave];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int work = p.rows * p.chunks * (p.draft ? 2 : 1);
-    load_table(table);
-    for (int idx = blockIdx.x; idx < work; idx += gridDim.x) {
-        const int all = idx / p.chunks, chunk = idx - all * p.chunks;
-        const bool isq = all >= p.rows;
-        const int r = isq ? all - p.rows : all;
-        const T *row = isq ? (const T *)p.draft + (size_t)r * p.draft_stride : (const T *)p.logits + (size_t)r * p.stride;
-        const int b = request_of(p.row_start, p.n, r);
-        if (isq && r + 1 >= p.row_start[b + 1]) continue;  // uniform: no draft behind the request's last row
-        const double scale = weight_scale(p.temperature[b]);
-        float x[kPer];
+    static_assert(kExpSteps <= kThreads, "a thread an entry");
+    __shared__ double table[kExpSteps];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int chunk = blockIdx.x * (kThreads / kWave) + w, all = row0 + blockIdx.y;  // the target's rows, then the draft's
+    const bool isq = all >= p.rows;
+    const int r = isq ? all - p.rows : all;
+    const T *row = isq ? (const T *)p.draft + (size_t)r * p.draft_stride : (const T *)p.logits + (size_t)r * p.stride;
+    const int first = chunk * kVerifyChunk + lane * 8;
+    const bool whole = (chunk + 1) * kVerifyChunk <= p.vocab;  // uniform
+    const int draft = r + 1 < p.rows ? p.tokens[r + 1] : -1;
+    int b = 0;
+    bool live = chunk < p.chunks;  // uniform over the wave
+    if (isq) {
+        b = request_of(p.row_start, p.n, r);
+        live = live && r + 1 < p.row_start[b + 1];  // no draft behind the request's last row
+    }
+    Eight<PR> x[kParts];
+    if (live && whole) {
 #pragma unroll
-        for (int i = 0; i < kPer; i += VEC) {
-            float part[VEC];
-            load_logits<PR>(part, row, chunk * kVerifyChunk + (i / VEC * kThreads + tid) * VEC, p.vocab);
+        for (int v = 0; v < kParts; ++v) x[v].load_whole(row, first + v * kPart);
+    } else if (live) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[i + k] = part[k];
+        for (int v = 0; v < kParts; ++v) x[v].load(row, first + v * kPart, p.vocab);
+    }
+    make_table(table);
+    if (!live) return;
+    if (!isq) b = request_of(p.row_start, p.n, r);
+    const float temperature = p.temperature[b];
+    const double scale = weight_scale(temperature), floor = weight_floor(temperature);
+    float m = -INFINITY, size = 0.0f;
+    bool bad = false;
+#pragma unroll
+    for (int v = 0; v < kParts; ++v) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            const float a = x[v][k], c = x[v][k + 1];
+            m = fmaxf(fmaxf(m, a), c);
+            size = fmaxf(fmaxf(size, fabsf(a)), fabsf(c));
+            bad |= __builtin_isunordered(a, c);
         }
-        float m = -INFINITY;
-        int top = 0x7fffffff;
-        bool bad = false;
+        x[v].keep();
+    }
+    double sum = 0.0;
+    float ref = 0.0f;
+    int top = 0x7fffffff;
+    if (scale > 0.0 && __all((double)size <= -0.9 * floor)) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int at = chunk * kVerifyChunk + (i / VEC * kThreads + tid) * VEC + i % VEC;
-            bad |= x[i] != x[i];
-            if (x[i] > m) m = x[i], top = at;
+        for (int v = 0; v < kParts; ++v)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const Weight z = weight_parts((double)x[v][k], scale, table);
+                sum = __builtin_fma(z.f, z.r2, sum);
+                if (k % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (more at once take the registers of other waves)
+            }
+        sum = wave_sum(sum);
+    } else {
+        ref = wave_max(m);
+        if (ref > -INFINITY && ref < INFINITY) {  // else there is nothing, or no distribution
+#pragma unroll
+            for (int v = kParts - 1; v >= 0; --v)
+#pragma unroll
+                for (int k = 7; k >= 0; --k) {
+                    if (scale > 0.0)
+                        sum += weight((double)x[v][k] - (double)ref, scale, floor, table);
+                    else if (x[v][k] == ref)
+                        top = x[v].from + k;
+                    if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                }
+            if (scale > 0.0)
+                sum = wave_sum(sum);
+            else
+                top = wave_min(top);
         }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) take_larger(m, top, __shfl_xor(m, off), __shfl_xor(top, off));
-        bad = __any(bad);
-        __syncthreads();  // the chunk before has been read
-        if (lane == 0) s_max[w] = m, s_top[w] = top, s_bad[w] = bad;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kThreads / kWave; ++i) {
-            take_larger(m, top, s_max[i], s_top[i]);
-            bad |= s_bad[i] != 0;
-        }
-        double sum = 0.0;
-        if (scale > 0.0 && m > -INFINITY && m < INFINITY) {  // uniform
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) sum += exp2_wide(((double)x[i] - (double)m) * scale, table);
-            sum = block_sum(sum, s_sum);
-        }
-        if (tid == 0) p.stats[(size_t)all * p.chunks + chunk] = VerifyStat{sum, bad ? NAN : m, top};
+    }
+    const bool none = __any(bad) || ref == INFINITY;
+    if (lane == 0) {
+        p.stats[(size_t)all * p.chunks + chunk] = VerifyStat{sum, none ? NAN : ref, top};
+        if (draft >= chunk * kVerifyChunk && draft < min((chunk + 1) * kVerifyChunk, p.vocab)) p.picked[all] = from_elem<PR>(row[draft]);
     }
 }
 
-// Sums of max(p - q, 0) over the chunks of the rows whose draft was refused.
+// Where the requests stop, and the sums of max(p - q, 0) over the chunks of the rows whose draft was refused: two chunks a
+// workgroup, each of which decides for itself.
+constexpr int kRestChunks = kRest / kWave / kParts;
 template <Prec PR>
-__global__ __launch_bounds__(kDecide) void verify_rest_kernel(VerifyParams p) {
-    __shared__ double s_sum[kDecide / kWave], table[32];
-    __shared__ int s_stop;
-    constexpr int N = kVerifyChunk / kDecide;
-    load_table(table);
-    const int b = blockIdx.y;
-    Stop d;
-    if (!decide<PR>(p, b, table, &s_stop, d) || !d.refused || !d.p.ok || !d.q.ok || !(d.scale > 0.0)) return;
-    for (int chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
-        double w[N], sum = 0.0;
-        row_weights<PR>(p, d, true, -1, chunk * kVerifyChunk + (int)threadIdx.x * N, table, w);
+__global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
+    using T = typename PrecT<PR>::T;
+    __shared__ double table[kExpSteps], s_sum[kRest / kWave];
+    __shared__ Decide s_decide;
+    const int b = blockIdx.y, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Request q = begin(p, b, table);
+    const VerifyStop at = decide(p, q, table, s_decide);
+    if (at.row < 0) return;  // uniform
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.stops[at.first] = at;
+    if (!(at.kind & VS_REST)) return;
+    const T *row = (const T *)p.logits + (size_t)at.row * p.stride, *drow = (const T *)p.draft + (size_t)at.row * p.draft_stride;
+    Eight<PR> x, y, xn, yn;
+    auto load = [&](int c0) {
+        const int i = c0 * kVerifyChunk + w * kPart + lane * 8;  // (a chunk is kParts waves')
+        const bool whole = (c0 + kRestChunks) * kVerifyChunk <= p.vocab;  // uniform
+        if (whole) {
+            xn.load_whole(row, i);
+            yn.load_whole(drow, i);
+        } else {
+            xn.load(row, i, p.vocab);
+            yn.load(drow, i, p.vocab);
+        }
+    };
+    load(blockIdx.x * kRestChunks);
+#pragma unroll 1
+    for (int c0 = blockIdx.x * kRestChunks; c0 < p.chunks; c0 += gridDim.x * kRestChunks) {
+        x = xn;
+        y = yn;
+        if (c0 + (int)gridDim.x * kRestChunks < p.chunks) load(c0 + gridDim.x * kRestChunks);
+        double sum = 0.0;
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum += w[k];
-        sum = block_sum(sum, s_sum);
-        if (threadIdx.x == 0) p.rest[(size_t)d.row * p.chunks + chunk] = sum;
+        for (int k = 0; k < 8; ++k) sum += left_weight(x[k], y[k], at, q, table);
+        sum = wave_sum(sum);
+        __syncthreads();
+        if (lane == 0) s_sum[w] = sum;
+        __syncthreads();
+        const int chunk = c0 + (int)threadIdx.x;
+        if (threadIdx.x < kRestChunks && chunk < p.chunks) {
+            double t = 0.0;
+#pragma unroll
+            for (int v = 0; v < kParts; ++v) t += s_sum[threadIdx.x * kParts + v];
+            p.rest[(size_t)at.first * p.chunks + chunk] = t;
+        }
     }
 }
 
 // The accepted rows and the next token. Workgroup: a request.
 template <Prec PR>
-__global__ __launch_bounds__(kDecide) void verify_token_kernel(VerifyParams p) {
-    __shared__ double s_sum[kDecide / kWave], table[32], s_before;
-    __shared__ int s_stop, s_from, s_chunk, s_token, s_last;
-    constexpr int N = kVerifyChunk / kDecide;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    load_table(table);
-    Stop d;
-    const bool any = decide<PR>(p, b, table, &s_stop, d);
-    const bool law = any && d.p.ok && d.scale >= 0.0;
-    if (tid == 0) p.accepted[b] = any ? d.row - d.first + 1 : 0;
-    if (!law || d.scale == 0.0) {  // uniform
-        if (tid == 0) p.next_token[b] = law ? d.p.top : -1;
+__global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
+    constexpr int N = 4, kDraw = kVerifyChunk / N;  // neighbouring tokens of a thread, threads that a chunk takes
+    static_assert(kDraw <= kToken && kDraw % kWave == 0, "whole waves");
+    __shared__ double table[kExpSteps], s_sum[kDraw / kWave], s_aim;
+    __shared__ Decide s_decide;
+    __shared__ int s_from, s_chunk, s_token, s_last;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const double u = p.sample_u[b];
+    const Request q = begin(p, b, table);
+    const double scale = q.scale, floor = q.floor;
+    VerifyStop at{};
+    at.row = -1;
+    if (!p.draft)
+        at = decide(p, q, table, s_decide);
+    else if (q.first < q.end)
+        at = p.stops[q.first];  // decided with the rest's sums
+    const bool law = at.row >= 0 && (at.kind & VS_LAW);
+    if (tid == 0) p.accepted[b] = at.row >= 0 ? at.row - at.first + 1 : 0;
+    if (!law || scale == 0.0) {  // uniform
+        if (tid == 0) p.next_token[b] = law ? at.top : -1;
         return;
     }
-    // What is drawn from: the chunks' sums of p, of p without the refused token, or of the rest. (Where that is empty, p.)
-    bool rest = d.refused && d.q.ok;
-    const bool point = d.refused && !rest && d.draft >= 0;
-    int without = point ? d.draft : -1;
+    // What is drawn from: the rest, p without the refused token, or p (also where those are empty).
+    bool rest = at.kind & VS_REST;
+    int without = !rest && (at.kind & VS_REFUSED) ? at.draft : -1;
+    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks;
     double cut = 0.0;  // the sum of the refused token's chunk without it
-    if (point) {
-        double x[N], sum = 0.0;
-        row_weights<PR>(p, d, false, without, without / kVerifyChunk * kVerifyChunk + tid * N, table, x);
+    if (without >= 0) {
+        const int c = without / kVerifyChunk;
+        const VerifyStat s = st[c];
+        const float l = from_elem<PR>(((const typename PrecT<PR>::T *)p.logits)[(size_t)at.row * p.stride + without]);
+        const double f = weight((double)s.max - (double)at.p_max, scale, floor, table);
+        const double mine = s.max > -INFINITY ? weight_of(l, s.max, scale, floor, table) : 0.0;
+        cut = (s.sum - mine) * f;
+        if (mine * 256.0 > s.sum * 255.0) {  // uniform: little is left, of which the difference loses digits
+            double x[N], sum = 0.0;
+            if (tid < kDraw) {
+                row_weights<PR>(p, at, false, without, c * kVerifyChunk + tid * N, q, table, x);
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum += x[k];
-        cut = block_sum(sum, s_sum);
+                for (int k = 0; k < N; ++k) sum += x[k];
+                sum = wave_sum(sum);
+                if (lane == 0) s_sum[w] = sum;
+            }
+            __syncthreads();
+            cut = 0.0;
+#pragma unroll
+            for (int v = 0; v < kDraw / kWave; ++v) cut += s_sum[v];
+        }
     }
-    const VerifyStat *st = p.stats + (size_t)d.row * p.chunks;
     auto chunk_sum = [&](int c) {
-        if (rest) return p.rest[(size_t)d.row * p.chunks + c];
+        if (c >= p.chunks) return 0.0;
+        if (rest) return p.rest[(size_t)q.first * p.chunks + c];
         if (without >= 0 && c == without / kVerifyChunk) return cut;
-        return st[c].sum * exp2_wide(((double)st[c].max - (double)d.p.max) * d.scale, table);
+        const VerifyStat s = st[c];
+        return s.sum * weight((double)s.max - (double)at.p_max, scale, floor, table);  // (an empty chunk's sum is 0)
     };
     if (w == 0) {  // one wave: the chunk in which the running sum passes the number
+        double first, t;  // this lane's first chunk, the sum
         auto total = [&]() {
-            double t = 0.0;
-            for (int c = lane; c < p.chunks; c += kWave) t += chunk_sum(c);
-            return wave_sum(t);
+            first = chunk_sum(lane);
+            double x = first;
+            for (int c = lane + kWave; c < p.chunks; c += kWave) x += chunk_sum(c);
+            t = wave_sum(x);
         };
-        double t = total();
+        total();
         if (!(t > 0.0)) {
             rest = false;
             without = -1;
-            t = total();
+            total();
         }
-        const double u = p.sample_u[b], aim = (u > 0.0 ? fmin(u, 0x1.fffffffffffffp-1) : 0.0) * t;
-        double before = 0.0, at_before = 0.0;
-        int chunk = -1, last = -1;  // the chunk, and the last one that is not empty
-        double last_before = 0.0;
+        const double aim = (u > 0.0 ? fmin(u, 0x1.fffffffffffffp-1) : 0.0) * t;
+        double before = 0.0, base = 0.0, last_base = 0.0;
+        int chunk = -1, last = 0;  // the chunk, and the last one that is not empty
         for (int c0 = 0; c0 < p.chunks && chunk < 0; c0 += kWave) {
-            const double x = c0 + lane < p.chunks ? chunk_sum(c0 + lane) : 0.0;
-            double run = x;
-#pragma unroll
-            for (int off = 1; off < kWave; off <<= 1) {
-                const double y = __shfl_up(run, off);
-                if (lane >= off) run += y;
-            }
+            const double x = c0 == 0 ? first : chunk_sum(c0 + lane), run = scan_sum(x);
             const uint64_t past = __ballot(before + run > aim && x > 0.0), some = __ballot(x > 0.0);
-            if (past) {
-                const int l = __ffsll((unsigned long long)past) - 1;
-                chunk = c0 + l;
-                at_before = l > 0 ? before + __shfl(run, max(l - 1, 0)) : before;
-            }
             if (some) {
                 const int l = 63 - __clzll((long long)some);
                 last = c0 + l;
-                last_before = l > 0 ? before + __shfl(run, max(l - 1, 0)) : before;
+                last_base = l > 0 ? before + of_lane(run, max(l - 1, 0)) : before;
             }
-            before += __shfl(run, 63);
+            if (past) {
+                const int l = __ffsll((unsigned long long)past) - 1;
+                chunk = c0 + l;
+                base = l > 0 ? before + of_lane(run, max(l - 1, 0)) : before;
+            }
+            before += of_lane(run, 63);
         }
         if (chunk < 0) {  // rounding: behind the last sum
             chunk = last;
-            at_before = last_before;
+            base = last_base;
         }
         if (lane == 0) {
             s_chunk = chunk;
-            s_before = aim - at_before;
+            s_aim = aim - base;
             s_token = 0x7fffffff;
             s_last = -1;
             s_from = rest ? 2 : without >= 0 ? 1 : 0;
@@ -396,24 +570,18 @@ __global__ __launch_bounds__(kDecide) void verify_token_kernel(VerifyParams p) {
     __syncthreads();
     rest = s_from == 2;
     if (s_from == 0) without = -1;
-    const int chunk = max(s_chunk, 0);
-    const double aim = s_before;
-    double x[N], run = 0.0;
-    const int i = chunk * kVerifyChunk + tid * N;
-    row_weights<PR>(p, d, rest, without, i, table, x);
+    const double aim = s_aim;
+    const int i = s_chunk * kVerifyChunk + tid * N;
+    double x[N] = {}, run = 0.0;
+    if (tid < kDraw) row_weights<PR>(p, at, rest, without, i, q, table, x);  // whole waves
 #pragma unroll
     for (int k = 0; k < N; ++k) run += x[k];
-    // sums of the threads before this one
-    double before = run;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const double y = __shfl_up(before, off);
-        if (lane >= off) before += y;
-    }
-    if (lane == 63) s_sum[w] = before;
+    const double upto = scan_sum(run);
+    if (tid < kDraw && lane == 63) s_sum[w] = upto;
     __syncthreads();
-    double base = before - run;
-    for (int v = 0; v < w; ++v) base += s_sum[v];
+    double base = upto - run;  // the sum before this thread's tokens
+#pragma unroll
+    for (int v = 0; v < kDraw / kWave; ++v) base += v < w ? s_sum[v] : 0.0;
     int found = 0x7fffffff, last = -1;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -434,19 +602,23 @@ namespace {
 template <Prec PR>
 hipError_t launch_verify(const VerifyParams &p, hipStream_t s) {
     if (p.rows > 0) {
-        const int64_t work = (int64_t)p.rows * p.chunks * (p.draft ? 2 : 1);
-        hipLaunchKernelGGL(verify_stats_kernel<PR>, dim3((unsigned)std::min<int64_t>(work, 1 << 20)), dim3(kThreads), 0, s, p);
-        if (p.draft)
-            hipLaunchKernelGGL(verify_rest_kernel<PR>, dim3((unsigned)std::min(p.chunks, 1024), (unsigned)p.n), dim3(kDecide), 0, s, p);
+        const int per = kThreads / kWave, rows = p.rows * (p.draft ? 2 : 1), most = 1 << 15;
+        for (int r = 0; r < rows; r += most)
+            hipLaunchKernelGGL(verify_stats_kernel<PR>, dim3((unsigned)((p.chunks + per - 1) / per), (unsigned)std::min(rows - r, most)),
+                               dim3(kThreads), 0, s, p, r);
+        if (p.draft)  // (about as many workgroups as run at once: each decides first)
+            hipLaunchKernelGGL(verify_rest_kernel<PR>,
+                               dim3((unsigned)std::min((p.chunks + kRestChunks - 1) / kRestChunks, std::max(2 * kCUs / p.n, 1)), (unsigned)p.n),
+                               dim3(kRest), 0, s, p);
     }
-    hipLaunchKernelGGL(verify_token_kernel<PR>, dim3((unsigned)p.n), dim3(kDecide), 0, s, p);
+    hipLaunchKernelGGL(verify_token_kernel<PR>, dim3((unsigned)p.n), dim3(kToken), 0, s, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_paged_verify(bool bf16, const VerifyParams &p, hipStream_t s) {
-    if (p.n < 1 || p.n > kPagedMaxSeqs || p.rows < 0 || p.vocab < 1 || p.chunks != (p.vocab + kVerifyChunk - 1) / kVerifyChunk ||
+    if (p.n < 1 || p.n > kPagedMaxSeqs || p.rows < 0 || p.vocab < 1 || p.chunks != (p.vocab - 1) / kVerifyChunk + 1 ||
         (int64_t)p.rows * p.chunks * 2 > INT32_MAX)
         return hipErrorInvalidValue;
     return bf16 ? launch_verify<Prec::BF16>(p, s) : launch_verify<Prec::F32>(p, s);

@@ -38,9 +38,11 @@ def test_draws_cut_the_unit_interval():
 
 @pytest.mark.parametrize("rows,vocab,draft", [(0, 5, 0), (1, 1, 0), (7, 4096, 1), (7, 4097, 0), (300, 131072, 1)])
 def test_workspace_bytes(rows, vocab, draft):
-    n = binding.PagedCache.verify_workspace_bytes(rows, vocab, draft)
-    parts = rows * -(-vocab // 4096)
-    assert n % 256 == 0 and parts * (40 if draft else 16) <= n < parts * (40 if draft else 16) + 256
+    size = binding.PagedCache.verify_workspace_bytes
+    n = size(rows, vocab, draft)
+    assert n % 256 == 0 and n >= (16 * rows if vocab > 0 else 0) and size(rows, vocab, 0) <= size(rows, vocab, 1)
+    assert size(rows + 300, vocab, draft) > n and size(rows + 1, 100 * vocab, draft) >= n  # it follows rows and vocabulary
+    assert n <= 64 * rows * (2 + vocab // 1024) + 256  # and is a small part of the logits
 
 
 def test_bad_sizes_are_refused():
