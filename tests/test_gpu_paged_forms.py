@@ -71,7 +71,11 @@ FORMS = [  # dtype, heads, kv heads, head dim, page, contexts, new tokens, rotar
     ("f32", 1, 1, 16, 16, [0], [1], dict(layout="half", dim=10), (True, True)),
     ("f32", 2, 1, 32, 16, [2**20 - 5], [5], dict(layout="half", scaling="linear", factor=16.0), (True, True)),
     ("f32", 7, 7, 64, 16, [40], [11], dict(layout="half", dim=44, freqs=[0.01 * (j + 1) for j in range(22)]), (False, True)),
-    ("f32", 40, 10, 64, 64, [3, 900], [500, 131], dict(layout="half"), (True, True))]
+    ("f32", 40, 10, 64, 64, [3, 900], [500, 131], dict(layout="half"), (True, True)),
+    # several rows a workgroup, the last one of fewer; two heads a thread, the last one of one
+    ("f32", 32, 8, 64, 64, [0, 10], [4000, 101], dict(layout="half", dim=48), (True, True)),
+    ("bf16", 7, 3, 64, 64, [40, 0], [200, 101], dict(layout="half", dim=48), (True, True)),
+    ("bf16", 5, 5, 128, 64, [40, 0], [300, 1], dict(layout="interleaved", dim=100), (True, False))]
 
 
 @pytest.mark.parametrize("case", FORMS, ids=range(len(FORMS)))
