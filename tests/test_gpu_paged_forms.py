@@ -74,7 +74,7 @@ FORMS = [  # dtype, heads, kv heads, head dim, page, contexts, new tokens, rotar
     ("f32", 40, 10, 64, 64, [3, 900], [500, 131], dict(layout="half"), (True, True)),
     # several rows a workgroup, the last one of fewer; two heads a thread, the last one of one
     ("f32", 32, 8, 64, 64, [0, 10], [4000, 101], dict(layout="half", dim=48), (True, True)),
-    ("bf16", 7, 3, 64, 64, [40, 0], [200, 101], dict(layout="half", dim=48), (True, True)),
+    ("bf16", 9, 3, 64, 64, [40, 0], [200, 101], dict(layout="half", dim=48), (True, True)),
     ("bf16", 5, 5, 128, 64, [40, 0], [300, 1], dict(layout="interleaved", dim=100), (True, False))]
 
 
