@@ -320,7 +320,8 @@ __device__ __forceinline__ bool next_request(const PagedAttnParams &p, int i, in
     if constexpr (!WIN) return next_unit<false>(p, i, cap, u, count);
     PagedEntry e;
     const bool more = next_entry(p, i, e, count);
-    u = PagedUnit{e.slot, e.ctx, e.m, e.r0, 0, e.kind == PE_WHOLE ? -1 : 0, kAllSpans, -1};
+    const bool mine = e.kind == PE_WHOLE || (p.all_whole && e.m > 0);
+    u = PagedUnit{e.slot, e.ctx, e.m, e.r0, 0, mine ? -1 : 0, kAllSpans, -1};
     return more;
 }
 
@@ -1194,20 +1195,29 @@ struct WindowCall {
     bool whole;
     int64_t tiles;
     bool join;
+    hipError_t launch_requests(const PagedAttnParams &p, hipStream_t s) const {
+        hipLaunchKernelGGL((paged_request_kernel<HD, true>), dim3((unsigned)std::min(n * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
+                           4 * Tile<HD>::BYTES, s, p, 0);
+        return hipGetLastError();
+    }
     hipError_t operator()(const PagedAttnParams &call, hipStream_t s) const {
         constexpr int ROWS = 16 * RG;
         PagedAttnParams p = call;
+        if constexpr (P == Prec::BF16) {
+            // Blocks of up to kPagedFewRows rows on enough workgroups: all are taken whole, whatever the plan made of them (one
+            // far longer context, for which it would split them, is no longer than the others behind a window), and there is
+            // nothing else to launch. 16 of 32 rows at 800 to 4000 keys behind 1024 (32 heads of 128): 80.0 us with a span
+            // kernel and a join that find nothing to do, 67.7 without.
+            p.all_whole = most > kPagedWaveRows && most <= kPagedFewRows && n * p.n_kv >= kPagedTileGroups;
+            if (p.all_whole) return launch_requests(p, s);
+        }
         p.blocks = (int)((std::min<int64_t>(most, P == Prec::BF16 ? kPagedFewRows : most) + ROWS - 1) / ROWS);
         const dim3 grid((unsigned)std::min(p.blocks * p.n_kv, 1 << 20), (unsigned)p.spans, (unsigned)n);
         hipLaunchKernelGGL((paged_span_kernel<P, HD, RG, true>), grid, dim3(kSpanChunks * kWave),
                            kSpanChunks * (span_wave_lds<P, HD, RG>()), s, p, 0);
         hipError_t e = hipGetLastError();
         if constexpr (P == Prec::BF16) {
-            if (e == hipSuccess && whole) {
-                hipLaunchKernelGGL((paged_request_kernel<HD, true>), dim3((unsigned)std::min(n * p.n_kv, 16 * kCUs)), dim3(4 * kWave),
-                                   4 * Tile<HD>::BYTES, s, p, 0);
-                e = hipGetLastError();
-            }
+            if (e == hipSuccess && whole) e = launch_requests(p, s);
             if (e == hipSuccess && tiles > 0) e = launch_tiles<HD, true>(tiles, p, s);
         }
         return e == hipSuccess && join ? launch_join<P, HD, true>((int64_t)n * p.blocks, tiles, p, s) : e;
