@@ -475,7 +475,7 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
 
 /* The rows of the last plan into the pages of one layer: k and v rows ([n_kv_heads][head_dim]) to
  * their slots, keys and queries (q rows [n_heads][head_dim] to q_out, which may be q) turned by their
- * positions where rope_base > 0, in fp32 and rounded once. q and q_out NULL: keys and values only.
+ * positions where rope_base > 0 (in the form of cllm_paged_rotary's last call), in fp32 and rounded once. q and q_out NULL: keys and values only.
  * A step may be appended again (another layer, or the same with other values).
  * Errors: ERR_ARG, ERR_STATE (no plan yet), ERR_DEVICE. */
 cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
@@ -489,8 +489,8 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
  * keep their angle, those of fewer than `low` are stretched). freqs (host, dim / 2 doubles, or NULL) gives the
  * theta_j themselves in place of base and scaling. Sines and cosines are formed in double, times magnitude (0
  * means 1), and rounded once to fp32. The factors are made again on the cache's stream; a captured append keeps the
- * layout and dim that it was captured with, so capture it again behind this call.
- * Errors: ERR_ARG, ERR_STATE (rope_base 0), ERR_DEVICE. */
+ * layout and dim that it was captured with, so capture it again behind this call, which itself is not captured.
+ * Errors: ERR_ARG, ERR_STATE (rope_base 0, or the stream is being captured), ERR_DEVICE. */
 #define CLLM_ROTARY_HALVES 0
 #define CLLM_ROTARY_NEIGHBOURS 1
 #define CLLM_ROTARY_PLAIN 0
@@ -547,22 +547,23 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * accepted counts are on the device, as the lengths of the next plan are.
  *
  * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device, ascending;
- * row_start NULL: those of the last plan; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
+ * row_start NULL: those of the last plan, none where it was refused; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
  * and element's alignment) are the target's behind tokens[r]; tokens[r + 1] is its draft. With p = softmax(logits /
  * temperature[b]) and q the softmax of the draft's logits at the same temperature (draft_logits NULL, or a row of them
  * without a distribution: a point mass on the draft), the draft x stands where accept_u[r] q(x) < p(x). At the first row
  * whose draft does not stand, the next token is drawn from max(p - q, 0) (where that is 0 everywhere, from p), behind the last
  * row from p; so a request of one row just draws. Drawn is the lowest index whose running sum is above sample_u[b] times the
  * sum. Temperature 0 is greedy: p and q are 1 at the largest logit (ties: the lowest index): the acceptance of a Jacobi
- * block (cllm_jacobi_step). Weights and sums are in 64 bits.
+ * block (cllm_jacobi_step). Weights and sums are in 64 bits (below 2^-980 of the largest, weights are 0).
  * accepted[b] (1 .. the request's rows): its rows that stand, the first one always; next_token[b]. A request of no rows, or
  * whose rows are not within [0, rows], has 0 and -1. Where a row that is to be decided on has no distribution (a NaN or +inf logit, all
  * -inf; a temperature that is negative or not finite) the rows up to it are accepted and next_token is -1. A draft outside
- * [0, vocab) does not stand and takes nothing from p. A number outside [0, 1) counts as the nearest in it in the draw.
+ * [0, vocab) does not stand and takes nothing from p. A number outside [0, 1) counts as the nearest in it in the draw
+ * (NaN: 0). accepted and next_token overlap none of the other arrays.
  * workspace: device memory of at least cllm_paged_verify_bytes() bytes (draft: whether there are draft logits), 256-byte aligned, used
  * during the call: one for every stream that such calls run on at once. No allocation, no wait.
  * Errors: ERR_ARG (n outside [1, max_seqs], sizes, strides, NULL or inaccessible arrays), ERR_STATE (row_start NULL before
- * a plan), ERR_CAPACITY (workspace too small, rows x vocab above 2^41), ERR_DEVICE. */
+ * a plan), ERR_CAPACITY (workspace too small, vocab above 2^30, rows x vocab above 2^41), ERR_DEVICE. */
 cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start, int32_t rows, const int32_t *tokens, int32_t dtype,
                               int32_t vocab, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride,
                               const float *temperature, const double *accept_u, const double *sample_u, int32_t *accepted,

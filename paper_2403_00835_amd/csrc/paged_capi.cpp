@@ -364,6 +364,12 @@ cllm_status cllm_paged_rotary(cllm_paged *c, const cllm_paged_rotary_spec *spec)
     const int rot = (spec->dim == 0 ? f.head_dim : spec->dim) / 2;
     DeviceGuard dev(f.device);
     if (!dev.ok) return fail(c, CLLM_ERR_DEVICE, "the cache's device cannot be made current");
+    // (later appends take the new form at once, and must not find the old factors)
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(c->stream, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) {
+        (void)hipGetLastError();
+        return fail(c, CLLM_ERR_STATE, "the form of the rotation cannot be changed while the stream is captured");
+    }
     HIPCHK(c, launch_paged_rotary(c->rcos, c->rsin, f.max_ctx, rot, spec->magnitude == 0.0f ? 1.0 : (double)spec->magnitude, fr,
                                   c->stream));
     c->rot = rot;
@@ -536,7 +542,7 @@ cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, 
     *bytes = 0;
     if (rows < 0 || vocab < 1) return CLLM_ERR_ARG;
     const int64_t parts = (int64_t)rows * ((vocab - 1) / kVerifyChunk + 1);
-    if (2 * parts > INT32_MAX) return CLLM_ERR_CAPACITY;
+    if (vocab > 1 << 30 || 2 * parts > INT32_MAX) return CLLM_ERR_CAPACITY;  // (a chunk past the last is counted in 31 bits)
     const size_t n = rows;
     *bytes = round_up(draft ? parts * (2 * sizeof(VerifyStat) + sizeof(double)) + n * (sizeof(VerifyStop) + 2 * sizeof(float))
                             : parts * sizeof(VerifyStat) + n * sizeof(float));

@@ -297,6 +297,15 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
     return VerifyStop{};  // (not reached)
 }
 
+// A chunk's sum relative to the logit `to` in place of `from`: by two factors, as the sum may be 2^900 and each factor 2^-1000. What
+// is as good as nothing is made nothing (an empty chunk is), so that a chunk that is drawn holds a token of a weight above 2^-1000.
+__device__ __forceinline__ double joined_sum(double sum, float from, float to, const Request &q, const double *table) {
+    const double h = 0.5 * ((double)from - (double)to);
+    if (!(h >= q.floor)) return 0.0;
+    const double f = weight(h, q.scale, q.floor, table), x = sum * f * f;
+    return x < 0x1p-980 ? 0.0 : x;
+}
+
 // max(p - q, 0) of a token of logits l and lq.
 __device__ __forceinline__ double left_weight(float l, float lq, const VerifyStop &at, const Request &q, const double *table) {
 #pragma clang fp contract(off)  // the same p and q leave exactly nothing: both products are rounded
@@ -498,9 +507,8 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
         const int c = without / kVerifyChunk;
         const VerifyStat s = st[c];
         const float l = from_elem<PR>(((const typename PrecT<PR>::T *)p.logits)[(size_t)at.row * p.stride + without]);
-        const double f = weight((double)s.max - (double)at.p_max, scale, floor, table);
         const double mine = s.max > -INFINITY ? weight_of(l, s.max, scale, floor, table) : 0.0;
-        cut = (s.sum - mine) * f;
+        cut = joined_sum(s.sum - mine, s.max, at.p_max, q, table);
         if (mine * 256.0 > s.sum * 255.0) {  // uniform: little is left, of which the difference loses digits
             double x[N], sum = 0.0;
             if (tid < kDraw) {
@@ -521,7 +529,7 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
         if (rest) return p.rest[(size_t)q.first * p.chunks + c];
         if (without >= 0 && c == without / kVerifyChunk) return cut;
         const VerifyStat s = st[c];
-        return s.sum * weight((double)s.max - (double)at.p_max, scale, floor, table);  // (an empty chunk's sum is 0)
+        return joined_sum(s.sum, s.max, at.p_max, q, table);
     };
     if (w == 0) {  // one wave: the chunk in which the running sum passes the number
         double first, t;  // this lane's first chunk, the sum

@@ -246,6 +246,8 @@ def test_captured_appends(binding):
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=side):
             step()
+            with pytest.raises(binding.CllmError, match="ERR_STATE.*captured"):
+                c.rotary(dim=16)
         for i, (a, m, factor) in enumerate([([0, 0], [3, 5], 2.0), ([3, 5], [16, 8], 2.0), ([19, 13], [1, 0], 4.0), ([20, 13], [2, 2], 4.0)]):
             c.rotary(dim=32, scaling="linear", factor=factor)
             for x, v in ((ctx, a), (new, m)):

@@ -225,6 +225,27 @@ def test_far_logits(cache):
             check(cache, [0, 1, 2, 3, 4], [0] * 4, place(x, dtype, 0, 0), None, [1.0, 0.5, 1.0, 1.0], [0.5] * 4, [u] * 4)
 
 
+def test_chunks_far_apart(cache):
+    """Parts of a long row at very different heights: weights of one of them are all that counts, wherever the number falls, and
+    sums relative to different logits are joined."""
+    g = np.random.default_rng(12)
+    V = 150000  # more chunks of any size up to 2048 than a wave has lanes
+    base = g.standard_normal((1, V))
+    for heights, t in (((0, -2000, 3000), 1.0), ((-5000, -5000, -9000), 1.0), ((650, 600, -700), 1.0), ((0, 0, 5000), 0.3), ((-620, 0, 620), 1.0),
+                       ((1e4, 1e4 + 3, 1e4 - 3), 2.0)):
+        x = base.copy()
+        for i, h in enumerate(heights):
+            x[0, i * 50000:(i + 1) * 50000] += h
+        x[0, 70000:74096] = -np.inf  # a masked stretch
+        for u in (0.0, 1e-9, 0.4, 0.9, np.nextafter(1, 0), 1.0):
+            a, tok = check(cache, [0, 1], [0], place(x, torch.float32, 0, 0), None, [t], [0.0], [u])
+        two = np.repeat(x, 2, 0)
+        for draft in (int(x[0].argmax()), 5, 70001, 120000):
+            for u in (0.0, 0.2, 0.999):
+                check(cache, [0, 2], [0, draft], place(two, torch.float32, 0, 0), None, [t], [u, 0], [0.37])
+                check(cache, [0, 2], [0, draft], place(two, torch.float32, 0, 0), place(np.roll(two, 3, 1), torch.float32, 0, 0), [t], [u, 0], [0.37])
+
+
 def test_rows_of_nobody(cache):
     """row_start that leaves the rows' bounds, or falls: those requests have nothing, the others what they have alone."""
     g = np.random.default_rng(9)

@@ -49,7 +49,7 @@ def test_bad_sizes_are_refused():
     n = ctypes.c_size_t(7)
     L = binding.lib()
     assert L.cllm_paged_verify_bytes(1, 1, 0, None) == 1
-    for rows, vocab, want in ((-1, 5, 1), (1, 0, 1), (1, -3, 1), (2**20, 2**31 - 1, 3), (2**31 - 1, 1, 3)):
+    for rows, vocab, want in ((-1, 5, 1), (1, 0, 1), (1, -3, 1), (2**20, 2**30, 3), (1, 2**30 + 1, 3), (1, 2**31 - 1, 3), (2**31 - 1, 1, 3)):
         assert L.cllm_paged_verify_bytes(rows, vocab, 1, ctypes.byref(n)) == want and n.value == 0
     with pytest.raises(binding.CllmError, match="ERR_CAPACITY"):
         binding.PagedCache.verify_workspace_bytes(2**31 - 1, 4097, True)
