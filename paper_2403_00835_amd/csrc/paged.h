@@ -149,6 +149,7 @@ struct alignas(16) VerifyStop {
     float p_max, q_max;     // what they are relative to
     int first, row;       // the request's first row, the one it stops at; row -1: the request has none
     int draft;            // a refused draft that is a token, or -1
+    float logit;          // its logit in the row
     int kind;             // VS_*
     int top;
 };

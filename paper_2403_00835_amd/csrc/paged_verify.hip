@@ -38,7 +38,8 @@ __device__ __forceinline__ void lds_barrier() {
 }
 // The table, in LDS, by the first kExpSteps threads.
 __device__ __forceinline__ void make_table(double (&table)[kExpSteps]) {
-    if (threadIdx.x < kExpSteps) table[threadIdx.x] = exp_step(threadIdx.x);
+    if (threadIdx.x < kExpSteps)
+        table[threadIdx.x] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, exp_step(threadIdx.x)) - ((uint64_t)threadIdx.x << 44));
     lds_barrier();
 }
 
@@ -58,8 +59,8 @@ __device__ __forceinline__ double weight_scale(float temperature) {
 // -1000 / scale (of a temperature).
 __device__ __forceinline__ double weight_floor(float temperature) { return -693.14718055994531 * (double)temperature; }
 
-// 2^(d scale), d scale within +-1000, as f 2^r: f = 2^(k / 256) from the table (LDS) with k / 256's whole part added to its
-// exponent, 2^r, |r| <= 1 / 512, by its Taylor polynomial, whose first term left out is 2^-42 of it. The product d scale is not
+// 2^(d scale), d scale within +-1000, as f 2^r: f = 2^(k / 256) from the table (LDS), whose entry j holds 2^(j / 256) less j in
+// the last eight bits before its exponent's, where all of k is added (j is k's remainder, and the rest its whole part), 2^r, |r| <= 1 / 512, by its Taylor polynomial, whose first term left out is 2^-42 of it. The product d scale is not
 // rounded on its own.
 struct Weight {
     double f, r2;
@@ -74,8 +75,7 @@ __device__ __forceinline__ Weight weight_parts(double d, double scale, const dou
     y = __builtin_fma(y, r, 0x1.62e42fefa39efp-1);
     y = __builtin_fma(y, r, 1.0);
     const u32x2 e = __builtin_bit_cast(u32x2, table[k & (kExpSteps - 1)]);
-    uint32_t high;
-    asm("v_lshl_add_u32 %0, %1, 12, %2" : "=v"(high) : "v"(k & ~(kExpSteps - 1u)), "v"(e[1]));  // (the compiler makes three of it)
+    const uint32_t high = (k << 12) + e[1];
     return {__builtin_bit_cast(double, u32x2{e[0], high}), y};
 }
 // Below 2^-1000: about 2^-1000, which no sum that holds a weight above 2^-900 minds; floor = -1000 / scale.
@@ -90,6 +90,7 @@ __device__ __forceinline__ double weight_of(float l, float m, double scale, doub
 }
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // The logits i .. i + 7 of a row, at any element's address, as eight neighbours from `from` on; those of them that are before i
 // or past the row's end are -inf.
@@ -119,6 +120,19 @@ struct Eight {
     __device__ __forceinline__ float operator[](int k) const {
         if constexpr (PR == Prec::BF16) return __uint_as_float(k % 2 ? raw[0][k / 2] & 0xffff0000u : raw[0][k / 2] << 16);
         return __uint_as_float(raw[k / VEC][k % VEC]);
+    }
+    // The largest magnitude (where there is a NaN, NaN or that of the others).
+    __device__ __forceinline__ float size() const {
+        if constexpr (PR == Prec::BF16) {
+            u16x2 m{};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, raw[0][i] & 0x7fff7fffu));
+            return __uint_as_float((uint32_t)max(m[0], m[1]) << 16);
+        }
+        float m = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf((*this)[k]));
+        return m;
     }
     __device__ __forceinline__ void put(int k, float x) {  // (a value of T)
         uint32_t &w = reinterpret_cast<uint32_t *>(raw)[PR == Prec::BF16 ? k / 2 : k];
@@ -185,17 +199,17 @@ __device__ __forceinline__ int wave_min(int x) {
     return x;
 }
 
-// A row's distribution from the statistics of its chunks, by one wave.
+// A row's distribution from the statistics of its chunks, by one wave. head: of chunk `lane`, where there is one.
 struct Law {
     float max;    // what weights are relative to: the largest of its chunks' (greedy requests: the largest logit)
     double norm;  // 1 / the sum of the weights
     int top;      // greedy requests: the largest logit's lowest index
     bool ok;      // neither NaN nor +inf among the logits, nor all -inf
 };
-__device__ __forceinline__ Law row_law(const VerifyStat *st, int chunks, double scale, double floor, const double *table) {
+__device__ __forceinline__ Law row_law(const VerifyStat &head, const VerifyStat *st, int chunks, double scale, double floor, const double *table) {
     const int lane = threadIdx.x & 63;
     constexpr VerifyStat kNone{0.0, -INFINITY, 0x7fffffff};
-    const VerifyStat mine = lane < chunks ? st[lane] : kNone;  // (the first 64 chunks: most vocabularies' all)
+    const VerifyStat mine = lane < chunks ? head : kNone;  // (the first 64 chunks: most vocabularies' all)
     float m = mine.max;
     bool bad = m != m;
     for (int c = lane + kWave; c < chunks; c += kWave) {
@@ -244,8 +258,10 @@ struct Decide {  // LDS
     int stop;
 };
 
-// Where a request stops, by the whole workgroup: a row a wave.
-__device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Request &q, const double *table, Decide &s) {
+// Where a request stops, by the whole workgroup: a row a wave. heads (or null): statistics of the first 64 chunks of the row at
+// which it stops, in the entry of the row's wave.
+__device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Request &q, const double *table, Decide &s,
+                                             VerifyStat (*heads)[kWave]) {
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / kWave, first = q.first, end = q.end;
     const double scale = q.scale, floor = q.floor;
     if (first >= end) {  // uniform
@@ -254,19 +270,40 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
         return none;
     }
     if (threadIdx.x == 0) s.stop = end;
+    const int lane = threadIdx.x & 63;
+    struct Row {  // what a row's decision reads; the next one's is on its way beside this one's
+        VerifyStat p, q;
+        double u;
+        float lp, lq;
+        int x;
+    } next{};
+    auto load = [&](int r) {
+        if (r >= end) return;
+        if (lane < p.chunks) next.p = p.stats[(size_t)r * p.chunks + lane];
+        next.lp = p.picked[r];  // (the draft's logit, where it is a token)
+        if (r + 1 == end) return;  // no draft
+        next.x = p.tokens[r + 1];
+        next.u = p.accept_u[r];
+        if (!p.draft) return;
+        if (lane < p.chunks) next.q = p.stats[(size_t)(p.rows + r) * p.chunks + lane];
+        next.lq = p.picked[p.rows + r];
+    };
+    load(first + w);
     __syncthreads();
     for (int r0 = first; r0 < end; r0 += waves) {
         const int r = r0 + w;
         if (r < end) {
+            const Row at = next;
+            load(r + waves);
             const bool drafted = r + 1 < end;
             const VerifyStat *st = p.stats + (size_t)r * p.chunks, *sq = p.stats + (size_t)(p.rows + r) * p.chunks;
-            const int x = drafted ? p.tokens[r + 1] : -1;
+            const int x = drafted ? at.x : -1;
             const bool known = x >= 0 && x < p.vocab;
-            const double u = drafted ? p.accept_u[r] : 0.0;
-            const float lp = p.picked[r], lq = p.draft ? p.picked[p.rows + r] : 0.f;  // the draft's, where it is a token
-            const Law law = row_law(st, p.chunks, scale, floor, table);
+            const double u = at.u;
+            const float lp = at.lp, lq = at.lq;
+            const Law law = row_law(at.p, st, p.chunks, scale, floor, table);
             Law lawq{0.f, 0.0, 0, false};
-            if (p.draft && drafted && scale > 0.0) lawq = row_law(sq, p.chunks, scale, floor, table);
+            if (p.draft && drafted && scale > 0.0) lawq = row_law(at.q, sq, p.chunks, scale, floor, table);
             bool stands = false;
             if (law.ok && drafted && known) {
                 if (scale == 0.0) {
@@ -277,17 +314,19 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
                     stands = u * qx < px;
                 }
             }
-            if (!stands && (threadIdx.x & 63) == 0) {
-                VerifyStop &at = s.at[w];
-                at.p_norm = law.norm;
-                at.q_norm = lawq.norm;
-                at.p_max = law.max;
-                at.q_max = lawq.max;
-                at.first = first;
-                at.row = r;
-                at.draft = known ? x : -1;
-                at.kind = (drafted ? VS_REFUSED : 0) | (law.ok && scale >= 0.0 ? VS_LAW : 0) | (law.ok && lawq.ok ? VS_REST : 0);
-                at.top = law.top;
+            if (!stands && heads) heads[w][lane] = at.p;
+            if (!stands && lane == 0) {
+                VerifyStop &stop = s.at[w];
+                stop.p_norm = law.norm;
+                stop.q_norm = lawq.norm;
+                stop.p_max = law.max;
+                stop.q_max = lawq.max;
+                stop.first = first;
+                stop.row = r;
+                stop.draft = known ? x : -1;
+                stop.logit = lp;
+                stop.kind = (drafted ? VS_REFUSED : 0) | (law.ok && scale >= 0.0 ? VS_LAW : 0) | (law.ok && lawq.ok ? VS_REST : 0);
+                stop.top = law.top;
                 atomicMin(&s.stop, r);
             }
         }
@@ -338,8 +377,12 @@ __device__ __forceinline__ void row_weights(const VerifyParams &p, const VerifyS
 
 // The sum of weights of chunks of 2048 logits of the target's rows and then of the draft's, and the logit that they are relative
 // to: 0 where 64 bits hold every weight, which saves a difference and a bound for each (such chunks are most), or the largest
-// one. Of greedy requests the largest logit and its index instead. A chunk a wave, its logits in registers as they came, which
-// leaves room for eight waves a SIMD.
+// one. Of greedy requests the largest logit and its index instead. A chunk a wave, its logits in registers as they came (80
+// registers in bf16, 94 in fp32: six and five waves a SIMD).
+// Bound: 64-bit arithmetic, about ten instructions a logit, beside the reading: 64 requests of up to seven rows of 99,991 bf16
+// logits, the target's and the draft's (89.6 MB), 31.0 us, 2.9 TB/s; 512 rows of 32,000 fp32 logits (65.5 MB) 18.6 us, 3.5
+// TB/s; latency: five rows 6.3 us. Weights relative to the largest logit, each with its difference and bound, took 39 us in
+// place of 31; four chunks a wave with the next one's loads ahead took the registers of other waves and no less time.
 template <Prec PR>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, int row0) {
     using T = typename PrecT<PR>::T;
@@ -372,22 +415,16 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
     if (!isq) b = request_of(p.row_start, p.n, r);
     const float temperature = p.temperature[b];
     const double scale = weight_scale(temperature), floor = weight_floor(temperature);
-    float m = -INFINITY, size = 0.0f;
-    bool bad = false;
+    float size = 0.0f;
 #pragma unroll
     for (int v = 0; v < kParts; ++v) {
-#pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            const float a = x[v][k], c = x[v][k + 1];
-            m = fmaxf(fmaxf(m, a), c);
-            size = fmaxf(fmaxf(size, fabsf(a)), fabsf(c));
-            bad |= __builtin_isunordered(a, c);
-        }
+        size = fmaxf(size, x[v].size());
         x[v].keep();
     }
     double sum = 0.0;
     float ref = 0.0f;
     int top = 0x7fffffff;
+    bool none;
     if (scale > 0.0 && __all((double)size <= -0.9 * floor)) {
 #pragma unroll
         for (int v = 0; v < kParts; ++v)
@@ -398,8 +435,22 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
                 if (k % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (more at once take the registers of other waves)
             }
         sum = wave_sum(sum);
+        none = sum != sum;
     } else {
+        float m = -INFINITY;
+        bool bad = false;
+#pragma unroll
+        for (int v = 0; v < kParts; ++v) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float a = x[v][k], c = x[v][k + 1];
+                m = fmaxf(fmaxf(m, a), c);
+                bad |= __builtin_isunordered(a, c);
+            }
+            x[v].keep();
+        }
         ref = wave_max(m);
+        none = __any(bad) || ref == INFINITY;
         if (ref > -INFINITY && ref < INFINITY) {  // else there is nothing, or no distribution
 #pragma unroll
             for (int v = kParts - 1; v >= 0; --v)
@@ -417,7 +468,6 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
                 top = wave_min(top);
         }
     }
-    const bool none = __any(bad) || ref == INFINITY;
     if (lane == 0) {
         p.stats[(size_t)all * p.chunks + chunk] = VerifyStat{sum, none ? NAN : ref, top};
         if (draft >= chunk * kVerifyChunk && draft < min((chunk + 1) * kVerifyChunk, p.vocab)) p.picked[all] = from_elem<PR>(row[draft]);
@@ -425,8 +475,10 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
 }
 
 // Where the requests stop, and the sums of max(p - q, 0) over the chunks of the rows whose draft was refused: two chunks a
-// workgroup, each of which decides for itself.
-constexpr int kRestChunks = kRest / kWave / kParts;
+// workgroup at a time, each of which decides for itself.
+// Bound: latency (what a decision reads, then a row's logits) and 64-bit arithmetic: one request of 32,000 tokens 6.1 us, 64
+// of 99,991 13.6, in 13 workgroups of two rounds each (25 of one round 16.4, 7 of four 17.1).
+constexpr int kRestChunks = kRest / kWave / kParts, kRestFit = 4;
 template <Prec PR>
 __global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
     using T = typename PrecT<PR>::T;
@@ -434,7 +486,7 @@ __global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
     __shared__ Decide s_decide;
     const int b = blockIdx.y, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Request q = begin(p, b, table);
-    const VerifyStop at = decide(p, q, table, s_decide);
+    const VerifyStop at = decide(p, q, table, s_decide, nullptr);
     if (at.row < 0) return;  // uniform
     if (blockIdx.x == 0 && threadIdx.x == 0) p.stops[at.first] = at;
     if (!(at.kind & VS_REST)) return;
@@ -475,21 +527,27 @@ __global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
 }
 
 // The accepted rows and the next token. Workgroup: a request.
+// Bound: latency, of three to five reads that wait for one another, each about 1 us: one request 4.7 us, 64 of 99,991 tokens
+// 6.0; where it decides, 16 of 32 rows, 7.8. Neighbours and waves in the tokens' order pick the token by ballots: atomics on
+// LDS for it, lane by lane, took 4.4 us more.
 template <Prec PR>
 __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     constexpr int N = 4, kDraw = kVerifyChunk / N;  // neighbouring tokens of a thread, threads that a chunk takes
     static_assert(kDraw <= kToken && kDraw % kWave == 0, "whole waves");
     __shared__ double table[kExpSteps], s_sum[kDraw / kWave], s_aim;
     __shared__ Decide s_decide;
-    __shared__ int s_from, s_chunk, s_token, s_last;
+    __shared__ VerifyStat s_heads[kToken / kWave][kWave];
+    __shared__ int s_from, s_chunk, s_found[kDraw / kWave], s_last[kDraw / kWave];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const double u = p.sample_u[b];
     const Request q = begin(p, b, table);
     const double scale = q.scale, floor = q.floor;
     VerifyStop at{};
     at.row = -1;
+    double rest_head = 0.0;  // the rest's sum of chunk `lane`, where there is a rest; on its way beside what says so
+    if (p.draft && q.first < q.end && lane < p.chunks) rest_head = p.rest[(size_t)q.first * p.chunks + lane];
     if (!p.draft)
-        at = decide(p, q, table, s_decide);
+        at = decide(p, q, table, s_decide, s_heads);
     else if (q.first < q.end)
         at = p.stops[q.first];  // decided with the rest's sums
     const bool law = at.row >= 0 && (at.kind & VS_LAW);
@@ -501,13 +559,13 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     // What is drawn from: the rest, p without the refused token, or p (also where those are empty).
     bool rest = at.kind & VS_REST;
     int without = !rest && (at.kind & VS_REFUSED) ? at.draft : -1;
-    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks;
+    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks, *head = s_heads[(at.row - at.first) % (kToken / kWave)];
+    auto stat = [&](int c) { return p.draft || c >= kWave ? st[c] : head[c]; };
     double cut = 0.0;  // the sum of the refused token's chunk without it
     if (without >= 0) {
         const int c = without / kVerifyChunk;
-        const VerifyStat s = st[c];
-        const float l = from_elem<PR>(((const typename PrecT<PR>::T *)p.logits)[(size_t)at.row * p.stride + without]);
-        const double mine = s.max > -INFINITY ? weight_of(l, s.max, scale, floor, table) : 0.0;
+        const VerifyStat s = stat(c);
+        const double mine = s.max > -INFINITY ? weight_of(at.logit, s.max, scale, floor, table) : 0.0;
         cut = joined_sum(s.sum - mine, s.max, at.p_max, q, table);
         if (mine * 256.0 > s.sum * 255.0) {  // uniform: little is left, of which the difference loses digits
             double x[N], sum = 0.0;
@@ -526,9 +584,9 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     }
     auto chunk_sum = [&](int c) {
         if (c >= p.chunks) return 0.0;
-        if (rest) return p.rest[(size_t)q.first * p.chunks + c];
+        if (rest) return c < kWave ? rest_head : p.rest[(size_t)q.first * p.chunks + c];
         if (without >= 0 && c == without / kVerifyChunk) return cut;
-        const VerifyStat s = st[c];
+        const VerifyStat s = stat(c);
         return joined_sum(s.sum, s.max, at.p_max, q, table);
     };
     if (w == 0) {  // one wave: the chunk in which the running sum passes the number
@@ -570,8 +628,6 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
         if (lane == 0) {
             s_chunk = chunk;
             s_aim = aim - base;
-            s_token = 0x7fffffff;
-            s_last = -1;
             s_from = rest ? 2 : without >= 0 ? 1 : 0;
         }
     }
@@ -599,10 +655,24 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
             if (base > aim && found == 0x7fffffff) found = i + k;
         }
     }
-    if (found != 0x7fffffff) atomicMin(&s_token, found);
-    if (last >= 0) atomicMax(&s_last, last);
+    // Lanes and waves are in the tokens' order: the first one's that found it, or the last one's that holds any.
+    const uint64_t finds = __ballot(found != 0x7fffffff), holds = __ballot(last >= 0);
+    const int first_found = __builtin_amdgcn_readlane(found, max(__ffsll((unsigned long long)finds) - 1, 0));
+    const int last_held = __builtin_amdgcn_readlane(last, max(63 - (int)__clzll((long long)holds), 0));
+    if (tid < kDraw && lane == 0) {
+        s_found[w] = finds ? first_found : -1;
+        s_last[w] = last_held;
+    }
     __syncthreads();
-    if (tid == 0) p.next_token[b] = s_token != 0x7fffffff ? s_token : s_last;
+    if (tid == 0) {
+        int token = -1, least = -1;
+#pragma unroll
+        for (int v = kDraw / kWave - 1; v >= 0; --v) {
+            if (s_found[v] >= 0) token = s_found[v];
+            if (least < 0) least = s_last[v];
+        }
+        p.next_token[b] = token >= 0 ? token : least;
+    }
 }
 
 namespace {
@@ -614,10 +684,11 @@ hipError_t launch_verify(const VerifyParams &p, hipStream_t s) {
         for (int r = 0; r < rows; r += most)
             hipLaunchKernelGGL(verify_stats_kernel<PR>, dim3((unsigned)((p.chunks + per - 1) / per), (unsigned)std::min(rows - r, most)),
                                dim3(kThreads), 0, s, p, r);
-        if (p.draft)  // (about as many workgroups as run at once: each decides first)
-            hipLaunchKernelGGL(verify_rest_kernel<PR>,
-                               dim3((unsigned)std::min((p.chunks + kRestChunks - 1) / kRestChunks, std::max(2 * kCUs / p.n, 1)), (unsigned)p.n),
-                               dim3(kRest), 0, s, p);
+        if (p.draft) {  // about as many workgroups as run at once, as each decides first, with about as many chunks each
+            const int units = (p.chunks + kRestChunks - 1) / kRestChunks, fit = std::max(kRestFit * kCUs / p.n, 1);
+            const int rounds = (units + fit - 1) / fit;
+            hipLaunchKernelGGL(verify_rest_kernel<PR>, dim3((unsigned)((units + rounds - 1) / rounds), (unsigned)p.n), dim3(kRest), 0, s, p);
+        }
     }
     hipLaunchKernelGGL(verify_token_kernel<PR>, dim3((unsigned)p.n), dim3(kToken), 0, s, p);
     return hipGetLastError();
