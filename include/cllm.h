@@ -475,8 +475,8 @@ cllm_status cllm_paged_plan(cllm_paged *c, int32_t n, const int32_t *seq_ids, co
 
 /* The rows of the last plan into the pages of one layer: k and v rows ([n_kv_heads][head_dim]) to
  * their slots, keys and queries (q rows [n_heads][head_dim] to q_out, which may be q) turned by their
- * positions where rope_base > 0 (in the form of cllm_paged_rotary's last call), in fp32 and rounded once. q and q_out NULL: keys and values only.
- * A step may be appended again (another layer, or the same with other values).
+ * positions where rope_base > 0 (in the form of cllm_paged_rotary's last call), in fp32 and rounded once. q and
+ * q_out NULL: keys and values only. A step may be appended again (another layer, or the same with other values).
  * Errors: ERR_ARG, ERR_STATE (no plan yet), ERR_DEVICE. */
 cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
                               int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_pages, void *v_pages);
@@ -547,21 +547,23 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * accepted counts are on the device, as the lengths of the next plan are.
  *
  * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device, ascending;
- * row_start NULL: those of the last plan, none where it was refused; rows: the host's bound of row_start[n]). Row r's logits (vocab of them, of dtype, any row stride
- * and element's alignment) are the target's behind tokens[r]; tokens[r + 1] is its draft. With p = softmax(logits /
+ * row_start NULL: those of the last plan, none where it was refused; rows: the host's bound of row_start[n]). Row r's
+ * logits (vocab of them, of dtype, any row stride and element's alignment) are the target's behind tokens[r];
+ * tokens[r + 1] is its draft. With p = softmax(logits /
  * temperature[b]) and q the softmax of the draft's logits at the same temperature (draft_logits NULL, or a row of them
  * without a distribution: a point mass on the draft), the draft x stands where accept_u[r] q(x) < p(x). At the first row
  * whose draft does not stand, the next token is drawn from max(p - q, 0) (where that is 0 everywhere, from p), behind the last
  * row from p; so a request of one row just draws. Drawn is the lowest index whose running sum is above sample_u[b] times the
  * sum. Temperature 0 is greedy: p and q are 1 at the largest logit (ties: the lowest index): the acceptance of a Jacobi
- * block (cllm_jacobi_step). Weights and sums are in 64 bits (below 2^-980 of the largest, weights are 0).
+ * block (cllm_jacobi_step). Weights and sums are in 64 bits
+ * (tokens of less than 2^-80 of the largest weight may count as nothing).
  * accepted[b] (1 .. the request's rows): its rows that stand, the first one always; next_token[b]. A request of no rows, or
  * whose rows are not within [0, rows], has 0 and -1. Where a row that is to be decided on has no distribution (a NaN or +inf logit, all
  * -inf; a temperature that is negative or not finite) the rows up to it are accepted and next_token is -1. A draft outside
  * [0, vocab) does not stand and takes nothing from p. A number outside [0, 1) counts as the nearest in it in the draw
  * (NaN: 0). accepted and next_token overlap none of the other arrays.
- * workspace: device memory of at least cllm_paged_verify_bytes() bytes (draft: whether there are draft logits), 256-byte aligned, used
- * during the call: one for every stream that such calls run on at once. No allocation, no wait.
+ * workspace: device memory of at least cllm_paged_verify_bytes() bytes (draft: whether there are draft logits), 256-byte
+ * aligned, used during the call: one for every stream that such calls run on at once. No allocation, no wait.
  * Errors: ERR_ARG (n outside [1, max_seqs], sizes, strides, NULL or inaccessible arrays), ERR_STATE (row_start NULL before
  * a plan), ERR_CAPACITY (workspace too small, vocab above 2^30, rows x vocab above 2^41), ERR_DEVICE. */
 cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start, int32_t rows, const int32_t *tokens, int32_t dtype,

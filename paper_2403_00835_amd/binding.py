@@ -438,6 +438,9 @@ class PagedCache:
 
         cache.plan(seq_ids, ctx_lens, new_lens, rows)      # pages and rows of the step
         per layer: cache.append(q, k, v, q, k_pages, v_pages); cache.attn(q, k_pages, v_pages, out)
+        cache.verify(tokens, logits, accepted, next_token, ...)     # what stands of the blocks, and what follows
+
+    rotary sets the form of the rotation; append takes gains of head norms, attn a window.
 
     The operators have no backward: a tensor that requires grad is refused unless gradients are off
     (torch.no_grad(), torch.inference_mode()).

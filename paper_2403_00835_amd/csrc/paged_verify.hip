@@ -377,12 +377,12 @@ __device__ __forceinline__ void row_weights(const VerifyParams &p, const VerifyS
 
 // The sum of weights of chunks of 2048 logits of the target's rows and then of the draft's, and the logit that they are relative
 // to: 0 where 64 bits hold every weight, which saves a difference and a bound for each (such chunks are most), or the largest
-// one. Of greedy requests the largest logit and its index instead. A chunk a wave, its logits in registers as they came (80
-// registers in bf16, 94 in fp32: six and five waves a SIMD).
-// Bound: 64-bit arithmetic, about ten instructions a logit, beside the reading: 64 requests of up to seven rows of 99,991 bf16
-// logits, the target's and the draft's (89.6 MB), 31.0 us, 2.9 TB/s; 512 rows of 32,000 fp32 logits (65.5 MB) 18.6 us, 3.5
-// TB/s; latency: five rows 6.3 us. Weights relative to the largest logit, each with its difference and bound, took 39 us in
-// place of 31; four chunks a wave with the next one's loads ahead took the registers of other waves and no less time.
+// one. Of greedy requests the largest logit and its index instead. A chunk a wave, its logits in registers as they came (72
+// registers in bf16, 90 in fp32).
+// Bound: arithmetic beside the reading (64 requests of one to seven rows of 99,991 bf16 logits, the target's and the draft's, 89.6 MB:
+// 30.0 us, 3.0 TB/s, the vector units at work for two thirds of it, half of that in 64 bits; 512 rows of 32,000 fp32
+// logits, 65.5 MB: 18.6 us, 3.5 TB/s), of a few rows latency (five: 6.3 us). Weights relative to the largest logit in every chunk
+// take 35 us in place of 31; eight waves a SIMD in place of seven, and the table from memory, the same 30.
 template <Prec PR>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, int row0) {
     using T = typename PrecT<PR>::T;
