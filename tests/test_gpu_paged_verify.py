@@ -103,6 +103,25 @@ def test_many_requests_and_long_ones(cache):
     assert a == [1, 100, 3]
 
 
+@pytest.mark.parametrize("stop", [0, 15, 16, 18, 19])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_where_a_long_request_over_many_chunks_stops(cache, stop, with_draft):
+    """The row of any wave, in its first or its second turn, or the last row, with more chunks than a wave has lanes."""
+    rng = random.Random(stop)
+    start, tokens, x, draft, _, au, su = problem(rng, [2, 20, 1], 140000, with_draft)
+    for r in range(2, 21):  # drafts that stand, up to the row
+        x[r, tokens[r + 1]] = 25.0 if r < 2 + stop else -25.0
+    for low in (None, 139999, 3):  # the refused draft is anywhere, or in the last chunk, or in the first
+        if low is not None and stop < 19:
+            x[2 + stop, tokens[3 + stop]] = 0.0
+            tokens[3 + stop] = low
+            x[2 + stop, low] = 1.0
+            au[2 + stop] = 1 - 2.0 ** -40
+        a, _ = check(cache, start, tokens, place(x, torch.float32, 0, 0), None if draft is None else place(draft, torch.float32, 0, 0),
+                     [0.8, 1.0, 1.0], au, su)
+        assert a[1] == stop + 1 or with_draft
+
+
 def test_the_drawn_tokens_have_the_targets_law(cache):
     """1024 requests of two rows at a time, all of one p and q: the first token that stands or is drawn is distributed as p, within five
     standard deviations of each count."""
