@@ -105,6 +105,11 @@ struct Sight {
     // The row at pos sees the key; it sees some key of [k, k + n), k <= pos.
     __device__ bool key(int pos, int k) const { return k <= pos && (!WIN || k > pos - window || k < sinks); }
     __device__ bool some(int pos, int k, int n) const { return !WIN || k + n - 1 > pos - window || k < sinks; }
+    // key() of the keys k .. k + 63, a bit each.
+    __device__ uint64_t bits(int pos, int k) const {
+        auto below = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };
+        return below(pos - k + 1) & (~below(pos - window + 1 - k) | below(sinks - k));
+    }
     // Some row of the positions up to `last` does not see some key of [k, k + n) that is behind it.
     __device__ bool cuts(int last, int k, int n) const { return WIN && max(k, sinks) <= min(k + n - 1, last - window); }
 };
@@ -123,6 +128,13 @@ struct Visible {
     }
     __device__ int piece(int j) const { return WIN && j >= sink_end ? j - sink_end + from : j; }
 };
+
+// Behind a window, a tile whose rows see few chunks is not split: the first of the plan's ranges takes them all and writes the
+// output. (One that sees every chunk is split as without a window, with the same bits.)
+template <bool WIN>
+__device__ __forceinline__ bool tile_is_whole(const PagedAttnParams &p, const Visible<WIN, kKeys> &chunks, int last) {
+    return WIN && chunks.count <= p.whole_chunks && chunks.count <= last / kKeys;
+}
 
 // Scores to probabilities: keys past qpos (relative to the chunk's first key, key0) are out. mx: the row's
 // maximum (-inf: it sees no key), l: its sum.
@@ -344,6 +356,12 @@ __device__ __forceinline__ void join_row(const PagedAttnParams &p, const PagedIt
         const int first = row / BR * BR, last = min(first + BR, it.m * p.group - it.row) - 1;  // (an item begins with a block)
         spans = Visible<WIN, kPagedSpanKeys>(see, it.ctx + map.token(first), it.ctx + map.token(last));
         count = spans.count;
+    }
+    if (WIN && it.count > 0) {
+        const int t0 = it.row / kPagedTileRows * kPagedTileRows, t1 = min(t0 + kPagedTileRows, it.m * p.group) - 1;
+        const RowMap tile(p, t0);
+        const int last = it.ctx + tile.token(t1 - t0);
+        if (tile_is_whole<WIN>(p, Visible<WIN, kKeys>(see, it.ctx + tile.token(0), last), last)) return;
     }
     float M = -INFINITY, l = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -870,6 +888,18 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Whether x is true in some thread of four waves, and a barrier for what they have written to LDS. Loads in flight (the next
+// chunk's) are not waited for, as __syncthreads_or() would. Between two calls there is another barrier.
+__device__ __forceinline__ bool any_of_workgroup(bool x, int (&waves)[4]) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool any = __any(x);
+    if ((threadIdx.x & 63) == 0) waves[w] = any;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));  // LDS alone
+    barrier_no_fence();
+    return waves[0] | waves[1] | waves[2] | waves[3];
+}
+
 // LDS of the tile kernel: two buffers of a chunk's K and V, and the classes of values that are not finite.
 template <int HD>
 constexpr int tile_lds() {
@@ -892,7 +922,10 @@ constexpr int tile_lds() {
 // nothing waits for one thing alone. Reads that run ahead of the softmax, softmax and products of two chunks
 // interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 800
 // TFLOP/s, 32 wide 640, 256 wide 490 (one workgroup a CU, and 32 registers spilled).
-// Behind a window (WIN) a tile walks the chunks that its rows see; a range of the plan's is that share of them.
+// Behind a window (WIN) a tile walks the chunks that its rows see; a range of the plan's is that share of them, or the first
+// is all (tile_is_whole). 2048 tokens at 16384 behind 4096 and 64 sinks take 166 us, 840 TFLOP/s of visible keys. A chunk that some
+// row does not see in whole takes 7 thousand clocks in place of 4: the look for values that are not finite, and the masks, as
+// bits of a word a row (key by key, with a wait for the next chunk's loads in the look, 10).
 template <int HD, bool WIN>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
     using TL = Tile<HD>;
@@ -900,6 +933,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
     extern __shared__ u32x4 s_raw[];
     uint8_t *s_kv = reinterpret_cast<uint8_t *>(s_raw);  // [buffer][K, V]
     uint32_t *s_cls = reinterpret_cast<uint32_t *>(s_kv + 4 * TL::BYTES);  // [column][16 rows]
+    __shared__ int s_bad[4];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r32 = lane & 31, hb = lane >> 5;
     const ChunkLoads<HD> loads(tid);
@@ -918,7 +952,13 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
         const Sight<WIN> see(p);
         const Visible<WIN, kKeys> chunks(see, tfirst, tlast);
         int c0 = u.k0, c1 = min(u.k1, tlast / kKeys + 1);
-        if (WIN && chunks.count <= tlast / kKeys) {  // (a tile that sees every chunk: as without a window, with the same bits)
+        const bool one = tile_is_whole<WIN>(p, chunks, tlast);  // uniform
+        if (one && u.k0 > 0) continue;
+        const int part = one ? -1 : u.part;
+        if (one) {
+            c0 = 0;
+            c1 = chunks.count;
+        } else if (WIN && chunks.count <= tlast / kKeys) {
             const int all = (kvlen + kKeys - 1) / kKeys;
             c0 = (int)((int64_t)min(u.k0, all) * chunks.count / all);
             c1 = (int)((int64_t)min(u.k1, all) * chunks.count / all);
@@ -966,7 +1006,7 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                             bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
                     }
                 }
-                if (__syncthreads_or(bad)) {
+                if (any_of_workgroup(bad, s_bad)) {
                     for (int col = tid; col < HD; col += 256) {
                         float acc = 0.f;
                         int key = 0;
@@ -986,16 +1026,13 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                         for (int r0 = 0; r0 < kPagedTileRows; r0 += 16) {
                             uint32_t bits = 0;
                             for (int r = r0; r < r0 + 16; ++r) {
-                                const int pos = u.ctx + map.token(min(r, rows - 1)), last = min(pos - key0, kKeys - 1);
+                                const int pos = u.ctx + map.token(min(r, rows - 1));
                                 if constexpr (WIN) {
-                                    // bits [0, n) of the chunk
-                                    auto below = [](int n) { return n <= 0 ? 0ull : n >= kKeys ? ~0ull : (1ull << n) - 1; };
-                                    const uint64_t seen =
-                                        below(last + 1) & (~below(pos - see.window + 1 - key0) | below(see.sinks - key0));
+                                    const uint64_t seen = see.bits(pos, key0);
                                     const bool plus = odd[0] & seen, minus = odd[1] & seen;
                                     acc = (odd[2] & seen) || (plus && minus) ? NAN : plus ? INFINITY : minus ? -INFINITY : 0.f;
                                 } else {
-                                    while (key <= last) next();
+                                    while (key <= min(pos - key0, kKeys - 1)) next();
                                 }
                                 bits |= (acc != acc ? 3u : acc == INFINITY ? 1u : acc == -INFINITY ? 2u : 0u) << (2 * (r - r0));
                             }
@@ -1050,11 +1087,14 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
             __builtin_amdgcn_sched_barrier(0);
             // st[kt][i] = S^T[key 32 kt + 8 (i / 4) + 4 hb + i % 4][row r32]
             if (key0 + kKeys - 1 > wfirst || see.cuts(wlast, key0, kKeys)) {
+                const uint64_t seen = WIN ? see.bits(qpos, key0) >> (4 * hb) : 0;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!see.key(qpos, key0 + 32 * kt + 8 * (i / 4) + 4 * hb + i % 4)) st[kt][i] = -INFINITY;
+                    for (int i = 0; i < 16; ++i) {
+                        const int k = 8 * (i / 4) + i % 4;
+                        if (WIN ? !((uint32_t)(seen >> (32 * kt)) >> k & 1) : key0 + 32 * kt + 4 * hb + k > qpos) st[kt][i] = -INFINITY;
+                    }
             }
             float mx = -INFINITY;
 #pragma unroll
@@ -1100,19 +1140,19 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
         l += __shfl_xor(l, 32);
         const int row = 32 * w + r32;
         if (row < rows) {
-            const size_t pr = (size_t)(u.part + row) * p.n_kv + h;
+            const size_t pr = (size_t)(part + row) * p.n_kv + h;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const f32x4 x = f32x4{o[dt][i], o[dt][i + 1], o[dt][i + 2], o[dt][i + 3]};
                     const int col = 32 * dt + 8 * (i / 4) + 4 * hb;
-                    if (u.part >= 0)
+                    if (part >= 0)
                         *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = x;
                     else
                         store_row<Prec::BF16>(p, u.r0 + token, head, col, x, M, l);
                 }
-            if (u.part >= 0 && hb == 0) {
+            if (part >= 0 && hb == 0) {
                 p.part_m[pr] = M;
                 p.part_l[pr] = l;
             }

@@ -499,7 +499,8 @@ cllm_status attend(cllm_paged *c, const void *q, int64_t q_stride, const void *k
     const int64_t most = (int64_t)c->max_new * c->group, spans = (c->max_len + kPagedSpanKeys - 1) / kPagedSpanKeys;
     int64_t units = pieces(c->tiled ? std::min<int64_t>(most, kPagedFewRows) : most, c->block_rows);
     units = std::min(units * spans, units + kPagedUnits / f.n_kv_heads + 1);
-    int64_t tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
+    const int64_t whole_tiles = c->tiled && most > kPagedFewRows ? pieces(most, kPagedTileRows) : 0;
+    int64_t tiles = whole_tiles;
     tiles = std::min(tiles * spans, tiles + 2 * (kPagedTileGroups / f.n_kv_heads + 1));
     // whether a plan of these bounds may have whole requests: any plan, as a graph of this call may run behind one of
     // more requests
@@ -514,6 +515,13 @@ cllm_status attend(cllm_paged *c, const void *q, int64_t q_stride, const void *k
     // a block's tokens end in at most block_rows positions; the window of the first begins anywhere in a span
     const int64_t reach = (int64_t)window + std::min(c->max_new, c->block_rows) - 1;
     const int64_t sink_spans = (p.sinks + kPagedSpanKeys - 1) / kPagedSpanKeys;
+    // Tiles are split to fill the device, for which their partial states are written and joined. Behind a window that pays less, and
+    // the less the more tiles there are and the wider the heads: with tiles for half the device never at heads of 128 or more
+    // (384 of heads of 128 that see 8 chunks: 53 us split, 43 not; 34 chunks: 104 and 98), else above about so many chunks (128 of
+    // heads of 128, 5 chunks: 28.1 and 23.5, 14: 33.9 and 36.5; 125 of 256, 10: 96.7 and 69.9, 18: 118 and 103; 24 of 256, 5: 53.8 and
+    // 47.6, 8: 53.8 and 55.5; 264 of 64, 8: 26.8 and 25.9, 14: 34.0 and 36.1; 80 of 64, 5: 20.1 and 22.2).
+    const int64_t groups = whole_tiles * f.n_kv_heads;
+    p.whole_chunks = groups >= kPagedTileGroups / 2 && f.head_dim >= 128 ? INT32_MAX : (int)std::min<int64_t>(groups * f.head_dim / 2048, INT32_MAX);
     p.spans = (int)std::min(spans, (reach + kPagedSpanKeys - 1) / kPagedSpanKeys + 1 + sink_spans);
     HIPCHK(c, launch_paged_attn_window(c->bf16, c->n, most, whole, tiles, spans > 1, p, c->stream));
     return CLLM_OK;
