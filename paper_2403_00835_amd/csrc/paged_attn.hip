@@ -1240,15 +1240,28 @@ struct WindowCall {
                            4 * Tile<HD>::BYTES, s, p, 0);
         return hipGetLastError();
     }
+    // Whether requests of up to kPagedFewRows rows are all taken whole, whatever the plan made of them, with nothing else to
+    // launch: one workgroup a request and key head, which walks the chunks that it sees (2.2 us each at heads of 128, 512
+    // workgroups at a time), in place of one a block and span (about 12 us, 512 at a time), of which several work on a
+    // request at once, and a join. us of a call at 4096 keys behind 16 / 256 / 1024, in spans and whole:
+    //   32 heads over 8 of 128: 1 x 64 requests 26.4 / 34.6 / 75.9 and 18.2 / 25.4 / 58.8; 1 x 16: 12.9 / 15.8 / 25.8 and 13.4 /
+    //   20.6 / 46.5; 16 x 32: 35.9 / 54.2 / 98.3 and 16.4 / 25.3 / 53.2; 16 x 8: 15.4 / 21.0 / 34.0 and 12.2 / 21.5 / 48.3
+    //   32 heads of 128: 32 x 1: 13.6 / 16.5 / 17.8 and 13.6 / 20.3 / 47.3; 8 heads of 64: 24 x 22: 14.2 / 22.9 / 31.1 and 10.8 / 17.4 /
+    //   37.4; 4 over 2 of 256: 16 x 16: 17.4 / 21.7 / 36.4 and 23.1 / 35.5 / 85.0
+    bool all_whole(const PagedAttnParams &p) const {
+        if (most > kPagedFewRows) return false;
+        const int64_t groups = (int64_t)n * p.n_kv, blocks = (most + 16 * RG - 1) / (16 * RG), slots = (HD <= 128 ? 2 : 1) * kCUs;
+        const double keys = std::min<double>((double)p.window + p.max_new - 1, p.max_len);
+        const double chunks = keys / kKeys + 1 + (p.sinks + kKeys - 1) / kKeys;
+        const double spans = keys / kPagedSpanKeys + 1 + (p.sinks + kPagedSpanKeys - 1) / kPagedSpanKeys;
+        const double chunks_of_a_span = (most <= kPagedWaveRows ? 4 : 6) * (HD <= 64 ? 4.0 / 3 : HD <= 128 ? 1 : 2.0 / 3);
+        return chunks * std::max(groups, slots) <= chunks_of_a_span * spans * (blocks * groups);
+    }
     hipError_t operator()(const PagedAttnParams &call, hipStream_t s) const {
         constexpr int ROWS = 16 * RG;
         PagedAttnParams p = call;
         if constexpr (P == Prec::BF16) {
-            // Blocks of up to kPagedFewRows rows on enough workgroups: all are taken whole, whatever the plan made of them (one
-            // far longer context, for which it would split them, is no longer than the others behind a window), and there is
-            // nothing else to launch. 16 of 32 rows at 800 to 4000 keys behind 1024 (32 heads of 128): 80.0 us with a span
-            // kernel and a join that find nothing to do, 67.7 without.
-            p.all_whole = most > kPagedWaveRows && most <= kPagedFewRows && n * p.n_kv >= kPagedTileGroups;
+            p.all_whole = all_whole(p);
             if (p.all_whole) return launch_requests(p, s);
         }
         p.blocks = (int)((std::min<int64_t>(most, P == Prec::BF16 ? kPagedFewRows : most) + ROWS - 1) / ROWS);

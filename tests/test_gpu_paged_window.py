@@ -214,6 +214,52 @@ def test_many_requests_of_a_block_each(binding, heads, kv, hd, page, n, lo, hi, 
         assert (np.abs(host(o) - want) <= tol).all() and (np.abs(host(ls) - wl) <= tl).all()
 
 
+@pytest.mark.parametrize("heads,kv,hd,page,n,hi", [(32, 8, 128, 16, 64, 1), (32, 4, 64, 64, 40, 2), (8, 8, 128, 32, 30, 64), (6, 2, 32, 16, 70, 9),
+                                                   (16, 8, 256, 64, 40, 16), (64, 64, 64, 16, 9, 20)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 4), (200, 70), (600, 300)])
+def test_few_rows_give_the_same_bits_alone_and_beside_others(binding, heads, kv, hd, page, n, hi, window, sinks):
+    """Requests of few rows with bounds that say so, with values that are not finite where some rows see them: many of them, which a
+    workgroup each takes, give the bits that each has alone, where spans share it; and so in a graph of one plan behind another."""
+    rng = random.Random(n + window)
+    new, ctx = [rng.randint(1, hi) for _ in range(n)], [rng.randint(0, 900) for _ in range(n)]
+    new[2], new[4], ctx[4], ctx[5] = 0, hi, 0, 256
+    total = [a + b for a, b in zip(ctx, new)]
+    n_pages = sum(-(-t // page) for t in total)
+    R, bounds = sum(new), dict(max_new=hi, max_len=max(total))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c = make(binding, page=page, n_pages=n_pages, max_seqs=n, max_ctx=max(total), max_rows=R, heads=heads, kv=kv, hd=hd)
+        g = torch.Generator(device="cuda").manual_seed(n)
+        kp, vp = (torch.randn(c.pool_shape, generator=g, device="cuda").bfloat16() for _ in range(2))
+        q = (torch.randn(R, heads, hd, generator=g, device="cuda") * 1.5).bfloat16()
+        plan = lambda k, rows: c.plan(ints(list(range(k))), ints(ctx[:k]), ints(new[:k]), rows=rows, **bounds)
+        plan(n, R)
+        for s in (3, n - 1):  # (some rows see it, and the first ones of a block may not)
+            vp[int(c.block_table[s, max(ctx[s] - window // 2, 0) // page]), :, 3, 7 + s % 2] = float("nan") if s == 3 else float("inf")
+        kw = dict(window=window, sinks=sinks)
+        out, lse = run(c, q, kp, vp, **kw)
+        assert c.status()[0] == R
+        start = np.concatenate([[0], np.cumsum(new)])
+        for s in range(0, n, 1 if n < 32 else 3):
+            at = slice(start[s], start[s + 1])
+            c.plan(ints([s]), ints([ctx[s]]), ints([new[s]]), rows=new[s], max_len=max(total))
+            o, ls = run(c, q[at], kp, vp, **kw)
+            assert torch.equal(o.view(torch.int16), out[at].view(torch.int16)) and torch.equal(ls, lse[at])
+        plan(n // 2, R)
+        again = torch.empty_like(q)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.attn(q, kp, vp, again, **kw)
+        for k in (n // 2, n, 1, n):
+            plan(k, R)
+            again.fill_(7)
+            graph.replay()
+            assert c.status()[0] == start[k]
+            assert torch.equal(again[:start[k]].view(torch.int16), out[:start[k]].view(torch.int16)) and (again[start[k]:] == 7).all()
+        del graph
+
+
 @pytest.mark.parametrize("dtype,heads,kv,hd,ctx,m,n", [
     ("bf16", 4, 4, 128, 500, 40, 1), ("bf16", 8, 2, 64, 70, 16, 1), ("bf16", 8, 8, 64, 500, 40, 66), ("bf16", 4, 2, 128, 120, 90, 1),
     ("bf16", 1, 1, 256, 300, 130, 1), ("bf16", 2, 2, 32, 0, 200, 1), ("f32", 2, 2, 64, 60, 30, 1), ("f32", 2, 1, 16, 300, 40, 1)])
