@@ -133,7 +133,9 @@ struct PagedAttnParams {
     uint32_t group_inv;           // 2^24 / group, rounded up
     float scale_log2;
     int window, sinks;            // of the calls with a window: a row sees its last `window` tokens and the first `sinks`
-    int whole_chunks;            // tiles that see no more chunks are not split
+    int cap_part;                 // partial rows of row blocks that the cache holds
+    bool split;                   // (fp32) spans have partial states
+    int whole_chunks;             // tiles that see no more chunks are not split
     bool all_whole;               // every block is taken whole
     int spans, blocks;            // the most spans that a row block of such a call sees, the most row blocks of a request
 };

@@ -297,9 +297,17 @@ __device__ __forceinline__ bool next_entry(const PagedAttnParams &p, int i, Page
     return R > 0 && i < n;
 }
 
+// Partial row of a request's first row in the first span that it sees, or -1: the plan's place; in fp32 one of the call's own
+// (p.split: p.spans for every row of the plan), as the plan has none for more rows than it finds room for in all their spans.
+template <Prec P>
+__device__ __forceinline__ int window_part(const PagedAttnParams &p, const PagedEntry &e) {
+    if (P == Prec::BF16) return e.part;
+    return p.split ? p.spans * p.group * e.r0 : -1;
+}
+
 // What a workgroup of the span kernel takes, one after another: the plan's units; behind a window, of block x of every
 // gridDim.z-th request the y-th span that the block sees (all of them where the request has no partial states).
-template <int ROWS, bool WIN>
+template <Prec P, int ROWS, bool WIN>
 struct SpanUnits {
     int idx = blockIdx.x, z = blockIdx.z, count = 0;
     __device__ __forceinline__ bool next(const PagedAttnParams &p, int cap, PagedUnit &u, int &h) {
@@ -313,10 +321,10 @@ struct SpanUnits {
             PagedEntry e;
             while (next_entry(p, z, e, count)) {
                 z += gridDim.z;
-                const int j = blockIdx.y, row = idx / p.n_kv * ROWS;
-                if (e.kind != PE_BLOCKS || row >= e.m * p.group || (e.part < 0 && j > 0)) continue;
-                u = PagedUnit{e.slot, e.ctx, e.m, e.r0, row, j, e.part < 0 ? kAllSpans : j + 1,
-                              e.part < 0 ? -1 : e.part + j * e.m * p.group + row};
+                const int j = blockIdx.y, row = idx / p.n_kv * ROWS, part = window_part<P>(p, e);
+                if (e.kind != PE_BLOCKS || row >= e.m * p.group || (part < 0 && j > 0)) continue;
+                u = PagedUnit{e.slot, e.ctx, e.m, e.r0, row, j, part < 0 ? kAllSpans : j + 1,
+                              part < 0 ? -1 : part + j * e.m * p.group + row};
                 h = idx % p.n_kv;
                 return true;
             }
@@ -691,7 +699,7 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
     uint8_t *s_mine = s_all + (size_t)w * REGION;
     int h;
     PagedUnit u;
-    for (SpanUnits<ROWS, WIN> units; units.next(p, cap_units, u, h);) {
+    for (SpanUnits<P, ROWS, WIN> units; units.next(p, cap_units, u, h);) {
         if (!WIN && u.k0 < 0) continue;  // a whole request's (uniform)
         const int rows = min(ROWS, u.m * p.group - u.row);
         const RowMap map(p, u.row);
@@ -1166,6 +1174,16 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
 template <Prec P, int HD, bool WIN>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p, int cap_items) {
     constexpr int LPR = HD / 4, RPW = 256 / LPR, NG = (kPagedItemRows + RPW - 1) / RPW;
+    if constexpr (WIN && P == Prec::F32) {  // the call's own places: by requests
+        PagedEntry e;
+        for (int z = blockIdx.z, n; next_entry(p, z, e, n); z += gridDim.z)
+            for (int i = blockIdx.x; i / (p.n_kv * NG) * kPagedItemRows < e.m * p.group; i += gridDim.x) {
+                const int row = i / (p.n_kv * NG) * kPagedItemRows;
+                const PagedItem mine{e.ctx, e.m, e.r0, row, window_part<P>(p, e) + row, e.m * p.group, 0, 0};
+                join_row<P, HD, WIN>(p, mine, i % p.n_kv, i / p.n_kv % NG * RPW + threadIdx.x / LPR, threadIdx.x % LPR * 4);
+            }
+        return;
+    }
     const int32_t *st = p.bk.status;
     const int R = st[PS_ROWS], n = st[PS_ITEMS], br = st[PS_BOUND_ROWS], bn = st[PS_BOUND_NEW], bl = st[PS_BOUND_LEN];
     PagedItem it = p.bk.items[min((int)blockIdx.x / (p.n_kv * NG), cap_items - 1)];
@@ -1265,7 +1283,8 @@ struct WindowCall {
             if (p.all_whole) return launch_requests(p, s);
         }
         p.blocks = (int)((std::min<int64_t>(most, P == Prec::BF16 ? kPagedFewRows : most) + ROWS - 1) / ROWS);
-        const dim3 grid((unsigned)std::min(p.blocks * p.n_kv, 1 << 20), (unsigned)p.spans, (unsigned)n);
+        if (P == Prec::F32) p.split = p.spans > 1 && split(p);
+        const dim3 grid((unsigned)std::min(p.blocks * p.n_kv, 1 << 20), P == Prec::F32 && !p.split ? 1u : (unsigned)p.spans, (unsigned)n);
         hipLaunchKernelGGL((paged_span_kernel<P, HD, RG, true>), grid, dim3(kSpanChunks * kWave),
                            kSpanChunks * (span_wave_lds<P, HD, RG>()), s, p, 0);
         hipError_t e = hipGetLastError();
@@ -1273,7 +1292,22 @@ struct WindowCall {
             if (e == hipSuccess && whole) e = launch_requests(p, s);
             if (e == hipSuccess && tiles > 0) e = launch_tiles<HD, true>(tiles, p, s);
         }
+        if constexpr (P == Prec::F32) {
+            if (e != hipSuccess || !p.split) return e;
+            const int64_t work = (most + kPagedItemRows - 1) / kPagedItemRows * p.n_kv * ((kPagedItemRows + 1024 / HD - 1) / (1024 / HD));
+            hipLaunchKernelGGL((paged_join_kernel<P, HD, true>), dim3((unsigned)std::min<int64_t>(work, 8 * kCUs), 1, (unsigned)n), dim3(256),
+                               0, s, p, p.bk.cap_items);
+            return hipGetLastError();
+        }
         return e == hipSuccess && join ? launch_join<P, HD, true>((int64_t)n * p.blocks, tiles, p, s) : e;
+    }
+    // fp32: whether a block's spans are worked on side by side and joined, or one after another: where the blocks alone take two thirds
+    // of the device, the join and the partial states cost what the spans side by side save. us of a call behind 6 / 600 / 2000 keys, side by
+    // side and one after another: 2 heads over 1 of 64, 54 tokens (4 workgroups) 16.2 / 17.8 / 96.6 (no room) and 20.9 / 40.6 / 96.9; 28 tokens
+    // of 4 over 1 of 128 (28) 17.1 / 21.1 / 32.7 and 27.7 / 52.2 / 110; 2 x 300 of 8 of 32 (160) 13.3 / 30.9 / 61.5 and 18.4 / 31.2 / 61.5;
+    // 22 x 50 of 4 of 64 (176) 28.3 / 52.3 / 93.6 and 28.6 / 50.4 / 102; 3 x 150 of 8 of 128 (240) 30.8 / 63.3 / 118 and 27.9 / 54.5 / 118.
+    bool split(const PagedAttnParams &p) const {
+        return (int64_t)p.spans * p.rows * p.group <= p.cap_part && 3 * (int64_t)n * p.blocks * p.n_kv <= 2 * kCUs;
     }
 };
 

@@ -511,6 +511,7 @@ cllm_status attend(cllm_paged *c, const void *q, int64_t q_stride, const void *k
         return CLLM_OK;
     }
     p.window = window;
+    p.cap_part = c->cap_part;
     p.sinks = std::min(sinks, c->max_len);
     // a block's tokens end in at most block_rows positions; the window of the first begins anywhere in a span
     const int64_t reach = (int64_t)window + std::min(c->max_new, c->block_rows) - 1;
