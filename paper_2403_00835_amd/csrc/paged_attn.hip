@@ -785,7 +785,8 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
 // Bound: reading the cache, one chunk of 32 KiB a workgroup (head_dim 128, two a CU) ahead. 64 requests of 36
 // rows at 4000 keys, 8 key heads: 205 us, 5.1 TB/s. 16 ragged requests of 32 rows at 256 to 1280 keys, 32
 // heads: 218 MB in 49 us. The unit list is the span kernel's, and each passes over the other's units.
-// Behind a window (WIN) it walks the plan's requests.
+// Behind a window (WIN) it walks the plan's requests. 64 of four rows at 2000 to 32000 keys behind 4096, 8 key heads: 1057 MB in
+// 189 us, 5.6 TB/s.
 template <int HD, bool WIN>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_request_kernel(PagedAttnParams p, int cap_units) {
     constexpr Prec P = Prec::BF16;
