@@ -1002,7 +1002,8 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                 // request's last token are cleared, whatever the page holds there; others that are not
                 // finite (rare) are taken out, and what the rows that see them get from them is added to
                 // their outputs: a sum per row and column, as a class of two bits (0, +inf, -inf, NaN).
-                bool bad = false;
+                typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+                u16x2 size{};  // the largest magnitudes, as bits
 #pragma unroll
                 for (int i = 0; i < TL::BYTES / 16 / 256; ++i) {
                     u32x4 *v = reinterpret_cast<u32x4 *>(V) + tid + 256 * i;
@@ -1012,10 +1013,10 @@ __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kerne
                         const u32x4 x = *v;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+                            size = __builtin_elementwise_max(size, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
                     }
                 }
-                if (any_of_workgroup(bad, s_bad)) {
+                if (any_of_workgroup(max(size[0], size[1]) >= 0x7f80, s_bad)) {
                     for (int col = tid; col < HD; col += 256) {
                         float acc = 0.f;
                         int key = 0;
