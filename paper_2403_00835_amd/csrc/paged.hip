@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
     using PT = PrecT<PR>;
     using T = typename PT::T;
     constexpr int VEC = PT::VEC, H = VEC / 2;
-    __shared__ float s_pairs[F == SCATTERED ? 256 * 2 * VEC : 1];
+    __shared__ float s_pairs[F == SCATTERED ? 256 * 2 * (VEC + 1) : 1];
     const int R = bounded_rows(p.bk, p.rows, p.max_new, p.max_len);
     const int nv = p.hd / 2 / VEC, nv_shift = 31 - __clz(nv), half = p.hd / 2;
     const int q_segs = p.q ? (p.n_heads + U - 1) / U : 0, kv_segs = (p.n_kv + U - 1) / U;
@@ -479,28 +479,16 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
             auto is_turned = [&](int i) { return (i < H ? j0 + i : j1 + i - H) < p.rot; };
             if (turned) {
                 const size_t t = (size_t)p.bk.row_pos[r] * p.rot;
-                auto factors = [&](int j, int first) {
+                // (Those behind the row's last are not used; the table has hd / 2 for each position, so they are in it.)
+                float a[H], b[H];
+                load_floats(a, p.rcos + t + j0);
+                load_floats(b, p.rsin + t + j0);
 #pragma unroll
-                    for (int i = 0; i < H; ++i) {  // (a vector load where all are turned)
-                        const size_t k = t + min(j + i, p.rot - 1);
-                        c[first + i] = p.rcos[k];
-                        s[first + i] = p.rsin[k];
-                    }
-                };
-                if (F == HALVES || j1 + H <= p.rot) {
-                    float a[H], b[H];
-                    load_floats(a, p.rcos + t + j0);
-                    load_floats(b, p.rsin + t + j0);
+                for (int i = 0; i < H; ++i) c[i] = a[i], s[i] = b[i];
+                load_floats(a, p.rcos + t + j1);
+                load_floats(b, p.rsin + t + j1);
 #pragma unroll
-                    for (int i = 0; i < H; ++i) c[i] = a[i], s[i] = b[i];
-                    load_floats(a, p.rcos + t + j1);
-                    load_floats(b, p.rsin + t + j1);
-#pragma unroll
-                    for (int i = 0; i < H; ++i) c[H + i] = a[i], s[H + i] = b[i];
-                } else {
-                    factors(j0, 0);
-                    factors(j1, H);
-                }
+                for (int i = 0; i < H; ++i) c[H + i] = a[i], s[H + i] = b[i];
             }
             if (gain || turned) {
 #pragma unroll
@@ -527,41 +515,40 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
                         for (int i = 0; i < 2 * VEC; ++i) y[i] = y[i] * f * g[i];
                     }
                     if constexpr (F == SCATTERED) {
-                        // The head's elements into LDS, this thread's pairs at .. out of it and back turned. A head's threads are
-                        // in one wave, whose accesses to LDS are in order.
-                        float *mine = s_pairs + (threadIdx.x & ~(nv - 1)) * 2 * VEC;
-                        auto vectors = [&](bool out) {
-#pragma unroll
-                            for (int i = 0; i < 2 * VEC; i += 4) {
-                                f32x4 &l = *reinterpret_cast<f32x4 *>(mine + (i < VEC ? at + i : half + at + i - VEC));
-                                if (out) {
-                                    l = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
-                                } else {
-                                    const f32x4 v = l;
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) y[i + e] = v[e];
-                                }
-                            }
-                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        // The head's elements into LDS; out of it the partners of this thread's first elements, and back turned;
+                        // then what others have turned. A head's threads are in one wave, whose accesses to LDS are in order.
+                        // (A place is left free behind each vector, or all threads' elements would be in the same few banks.)
+                        float *mine = s_pairs + (threadIdx.x & ~(nv - 1)) * 2 * (VEC + 1);
+                        const uint32_t first = at / VEC * (VEC + 1), second = first + nv * (VEC + 1);
+                        auto other = [&](int i) {
+                            const uint32_t e = min(at + i, p.rot - 1) + p.rot;
+                            return e + e / VEC;
                         };
                         if (turned) {
                             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                            vectors(true);
-                            float a[VEC], b[VEC];
 #pragma unroll
                             for (int i = 0; i < VEC; ++i) {
-                                const int j = min(at + i, p.rot - 1);
-                                a[i] = mine[j];
-                                b[i] = mine[j + p.rot];
+                                mine[first + i] = y[i];
+                                mine[second + i] = y[VEC + i];
                             }
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                            float b[VEC];
+#pragma unroll
+                            for (int i = 0; i < VEC; ++i) b[i] = mine[other(i)];
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
                             for (int i = 0; i < VEC; ++i)
                                 if (at + i < p.rot) {
-                                    mine[at + i] = a[i] * c[i] - b[i] * s[i];
-                                    mine[at + i + p.rot] = b[i] * c[i] + a[i] * s[i];
+                                    mine[other(i)] = b[i] * c[i] + y[i] * s[i];
+                                    y[i] = y[i] * c[i] - b[i] * s[i];
                                 }
                             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                            vectors(false);
+#pragma unroll
+                            for (int i = 0; i < VEC; ++i) {
+                                const float x = mine[first + i], own = y[i];
+                                y[i] = at + i < p.rot ? own : x;
+                                y[VEC + i] = mine[second + i];
+                            }
                         }
                     } else if (turned) {
 #pragma unroll
