@@ -421,9 +421,10 @@ enum Pairs {
 // paged_append_kernel with a norm of each query and key head before the rotation, and every form of the rotation:
 // y = x / sqrt(mean(x^2) + eps) * gain in fp32, then the turned pairs, rounded once. A thread takes U heads of one
 // row, whose rotary factors and gains it loads once.
-// Bound: memory: 8000 rows of 32 and 8 heads of 128, 197 MB in 43.6 us, 4.5 TB/s where nothing is in the last-level cache
-// (paged_append_kernel there: 39); 512 rows 6.1 us, 8 rows of 12 heads of 16 3.5. Halves of other widths element by element
-// from memory took 18.8 us in place of 10.2 (2000 rows of 36 heads of 64, 24 elements turned).
+// Bound: memory: 8000 rows of 32 and 8 heads of 128, 197 MB in 42.5 us, 4.6 TB/s where nothing is in the last-level cache
+// (paged_append_kernel there: 39); 512 rows 6.0 us, 8 rows of 12 heads of 16 3.4. Halves of other widths (1740 rows of 36 heads of
+// 64, 24 elements turned: 9.0 us): element by element from memory 18.8; all elements through LDS as vectors, with the threads'
+// reads in few banks, 10.2.
 template <Prec PR, Pairs F, int U>
 __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendParams p, int per_row, uint32_t per_row_inv, int rpb) {
     using PT = PrecT<PR>;
@@ -614,9 +615,14 @@ template <Prec PR>
 hipError_t launch_forms(const PagedAppendParams &p, hipStream_t s) {
     // Two heads a thread, whose factors and gains are loaded once, where one a thread makes more workgroups than run at once
     // (48 heads of 128, bf16: 512 rows 6.1 us in place of 7.1, 8000 rows 43.6 in place of 50.5, four heads a thread 42.5; 8 rows
-    // of 12 heads of 16, fp32: 3.5 either way); halves through LDS are no faster (2000 rows of 36 heads of 64: 10.2, two 11.4).
+    // of 12 heads of 16, fp32: 3.5 either way); halves through LDS in bf16 alone (13,800 rows of 12 heads of 128, 126 elements
+    // turned: 23.9 in place of 27.3; 6300 rows of 32 heads of 64, 22 turned, fp32: 24.2 in place of 22.0).
     const bool many = p.rows >= 256;
-    if (p.rot > 0 && !p.inter && p.rot % PrecT<PR>::VEC != 0) return launch_forms<PR, SCATTERED, 1>(p, s);
+    if (p.rot > 0 && !p.inter && p.rot % PrecT<PR>::VEC != 0) {
+        if constexpr (PR == Prec::BF16)
+            if (many) return launch_forms<PR, SCATTERED, 2>(p, s);
+        return launch_forms<PR, SCATTERED, 1>(p, s);
+    }
     if (p.inter || p.rot == 0) return many ? launch_forms<PR, NEIGHBOURS, 2>(p, s) : launch_forms<PR, NEIGHBOURS, 1>(p, s);
     return many ? launch_forms<PR, HALVES, 2>(p, s) : launch_forms<PR, HALVES, 1>(p, s);
 }

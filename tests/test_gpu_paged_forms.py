@@ -75,7 +75,13 @@ FORMS = [  # dtype, heads, kv heads, head dim, page, contexts, new tokens, rotar
     # several rows a workgroup, the last one of fewer; two heads a thread, the last one of one
     ("f32", 32, 8, 64, 64, [0, 10], [4000, 101], dict(layout="half", dim=48), (True, True)),
     ("bf16", 9, 3, 64, 64, [40, 0], [200, 101], dict(layout="half", dim=48), (True, True)),
-    ("bf16", 5, 5, 128, 64, [40, 0], [300, 1], dict(layout="interleaved", dim=100), (True, False))]
+    ("bf16", 5, 5, 128, 64, [40, 0], [300, 1], dict(layout="interleaved", dim=100), (True, False)),
+    # pairs of other halves, two heads a thread, from a part of the first vector to all but the last pair
+    ("bf16", 9, 3, 64, 16, [40, 0], [300, 9], dict(layout="half", dim=20), (True, True)),
+    ("bf16", 7, 7, 256, 64, [3], [260], dict(layout="half", dim=250), (False, True)),
+    ("bf16", 3, 1, 32, 16, [0, 7], [280, 1], dict(layout="half", dim=30), (False, False)),
+    ("bf16", 4, 4, 128, 32, [100], [257], dict(layout="half", dim=126, magnitude=0.5), (True, False)),
+    ("f32", 5, 1, 128, 32, [100], [300], dict(layout="half", dim=6), (True, True))]
 
 
 @pytest.mark.parametrize("case", FORMS, ids=range(len(FORMS)))
