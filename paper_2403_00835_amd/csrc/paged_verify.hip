@@ -199,37 +199,74 @@ __device__ __forceinline__ int wave_min(int x) {
     return x;
 }
 
-// A row's distribution from the statistics of its chunks, by one wave. head: of chunk `lane`, where there is one.
+// The same over LANES lanes (all of a wave, or 16 neighbours), in each of them.
+template <int CTRL, class T>
+__device__ __forceinline__ T traded(T x) {
+    return moved<CTRL, 0xf>(x, x);
+}
+template <int LANES, class T, class F>
+__device__ __forceinline__ T group_all(T x, F f) {
+    static_assert(LANES == 16, "lanes whose sums are lane moves of a row");
+    x = f(x, traded<0xb1>(x));   // lane ^ 1
+    x = f(x, traded<0x4e>(x));   // lane ^ 2
+    x = f(x, traded<0x141>(x));  // 8 lanes mirrored
+    return f(x, traded<0x140>(x));  // 16 lanes mirrored
+}
+template <int LANES>
+__device__ __forceinline__ float group_max(float x) {
+    if constexpr (LANES == kWave) return wave_max(x);
+    else return group_all<LANES>(x, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LANES>
+__device__ __forceinline__ double group_sum(double x) {
+    if constexpr (LANES == kWave) return wave_sum(x);
+    else return group_all<LANES>(x, [](double a, double b) { return a + b; });
+}
+template <int LANES>
+__device__ __forceinline__ int group_min(int x) {
+#pragma unroll
+    for (int off = LANES / 2; off >= 1; off >>= 1) x = min(x, __shfl_xor(x, off));
+    return x;
+}
+template <int LANES>
+__device__ __forceinline__ bool group_any(bool x) {
+    if constexpr (LANES == kWave) return __any(x);
+    else return __ballot(x) >> (threadIdx.x & (kWave - LANES)) & ((1ull << LANES) - 1);
+}
+
+// A row's distribution from the statistics of its chunks, by LANES lanes (LANES < 64: at most so many chunks). head: of the
+// lane's first chunk, where there is one.
 struct Law {
     float max;    // what weights are relative to: the largest of its chunks' (greedy requests: the largest logit)
     double norm;  // 1 / the sum of the weights
     int top;      // greedy requests: the largest logit's lowest index
     bool ok;      // neither NaN nor +inf among the logits, nor all -inf
 };
+template <int LANES>
 __device__ __forceinline__ Law row_law(const VerifyStat &head, const VerifyStat *st, int chunks, double scale, double floor, const double *table) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & (LANES - 1);
     constexpr VerifyStat kNone{0.0, -INFINITY, 0x7fffffff};
-    const VerifyStat mine = lane < chunks ? head : kNone;  // (the first 64 chunks: most vocabularies' all)
+    const VerifyStat mine = lane < chunks ? head : kNone;  // (the first chunks: most vocabularies' all)
     float m = mine.max;
     bool bad = m != m;
-    for (int c = lane + kWave; c < chunks; c += kWave) {
+    for (int c = lane + LANES; LANES == kWave && c < chunks; c += LANES) {
         const float x = st[c].max;
         bad |= x != x;
         m = fmaxf(m, x);
     }
-    Law w{wave_max(m), 0.0, 0x7fffffff, false};
-    w.ok = !__any(bad) && w.max > -INFINITY && w.max < INFINITY;
+    Law w{group_max<LANES>(m), 0.0, 0x7fffffff, false};
+    w.ok = !group_any<LANES>(bad) && w.max > -INFINITY && w.max < INFINITY;
     if (!w.ok) return w;
     if (scale > 0.0) {
         double sum = mine.sum * weight((double)mine.max - (double)w.max, scale, floor, table);
-        for (int c = lane + kWave; c < chunks; c += kWave)
+        for (int c = lane + LANES; LANES == kWave && c < chunks; c += LANES)
             sum += st[c].sum * weight((double)st[c].max - (double)w.max, scale, floor, table);
-        w.norm = inverse(wave_sum(sum));
+        w.norm = inverse(group_sum<LANES>(sum));
     } else {
         int top = mine.max == w.max ? mine.top : 0x7fffffff;
-        for (int c = lane + kWave; c < chunks; c += kWave)
+        for (int c = lane + LANES; LANES == kWave && c < chunks; c += LANES)
             if (st[c].max == w.max) top = min(top, st[c].top);
-        w.top = wave_min(top);
+        w.top = group_min<LANES>(top);
     }
     return w;
 }
@@ -253,16 +290,20 @@ __device__ __forceinline__ Request begin(const VerifyParams &p, int b, double (&
     return q;
 }
 
+// Up to so many chunks a wave decides on four rows at once: 18 requests of 14 to 44 rows of 12,233 tokens 27.5 us in place of 31.8, 16 of
+// 32 rows of 32,000 25.6 in place of 26.4.
+constexpr int kFewChunks = 16;
 struct Decide {  // LDS
-    VerifyStop at[kToken / kWave];
+    VerifyStop at[kToken / kFewChunks];
     int stop;
 };
 
-// Where a request stops, by the whole workgroup: a row a wave. heads (or null): statistics of the first 64 chunks of the row at
-// which it stops, in the entry of the row's wave.
-__device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Request &q, const double *table, Decide &s,
-                                             VerifyStat (*heads)[kWave]) {
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / kWave, first = q.first, end = q.end;
+// Where a request stops, by the whole workgroup: a row LANES lanes. heads (or null): statistics of the first LANES chunks of the row
+// at which it stops, in those lanes' places.
+template <int LANES>
+__device__ __forceinline__ VerifyStop decide_by(const VerifyParams &p, const Request &q, const double *table, Decide &s, VerifyStat *heads) {
+    const int rows = blockDim.x / LANES, first = q.first, end = q.end;  // (rows: at once)
+    const int slot = LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : (int)threadIdx.x / LANES;
     const double scale = q.scale, floor = q.floor;
     if (first >= end) {  // uniform
         VerifyStop none{};
@@ -270,7 +311,7 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
         return none;
     }
     if (threadIdx.x == 0) s.stop = end;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & (LANES - 1);
     struct Row {  // what a row's decision reads; the next one's is on its way beside this one's
         VerifyStat p, q;
         double u;
@@ -288,22 +329,22 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
         if (lane < p.chunks) next.q = p.stats[(size_t)(p.rows + r) * p.chunks + lane];
         next.lq = p.picked[p.rows + r];
     };
-    load(first + w);
+    load(first + slot);
     __syncthreads();
-    for (int r0 = first; r0 < end; r0 += waves) {
-        const int r = r0 + w;
+    for (int r0 = first; r0 < end; r0 += rows) {
+        const int r = r0 + slot;
         if (r < end) {
             const Row at = next;
-            load(r + waves);
+            load(r + rows);
             const bool drafted = r + 1 < end;
             const VerifyStat *st = p.stats + (size_t)r * p.chunks, *sq = p.stats + (size_t)(p.rows + r) * p.chunks;
             const int x = drafted ? at.x : -1;
             const bool known = x >= 0 && x < p.vocab;
             const double u = at.u;
             const float lp = at.lp, lq = at.lq;
-            const Law law = row_law(at.p, st, p.chunks, scale, floor, table);
+            const Law law = row_law<LANES>(at.p, st, p.chunks, scale, floor, table);
             Law lawq{0.f, 0.0, 0, false};
-            if (p.draft && drafted && scale > 0.0) lawq = row_law(at.q, sq, p.chunks, scale, floor, table);
+            if (p.draft && drafted && scale > 0.0) lawq = row_law<LANES>(at.q, sq, p.chunks, scale, floor, table);
             bool stands = false;
             if (law.ok && drafted && known) {
                 if (scale == 0.0) {
@@ -314,9 +355,10 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
                     stands = u * qx < px;
                 }
             }
-            if (!stands && heads) heads[w][lane] = at.p;
-            if (!stands && lane == 0) {
-                VerifyStop &stop = s.at[w];
+            if (!stands && heads) heads[threadIdx.x] = at.p;
+            const uint64_t ends = __ballot(!stands);
+            if (ends && (int)(threadIdx.x & 63) == __ffsll((unsigned long long)ends) - 1) {  // the wave's first that does
+                VerifyStop &stop = s.at[slot];
                 stop.p_norm = law.norm;
                 stop.q_norm = lawq.norm;
                 stop.p_max = law.max;
@@ -331,9 +373,12 @@ __device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Reques
             }
         }
         __syncthreads();
-        if (s.stop < r0 + waves) return s.at[s.stop - r0];  // uniform: the last row at the latest
+        if (s.stop < r0 + rows) return s.at[s.stop - r0];  // uniform: the last row at the latest
     }
     return VerifyStop{};  // (not reached)
+}
+__device__ __forceinline__ VerifyStop decide(const VerifyParams &p, const Request &q, const double *table, Decide &s, VerifyStat *heads) {
+    return p.chunks <= kFewChunks ? decide_by<kFewChunks>(p, q, table, s, heads) : decide_by<kWave>(p, q, table, s, heads);
 }
 
 // A chunk's sum relative to the logit `to` in place of `from`: by two factors, as the sum may be 2^900 and each factor 2^-1000. What
@@ -476,8 +521,8 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
 
 // Where the requests stop, and the sums of max(p - q, 0) over the chunks of the rows whose draft was refused: two chunks a
 // workgroup at a time, each of which decides for itself.
-// Bound: latency (what a decision reads, then a row's logits) and 64-bit arithmetic: one request of 32,000 tokens 6.1 us, 64
-// of 99,991 13.6, in 13 workgroups of two rounds each (25 of one round 16.4, 7 of four 17.1).
+// Bound: latency (what a decision reads, then a row's logits) and 64-bit arithmetic: one request of 32,000 tokens 5.6 us, 64
+// of 99,991 13.4, in 13 workgroups of two rounds each (25 of one round 16.4, 7 of four 17.1).
 constexpr int kRestChunks = kRest / kWave / kParts, kRestFit = 4;
 template <Prec PR>
 __global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
@@ -528,7 +573,7 @@ __global__ __launch_bounds__(kRest) void verify_rest_kernel(VerifyParams p) {
 
 // The accepted rows and the next token. Workgroup: a request.
 // Bound: latency, of three to five reads that wait for one another, each about 1 us: one request 4.7 us, 64 of 99,991 tokens
-// 6.0; where it decides, 16 of 32 rows, 7.8. Neighbours and waves in the tokens' order pick the token by ballots: atomics on
+// 6.0; where it decides, 16 of 32 rows, 6.2. Neighbours and waves in the tokens' order pick the token by ballots: atomics on
 // LDS for it, lane by lane, took 4.4 us more.
 template <Prec PR>
 __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
@@ -536,7 +581,7 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     static_assert(kDraw <= kToken && kDraw % kWave == 0, "whole waves");
     __shared__ double table[kExpSteps], s_sum[kDraw / kWave], s_aim;
     __shared__ Decide s_decide;
-    __shared__ VerifyStat s_heads[kToken / kWave][kWave];
+    __shared__ VerifyStat s_heads[kToken];
     __shared__ int s_from, s_chunk, s_found[kDraw / kWave], s_last[kDraw / kWave];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const double u = p.sample_u[b];
@@ -559,7 +604,7 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     // What is drawn from: the rest, p without the refused token, or p (also where those are empty).
     bool rest = at.kind & VS_REST;
     int without = !rest && (at.kind & VS_REFUSED) ? at.draft : -1;
-    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks, *head = s_heads[(at.row - at.first) % (kToken / kWave)];
+    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks, *head = s_heads + (p.chunks <= kFewChunks ? (at.row - at.first) * kFewChunks : (at.row - at.first) * kWave) % kToken;
     auto stat = [&](int c) { return p.draft || c >= kWave ? st[c] : head[c]; };
     double cut = 0.0;  // the sum of the refused token's chunk without it
     if (without >= 0) {

@@ -122,6 +122,23 @@ def test_where_a_long_request_over_many_chunks_stops(cache, stop, with_draft):
         assert a[1] == stop + 1 or with_draft
 
 
+@pytest.mark.parametrize("vocab", [5000, 32768])
+@pytest.mark.parametrize("with_draft", [False, True])
+def test_where_a_longer_request_over_few_chunks_stops(cache, vocab, with_draft):
+    """Rows of a wave's four, of any wave and any turn, greedy and not."""
+    rng = random.Random(vocab)
+    start, tokens, x, draft, _, au, su = problem(rng, [1, 150, 2], vocab, with_draft)
+    base = x.copy()
+    for stop in (0, 1, 31, 32, 63, 64, 67, 130, 148, 149):
+        x[:] = base
+        for r in range(1, 150):
+            x[r, tokens[r + 1]] = 25.0 if r < 1 + stop else -25.0
+        for t in (0.0, 0.7):
+            a, _ = check(cache, start, tokens, place(x, torch.bfloat16, 0, 0), None if draft is None else place(draft, torch.bfloat16, 0, 0),
+                         [1.0, t, 0.0], au, su)
+            assert a[1] == stop + 1 or with_draft and t
+
+
 def test_the_drawn_tokens_have_the_targets_law(cache):
     """1024 requests of two rows at a time, all of one p and q: the first token that stands or is drawn is distributed as p, within five
     standard deviations of each count."""
