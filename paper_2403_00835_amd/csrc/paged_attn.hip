@@ -689,7 +689,7 @@ struct ChunkLoads {
 template <Prec P, int HD, int RG, bool WIN>
 __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ? 2 : 1) void paged_span_kernel(PagedAttnParams p,
                                                                                                   int cap_units) {
-    constexpr bool WHOLE = P == Prec::F32;  // several spans without partials
+    constexpr bool WHOLE = P == Prec::F32 && !WIN;  // several spans without partials
     constexpr int NW = kSpanChunks, REGION = span_wave_lds<P, HD, RG>(), SROW = HD + 4, ROWS = 16 * RG;
     constexpr int ITEMS = (ROWS * HD / 4 + NW * kWave - 1) / (NW * kWave);
     extern __shared__ u32x4 s_raw[];
@@ -709,6 +709,75 @@ __global__ __launch_bounds__(kSpanChunks * kWave, P == Prec::BF16 && HD <= 128 ?
         const Visible<WIN, kPagedSpanKeys> spans(see, WIN ? u.ctx + map.token(0) : 0, blast);
         const int s0 = u.k0, s1 = min(u.k1, spans.count);
         const int32_t *table = p.bk.table + (size_t)u.slot * p.bk.max_pages;
+        if constexpr (WIN && P == Prec::F32) {
+            // The span's chunks, or without partial states every chunk that the block sees, four at a time: to the same states in the
+            // same order.
+            const Visible<WIN, kKeys> chunks(see, u.ctx + map.token(0), blast);
+            const int c0 = u.part < 0 ? 0 : spans.piece(s0) * kSpanChunks;
+            const int count = u.part < 0 ? chunks.count : s0 < s1 ? min(NW, blast / kKeys + 1 - c0) : 0;
+            auto chunk = [&](int j) { return u.part < 0 ? chunks.piece(j) : c0 + j; };
+            struct State {
+                float M = -INFINITY, l = 0.f;
+                f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+                __device__ __forceinline__ void add(float Mn, float ln, f32x4 on) {
+                    float v, vn;
+                    merge_weights(M, Mn, v, vn);
+                    l = merge_value(l, ln, v, vn);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = merge_value(o[e], on[e], v, vn);
+                }
+            } span[ITEMS], all[ITEMS];
+            bool some[ITEMS] = {};  // the row sees a chunk of the span
+            auto end_span = [&](int i) {
+                if (some[i]) all[i].add(span[i].M, span[i].l, span[i].o);
+                span[i] = State();
+                some[i] = false;
+            };
+            for (int j = 0; j < count; j += NW) {
+                const int key0 = chunk(j + w) * kKeys;
+                if (j + w < count && see.some(u.ctx + map.token(0), key0, kKeys)) {  // uniform over the wave
+                    if (RG == 1 || rows <= 16)
+                        span_chunk<P, HD, WIN, 1>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                    else
+                        span_chunk<P, HD, WIN, RG>(p, u, map, h, rows, key0, last_key, table, s_mine, s_m[w], s_l[w]);
+                }
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
+                    if (row >= rows) break;
+                    const int pos = u.ctx + map.token(row);
+#pragma unroll
+                    for (int k = 0; k < NW; ++k) {
+                        if (j + k >= count) break;
+                        const int c = chunk(j + k);
+                        if (j + k > 0 && c / kSpanChunks != chunk(j + k - 1) / kSpanChunks) end_span(i);
+                        if (c * kKeys > pos || !see.some(pos, c * kKeys, kKeys)) continue;
+                        span[i].add(s_m[k][row], s_l[k][row], *reinterpret_cast<const f32x4 *>(
+                            reinterpret_cast<const float *>(s_all + (size_t)k * REGION) + row * SROW + col));
+                        some[i] = true;
+                    }
+                }
+                __syncthreads();  // before the next chunks come into the regions
+            }
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int item = tid + i * NW * kWave, row = item / (HD / 4), col = item % (HD / 4) * 4;
+                if (row >= rows || s0 >= s1) break;
+                if (u.part >= 0) {
+                    const size_t pr = (size_t)(u.part + row) * p.n_kv + h;
+                    *reinterpret_cast<f32x4 *>(p.part_o + pr * HD + col) = span[i].o;
+                    if (col == 0) {
+                        p.part_m[pr] = span[i].M;
+                        p.part_l[pr] = span[i].l;
+                    }
+                } else {
+                    end_span(i);
+                    store_row<P>(p, u.r0 + map.token(row), h * p.group + map.head(row), col, all[i].o, all[i].M, all[i].l);
+                }
+            }
+            continue;
+        }
         // states of this thread's (row, four columns) items over the spans
         float Mr[WHOLE ? ITEMS : 1], lr[WHOLE ? ITEMS : 1];
         f32x4 orow[WHOLE ? ITEMS : 1];
@@ -1303,13 +1372,18 @@ struct WindowCall {
         }
         return e == hipSuccess && join ? launch_join<P, HD, true>((int64_t)n * p.blocks, tiles, p, s) : e;
     }
-    // fp32: whether a block's spans are worked on side by side and joined, or one after another: where the blocks alone take two thirds
-    // of the device, the join and the partial states cost what the spans side by side save. us of a call behind 6 / 600 / 2000 keys, side by
-    // side and one after another: 2 heads over 1 of 64, 54 tokens (4 workgroups) 16.2 / 17.8 / 96.6 (no room) and 20.9 / 40.6 / 96.9; 28 tokens
-    // of 4 over 1 of 128 (28) 17.1 / 21.1 / 32.7 and 27.7 / 52.2 / 110; 2 x 300 of 8 of 32 (160) 13.3 / 30.9 / 61.5 and 18.4 / 31.2 / 61.5;
-    // 22 x 50 of 4 of 64 (176) 28.3 / 52.3 / 93.6 and 28.6 / 50.4 / 102; 3 x 150 of 8 of 128 (240) 30.8 / 63.3 / 118 and 27.9 / 54.5 / 118.
+    // fp32: whether a block's spans are worked on side by side and joined, or its chunks four at a time by one workgroup: about 12 us
+    // for each 256 spans and 4 for the join, or 5 us and 7 for each four chunks. us of a call behind 6 / 300 / 2000 keys, side by side
+    // and one workgroup: 28 tokens of 4 heads over 1 of 128: 17.8 / 21.0 / 32.9 and 15.5 / 39 / 110; 5 requests of 3 to 41 tokens of 12
+    // heads of 64 behind 101: 19.4 and 16.3; 2 of 300 of 8 heads of 32: 14.3 / 24.6 / 61.3 and 10.5 / 17.0 / 61.6; 22 of 50 of 4
+    // heads of 64: 28.3 / 43.0 / 93.6 and 15.7 / 27.6 / 104.
     bool split(const PagedAttnParams &p) const {
-        return (int64_t)p.spans * p.rows * p.group <= p.cap_part && 3 * (int64_t)n * p.blocks * p.n_kv <= 2 * kCUs;
+        if ((int64_t)p.spans * p.rows * p.group > p.cap_part) return false;
+        const double keys = std::min<double>((double)p.window + std::min(p.max_new, 16 * RG) - 1, p.max_len);
+        const double chunks = keys / kKeys + 1 + (p.sinks + kKeys - 1) / kKeys;
+        const double spans = keys / kPagedSpanKeys + 1 + (p.sinks + kPagedSpanKeys - 1) / kPagedSpanKeys;
+        const double rounds = (double)n * p.blocks * p.n_kv / kCUs;
+        return 12 * std::max(rounds * spans, 1.0) + 4 < (5 + 7 * (chunks / kSpanChunks + 0.5)) * std::max(rounds, 1.0);
     }
 };
 
