@@ -149,13 +149,14 @@ struct Eight {
     }
 };
 
-// The request of a row: the last one that starts at or before it (a wave's two reads; n up to 1024).
-__device__ __forceinline__ int request_of(const int32_t *row_start, int n, int row) {
-    const int lane = threadIdx.x & 63;
-    if (n <= kWave) return max((int)__popcll(__ballot(lane < n && row_start[min(lane, n)] <= row)) - 1, 0);
-    const uint64_t far = __ballot(16 * lane < n && row_start[min(16 * lane, n)] <= row);
+// The request of a row: the last one that starts at or before it (a wave's two reads; n up to 1024). Of the plan's starts only
+// those of its own requests count: behind them is what an earlier plan of more left.
+__device__ __forceinline__ int request_of(const VerifyParams &p, int row) {
+    const int lane = threadIdx.x & 63, n = p.n, own = p.status ? min(n, p.status[PS_ENTRIES]) : n;
+    if (n <= kWave) return max((int)__popcll(__ballot(lane < own && p.row_start[min(lane, n)] <= row)) - 1, 0);
+    const uint64_t far = __ballot(16 * lane < own && p.row_start[min(16 * lane, n)] <= row);
     const int c = 16 * max((int)__popcll(far) - 1, 0);  // (a row before the first request is counted to that)
-    const uint64_t near = __ballot(lane < 16 && c + lane < n && row_start[min(c + lane, n)] <= row);
+    const uint64_t near = __ballot(lane < 16 && c + lane < own && p.row_start[min(c + lane, n)] <= row);
     return min(c + max((int)__popcll(near) - 1, 0), n - 1);
 }
 
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
     int b = 0;
     bool live = chunk < p.chunks;  // uniform over the wave
     if (isq) {
-        b = request_of(p.row_start, p.n, r);
+        b = request_of(p, r);
         live = live && r + 1 < p.row_start[b + 1];  // no draft behind the request's last row
     }
     Eight<PR> x[kParts];
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(VerifyParams p, 
     }
     make_table(table);
     if (!live) return;
-    if (!isq) b = request_of(p.row_start, p.n, r);
+    if (!isq) b = request_of(p, r);
     const float temperature = p.temperature[b];
     const double scale = weight_scale(temperature), floor = weight_floor(temperature);
     float size = 0.0f;
