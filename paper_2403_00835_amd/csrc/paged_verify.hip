@@ -299,6 +299,9 @@ struct Decide {  // LDS
     int stop;
 };
 
+// Place of a request's row, by `lanes` lanes, among the threads of verify_token_kernel.
+constexpr int head_of(int row, int lanes) { return row % (kToken / lanes) * lanes; }
+
 // Where a request stops, by the whole workgroup: a row LANES lanes. heads (or null): statistics of the first LANES chunks of the row
 // at which it stops, in those lanes' places.
 template <int LANES>
@@ -605,7 +608,7 @@ __global__ __launch_bounds__(kToken) void verify_token_kernel(VerifyParams p) {
     // What is drawn from: the rest, p without the refused token, or p (also where those are empty).
     bool rest = at.kind & VS_REST;
     int without = !rest && (at.kind & VS_REFUSED) ? at.draft : -1;
-    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks, *head = s_heads + (p.chunks <= kFewChunks ? (at.row - at.first) * kFewChunks : (at.row - at.first) * kWave) % kToken;
+    const VerifyStat *st = p.stats + (size_t)at.row * p.chunks, *head = s_heads + head_of(at.row - at.first, p.chunks <= kFewChunks ? kFewChunks : kWave);
     auto stat = [&](int c) { return p.draft || c >= kWave ? st[c] : head[c]; };
     double cut = 0.0;  // the sum of the refused token's chunk without it
     if (without >= 0) {

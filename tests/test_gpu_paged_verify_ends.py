@@ -1,6 +1,6 @@
-"""GPU tests of PagedCache.verify on the last plan's rows (row_start None) for more requests than that plan has, as a program that
-verifies for all of its slots does: behind a plan of more requests, whose starts the array still holds. Results are whole numbers
-and have to be equal to those of tests/verify_ref.py."""
+"""GPU tests of PagedCache.verify at the ends of what a call may be: for more requests than the last plan has (row_start None), as a
+program that verifies for all of its slots does, behind a plan of more requests, whose starts the array still holds; for
+requests of very many rows. Results are whole numbers and have to be equal to those of tests/verify_ref.py."""
 import random
 
 import numpy as np
@@ -78,3 +78,18 @@ def test_more_requests_than_the_last_plans(binding, n, with_draft, captured):
         side.synchronize()
         if captured:
             del graph
+
+
+def test_a_request_of_more_rows_than_31_bits_of_threads(binding):
+    """16 threads decide on a row: 2^27 rows and some, all of which stand, as the drafts' weights are above 0; the last row's token
+    is drawn from the statistics that were kept for its place."""
+    rows, vocab = 2 ** 27 + 70, 3
+    c = make(binding)
+    logits = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    logits[-1] = torch.tensor([0.0, 4.0, 2.0])
+    p = ref.law([0.0, 4.0, 2.0], 1.0)
+    start, tokens, zeros = ints([0, 0, rows]), ints([0]).expand(rows).contiguous(), f64([0.0]).expand(rows).contiguous()
+    accepted, following = ints([9, 9]), ints([9, 9])
+    for u in (0.5, 0.99):
+        c.verify(tokens, logits, accepted, following, torch.ones(2, device="cuda"), zeros, f64([0.5, u]), row_start=start)
+        assert accepted.tolist() == [0, rows] and following.tolist() == [-1, ref.draw(p, u)]
