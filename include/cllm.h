@@ -565,7 +565,7 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * workspace: device memory of at least cllm_paged_verify_bytes() bytes (draft: whether there are draft logits), 256-byte
  * aligned, used during the call: one for every stream that such calls run on at once. No allocation, no wait.
  * Errors: ERR_ARG (n outside [1, max_seqs], sizes, strides, NULL or inaccessible arrays), ERR_STATE (row_start NULL before
- * a plan), ERR_CAPACITY (workspace too small, vocab above 2^30, rows x vocab above 2^41), ERR_DEVICE. */
+ * a plan), ERR_CAPACITY (workspace too small, vocab above 2^30, rows x ceil(vocab / 2048) from 2^30 - 2^14 on), ERR_DEVICE. */
 cllm_status cllm_paged_verify(cllm_paged *c, int32_t n, const int32_t *row_start, int32_t rows, const int32_t *tokens, int32_t dtype,
                               int32_t vocab, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride,
                               const float *temperature, const double *accept_u, const double *sample_u, int32_t *accepted,

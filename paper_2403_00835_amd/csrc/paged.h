@@ -141,6 +141,7 @@ struct PagedAttnParams {
 };
 
 constexpr int kVerifyChunk = 2048;  // logits whose statistics one wave takes
+constexpr int kVerifyLaunch = 1 << 15;  // rows whose statistics one launch forms
 struct alignas(16) VerifyStat {
     double sum;  // of the weights, relative to max
     float max;   // a logit (greedy requests: the largest); NaN where one is, or +inf

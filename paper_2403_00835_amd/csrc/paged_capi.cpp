@@ -551,7 +551,8 @@ cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, 
     *bytes = 0;
     if (rows < 0 || vocab < 1) return CLLM_ERR_ARG;
     const int64_t parts = (int64_t)rows * ((vocab - 1) / kVerifyChunk + 1);
-    if (vocab > 1 << 30 || 2 * parts > INT32_MAX) return CLLM_ERR_CAPACITY;  // (a chunk past the last is counted in 31 bits)
+    // (a chunk past the last is counted in 31 bits, and so are the rows of a launch past the last one's)
+    if (vocab > 1 << 30 || 2 * parts > INT32_MAX - kVerifyLaunch) return CLLM_ERR_CAPACITY;
     const size_t n = rows;
     *bytes = round_up(draft ? parts * (2 * sizeof(VerifyStat) + sizeof(double)) + n * (sizeof(VerifyStop) + 2 * sizeof(float))
                             : parts * sizeof(VerifyStat) + n * sizeof(float));

@@ -729,9 +729,9 @@ namespace {
 template <Prec PR>
 hipError_t launch_verify(const VerifyParams &p, hipStream_t s) {
     if (p.rows > 0) {
-        const int per = kThreads / kWave, rows = p.rows * (p.draft ? 2 : 1), most = 1 << 15;
-        for (int r = 0; r < rows; r += most)
-            hipLaunchKernelGGL(verify_stats_kernel<PR>, dim3((unsigned)((p.chunks + per - 1) / per), (unsigned)std::min(rows - r, most)),
+        const int per = kThreads / kWave, rows = p.rows * (p.draft ? 2 : 1);
+        for (int r = 0; r < rows; r += kVerifyLaunch)
+            hipLaunchKernelGGL(verify_stats_kernel<PR>, dim3((unsigned)((p.chunks + per - 1) / per), (unsigned)std::min(rows - r, kVerifyLaunch)),
                                dim3(kThreads), 0, s, p, r);
         if (p.draft) {  // about as many workgroups as run at once, as each decides first, with about as many chunks each
             const int units = (p.chunks + kRestChunks - 1) / kRestChunks, fit = std::max(kRestFit * kCUs / p.n, 1);
@@ -747,7 +747,7 @@ hipError_t launch_verify(const VerifyParams &p, hipStream_t s) {
 
 hipError_t launch_paged_verify(bool bf16, const VerifyParams &p, hipStream_t s) {
     if (p.n < 1 || p.n > kPagedMaxSeqs || p.rows < 0 || p.vocab < 1 || p.chunks != (p.vocab - 1) / kVerifyChunk + 1 ||
-        (int64_t)p.rows * p.chunks * 2 > INT32_MAX)
+        (int64_t)p.rows * p.chunks * 2 > INT32_MAX - kVerifyLaunch)
         return hipErrorInvalidValue;
     return bf16 ? launch_verify<Prec::BF16>(p, s) : launch_verify<Prec::F32>(p, s);
 }
