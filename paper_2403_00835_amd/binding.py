@@ -449,6 +449,8 @@ class PagedCache:
     PyTorch's current stream in every call. block_table, seq_pages, free_list, row_start, row_slot and
     row_pos are int32 tensors over the cache's own books, to be read in that stream's order."""
 
+    rope_base = 0.0
+
     def __init__(self, n_heads, n_kv_heads, head_dim, page_size, n_pages, max_seqs, max_ctx, max_rows, dtype="bf16",
                  rope_base=0.0, device=0, stream=None):
         import torch
@@ -457,7 +459,7 @@ class PagedCache:
         self.L = lib()
         self.h = None
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
-        self.max_rows, self.rows = max_rows, 0
+        self.max_rows, self.rows, self.rope_base = max_rows, 0, rope_base
         self.dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self._int32, self._float32 = torch.int32, torch.float32
         self._logits = {torch.bfloat16: 1, torch.float32: 0}
@@ -575,11 +577,12 @@ class PagedCache:
         self.rows = rows
         _changed(self._ws)
 
-    def rotary(self, layout="half", dim=0, base=10000.0, scaling=None, factor=0.0, orig_ctx=0.0, low=0.0, high=0.0, magnitude=1.0,
+    def rotary(self, layout="half", dim=0, base=None, scaling=None, factor=0.0, orig_ctx=0.0, low=0.0, high=0.0, magnitude=1.0,
                freqs=None):
         """cllm_paged_rotary: the form of the rotation in later appends. layout "half" or "interleaved"; dim: the
-        elements of a head that are turned (0: all); scaling None, "linear" (factor) or "parts" (factor, orig_ctx, low,
-        high); freqs: the angles a position themselves, dim / 2 numbers, in place of base and scaling."""
+        elements of a head that are turned (0: all); base None: the cache's rope_base; scaling None, "linear" (factor)
+        or "parts" (factor, orig_ctx, low, high); freqs: the angles a position themselves, dim / 2 numbers, in place of
+        base and scaling."""
         self._on_stream()
         if layout not in ("half", "interleaved"):
             raise ValueError("layout must be 'half' or 'interleaved'")
@@ -591,8 +594,8 @@ class PagedCache:
             if scaling is not None or len(freqs) != (dim or self.head_dim) // 2:
                 raise ValueError(f"freqs: {(dim or self.head_dim) // 2} numbers, and no scaling")
             freqs = (_dbl * max(len(freqs), 1))(*[float(x) for x in freqs])
-        spec = cllm_paged_rotary_spec(("half", "interleaved").index(layout), dim, (None, "linear", "parts").index(scaling), base,
-                                      factor, orig_ctx, low, high, magnitude, freqs)
+        spec = cllm_paged_rotary_spec(("half", "interleaved").index(layout), dim, (None, "linear", "parts").index(scaling),
+                                      self.rope_base if base is None else base, factor, orig_ctx, low, high, magnitude, freqs)
         self._check(self.L.cllm_paged_rotary(self.h, ctypes.byref(spec)))
         _changed(self._ws)
 
