@@ -488,8 +488,9 @@ cllm_status cllm_paged_append(cllm_paged *c, const void *q, int64_t q_stride, co
  * 2 pi - low) / (high - low) within [0, 1] (BY_PARTS: pairs of more than `high` turns over the original context
  * keep their angle, those of fewer than `low` are stretched). freqs (host, dim / 2 doubles, or NULL) gives the
  * theta_j themselves in place of base and scaling. Sines and cosines are formed in double, times magnitude (0
- * means 1), and rounded once to fp32. The factors are made again on the cache's stream; a captured append keeps the
- * layout and dim that it was captured with, so capture it again behind this call, which itself is not captured.
+ * means 1), and rounded once to fp32. The factors are made again on the cache's stream, and a captured append
+ * takes them from then on; one that was captured with another layout or dim does nothing, and cllm_paged_status says
+ * so: capture it again behind this call, which itself is not captured.
  * Errors: ERR_ARG, ERR_STATE (rope_base 0, or the stream is being captured), ERR_DEVICE. */
 #define CLLM_ROTARY_HALVES 0
 #define CLLM_ROTARY_NEIGHBOURS 1
@@ -575,8 +576,8 @@ cllm_status cllm_paged_verify_bytes(int32_t rows, int32_t vocab, int32_t draft, 
 
 /* Waits for the stream and says how the last plan went: its rows and the free pages (either may be
  * NULL). Errors: ERR_ARG or ERR_CAPACITY (the plan was refused), ERR_STATE (append or attention of a
- * replayed graph ran behind a plan with other bounds than its own and did nothing; or the stream is
- * being captured), ERR_DEVICE. */
+ * replayed graph ran behind a plan with other bounds than its own, or append behind another form of the rotation,
+ * and did nothing; or the stream is being captured), ERR_DEVICE. */
 cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages);
 const char *cllm_paged_last_error(const cllm_paged *c);
 

@@ -35,7 +35,7 @@ constexpr int kPartRows = 1 << 20;     // above the partial rows of an fp32 cach
 constexpr int kPagedTileGroups = 512;   // workgroups that fill the device (two a CU): tiles of few requests are split into
                                         // about as many
 
-// Words of the status block, written by the plan.
+// Words of the status block, written by the plan (but PS_FORM).
 enum PagedStatus {
     PS_ROWS = 0,     // rows of the plan (0 when it was refused)
     PS_ENTRIES = 1,  // requests of the plan
@@ -46,6 +46,8 @@ enum PagedStatus {
     PS_BOUND_ROWS = 6, PS_BOUND_NEW = 7, PS_BOUND_LEN = 8,  // the plan's bounds
     PS_ITEMS = 9,    // row blocks whose partial states are joined
     PS_LATE = 10,    // a call made for other bounds than the plan's ran (and did nothing)
+    PS_FORM = 11,    // the form of the rotary factors, as rotary_form has it; written with them
+    PS_OTHER = 12,   // an append made for another form ran behind the plan (and did nothing)
     PS_WORDS = 16
 };
 enum PagedFlags { PF_ARG = 1, PF_ROWS = 2, PF_PAGES = 4 };
@@ -101,6 +103,9 @@ struct PagedPlanParams {
     int cap_part;                   // partial rows of row blocks; those of tiles are behind them
 };
 
+// Pairs that are turned and their layout, as one number (0: no rotation).
+inline int rotary_form(int rot, bool inter) { return 2 * rot + inter; }
+
 struct PagedAppendParams {
     PagedBooks bk;
     int rows, max_new, max_len;  // the bounds that the call was made for
@@ -111,6 +116,7 @@ struct PagedAppendParams {
     int n_heads, n_kv, hd;
     int rot;                     // pairs of a head that are turned (0: none)
     bool inter;                  // pairs (2 j, 2 j + 1) in place of (j, j + rot)
+    int form;                    // rotary_form of both
     const float *q_gain, *k_gain;  // [hd], or null: no norm
     float eps;
 };
@@ -188,12 +194,21 @@ __device__ __forceinline__ int bounded_rows(const PagedBooks &bk, int rows, int 
     if (blockIdx.x == 0 && threadIdx.x == 0) bk.status[PS_LATE] = 1;
     return 0;
 }
+// Those of an append: none either where the factors have been made again in another form than the call's (a replayed graph behind
+// cllm_paged_rotary), which has them at other places.
+__device__ __forceinline__ int append_rows(const PagedAppendParams &p) {
+    const int form = p.bk.status[PS_FORM], R = bounded_rows(p.bk, p.rows, p.max_new, p.max_len);
+    if (R == 0 || form == p.form) return R;
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.bk.status[PS_OTHER] = 1;
+    return 0;
+}
 
 hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int hd,
                              double rope_base, hipStream_t s);
 hipError_t launch_paged_plan(const PagedPlanParams &p, hipStream_t s);
 hipError_t launch_paged_verify(bool bf16, const VerifyParams &p, hipStream_t s);
-hipError_t launch_paged_rotary(float *rcos, float *rsin, int max_ctx, int rot, double magnitude, const PagedFreqs &f, hipStream_t s);
+hipError_t launch_paged_rotary(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int rot, bool inter, double magnitude,
+                               const PagedFreqs &f, hipStream_t s);
 hipError_t launch_paged_append(bool bf16, const PagedAppendParams &p, hipStream_t s);
 // The same with norms of the heads, and with any part of the head turned in either layout.
 hipError_t launch_paged_append_forms(bool bf16, const PagedAppendParams &p, hipStream_t s);

@@ -90,12 +90,12 @@ __device__ __forceinline__ void for_items(const int *start, int n, int total, F 
 
 // The stack of free pages (page 0 on top), empty tables, and the rotary factors: angle
 // t * base^(-2 j / hd) in double, rounded once to fp32.
-__global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64_t n_rot, int hd, double base) {
+__global__ void paged_init_kernel(PagedBooks bk, float *rcos, float *rsin, int64_t n_rot, int hd, double base, int form) {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i < bk.n_pages) bk.free_list[i] = bk.n_pages - 1 - (int)i;
     if (i < (int64_t)bk.max_seqs * bk.max_pages) bk.table[i] = -1;
     if (i < bk.max_seqs) bk.seq_pages[i] = 0;
-    if (i < PS_WORDS) bk.status[i] = i == PS_FREE ? bk.n_pages : 0;
+    if (i < PS_WORDS) bk.status[i] = i == PS_FREE ? bk.n_pages : i == PS_FORM && rcos ? form : 0;
     if (i < n_rot) {
         const int h2 = hd / 2, j = (int)(i % h2);
         const double ang = (double)(i / h2) * pow(base, -2.0 * j / (double)hd);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         if (b == 0) {
             bk.status[PS_ROWS] = bk.status[PS_ENTRIES] = bk.status[PS_UNITS] = bk.status[PS_TILES] = bk.status[PS_ITEMS] = 0;
             bk.status[PS_FLAGS] = flags;
-            bk.status[PS_LATE] = 0;
+            bk.status[PS_LATE] = bk.status[PS_OTHER] = 0;
         }
         return;
     }
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedPlanParam
         bk.status[PS_BOUND_ROWS] = p.rows;
         bk.status[PS_BOUND_NEW] = p.max_new;
         bk.status[PS_BOUND_LEN] = p.max_len;
-        bk.status[PS_LATE] = 0;
+        bk.status[PS_LATE] = bk.status[PS_OTHER] = 0;
     }
 }
 
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
     using PT = PrecT<PR>;
     using T = typename PT::T;
     constexpr int VEC = PT::VEC;
-    const int R = bounded_rows(p.bk, p.rows, p.max_new, p.max_len);
+    const int R = append_rows(p);
     const int h2 = p.hd / 2, nv = h2 / VEC, heads = p.n_heads + 2 * p.n_kv, h_first = p.q ? 0 : p.n_heads;
     const int per_row = (heads - h_first) * nv;
     const int64_t total = (int64_t)R * per_row;
@@ -357,9 +357,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendParams p) 
 }
 
 // Factors of one pair j at every position: cos and sin of t * f[j] in double, times the magnitude, rounded once.
-__global__ __launch_bounds__(256) void paged_rotary_kernel(float *rcos, float *rsin, int max_ctx, int rot, double magnitude,
-                                                           PagedFreqs f) {
+__global__ __launch_bounds__(256) void paged_rotary_kernel(PagedBooks bk, float *rcos, float *rsin, int max_ctx, int rot, int form,
+                                                           double magnitude, PagedFreqs f) {
     const int t = (int)blockIdx.x * 256 + threadIdx.x, j = blockIdx.y;
+    if (t == 0 && j == 0) bk.status[PS_FORM] = form;
     if (t >= max_ctx) return;
     const double ang = (double)t * f.f[j];
     rcos[(size_t)t * rot + j] = (float)(cos(ang) * magnitude);
@@ -431,7 +432,7 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
     using T = typename PT::T;
     constexpr int VEC = PT::VEC, H = VEC / 2;
     __shared__ float s_pairs[F == SCATTERED ? 256 * 2 * (VEC + 1) : 1];
-    const int R = bounded_rows(p.bk, p.rows, p.max_new, p.max_len);
+    const int R = append_rows(p);
     const int nv = p.hd / 2 / VEC, nv_shift = 31 - __clz(nv), half = p.hd / 2;
     const int q_segs = p.q ? (p.n_heads + U - 1) / U : 0, kv_segs = (p.n_kv + U - 1) / U;
     const float inv_hd = 1.0f / (float)p.hd;  // (a power of two)
@@ -584,10 +585,11 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
     }
 }
 
-hipError_t launch_paged_rotary(float *rcos, float *rsin, int max_ctx, int rot, double magnitude, const PagedFreqs &f, hipStream_t s) {
+hipError_t launch_paged_rotary(const PagedBooks &bk, float *rcos, float *rsin, int max_ctx, int rot, bool inter, double magnitude,
+                               const PagedFreqs &f, hipStream_t s) {
     if (!rcos || !rsin || rot < 1 || rot > kMaxRot || max_ctx < 1) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(paged_rotary_kernel, dim3((unsigned)((max_ctx + 255) / 256), (unsigned)rot), dim3(256), 0, s, rcos, rsin,
-                       max_ctx, rot, magnitude, f);
+    hipLaunchKernelGGL(paged_rotary_kernel, dim3((unsigned)((max_ctx + 255) / 256), (unsigned)rot), dim3(256), 0, s, bk, rcos,
+                       rsin, max_ctx, rot, rotary_form(rot, inter), magnitude, f);
     return hipGetLastError();
 }
 
@@ -643,7 +645,7 @@ hipError_t launch_paged_init(const PagedBooks &bk, float *rcos, float *rsin, int
     const int64_t n_rot = rcos ? (int64_t)max_ctx * (hd / 2) : 0;
     const int64_t n = std::max({n_rot, (int64_t)bk.max_seqs * bk.max_pages, (int64_t)bk.n_pages, (int64_t)PS_WORDS});
     hipLaunchKernelGGL(paged_init_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, bk, rcos, rsin, n_rot, hd,
-                       rope_base);
+                       rope_base, rotary_form(hd / 2, false));
     return hipGetLastError();
 }
 

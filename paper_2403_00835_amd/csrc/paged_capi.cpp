@@ -370,10 +370,11 @@ cllm_status cllm_paged_rotary(cllm_paged *c, const cllm_paged_rotary_spec *spec)
         (void)hipGetLastError();
         return fail(c, CLLM_ERR_STATE, "the form of the rotation cannot be changed while the stream is captured");
     }
-    HIPCHK(c, launch_paged_rotary(c->rcos, c->rsin, f.max_ctx, rot, spec->magnitude == 0.0f ? 1.0 : (double)spec->magnitude, fr,
-                                  c->stream));
+    const bool inter = spec->layout == CLLM_ROTARY_NEIGHBOURS;
+    HIPCHK(c, launch_paged_rotary(c->bk, c->rcos, c->rsin, f.max_ctx, rot, inter,
+                                  spec->magnitude == 0.0f ? 1.0 : (double)spec->magnitude, fr, c->stream));
     c->rot = rot;
-    c->inter = spec->layout == CLLM_ROTARY_NEIGHBOURS;
+    c->inter = inter;
     return CLLM_OK;
 }
 
@@ -425,6 +426,7 @@ cllm_status append(cllm_paged *c, const void *q, int64_t q_stride, const void *k
     p.hd = f.head_dim;
     p.rot = c->rot;
     p.inter = c->inter;
+    p.form = rotary_form(c->rot, c->inter);
     p.q_gain = q_gain;
     p.k_gain = k_gain;
     p.eps = eps;
@@ -645,6 +647,7 @@ cllm_status cllm_paged_status(cllm_paged *c, int32_t *rows, int32_t *free_pages)
     if (st[PS_FLAGS] & PF_ROWS) return fail(c, CLLM_ERR_CAPACITY, "the plan was refused: more rows than its bound");
     if (st[PS_FLAGS] & PF_PAGES) return fail(c, CLLM_ERR_CAPACITY, "the plan was refused: too few free pages");
     if (st[PS_LATE]) return fail(c, CLLM_ERR_STATE, "a call made for another plan's bounds ran after the plan and did nothing");
+    if (st[PS_OTHER]) return fail(c, CLLM_ERR_STATE, "an append made for another form of the rotation ran after the plan and did nothing");
     return CLLM_OK;
 }
 
