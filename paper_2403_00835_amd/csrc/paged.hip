@@ -506,11 +506,11 @@ __global__ __launch_bounds__(256) void paged_append_forms_kernel(PagedAppendPara
                             return head_sum(ss, nv) * inv_hd;
                         };
                         float ms = squares(), eps = p.eps;
-                        if (!(ms <= 3.4e38f)) {  // squares past fp32: of 2^-80 of the values, beside which eps is nothing
+                        if (!(ms + eps <= 3.4e38f)) {  // past fp32: of 2^-80 of the values
 #pragma unroll
                             for (int i = 0; i < 2 * VEC; ++i) y[i] *= 0x1p-80f;
                             ms = squares();
-                            eps = 0.f;
+                            eps = eps * 0x1p-80f * 0x1p-80f;
                         }
                         const float f = __builtin_amdgcn_rsqf(ms + eps);  // (the instruction: one unit in the last place)
 #pragma unroll

@@ -1,4 +1,6 @@
-"""GPU tests of the form of the rotation as a cache keeps it, against the float64 references of tests/test_gpu_paged_forms.py."""
+"""GPU tests of the form of the rotation as a cache keeps it, and of the norms' largest eps, against the float64 references of
+tests/test_gpu_paged_forms.py."""
+import numpy as np
 import pytest
 
 from tests.test_gpu_paged import host, ints, make
@@ -74,3 +76,20 @@ def test_a_captured_append_behind_another_form(binding, own, norms):
             right(own)
         side.synchronize()
         del graph
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("f32", 64), ("f32", 16)])
+@pytest.mark.parametrize("eps", [1e-6, 1e30, 1e38, 3e38, float(np.finfo(np.float32).max)])
+def test_means_and_eps_whose_sum_passes_fp32(binding, dtype, hd, eps):
+    """Heads of 1, 1e15, and mean squares at, near and far above eps."""
+    sizes = [1.0, 1e15, 1e18, 1.5e19, 1.8e19, 3e19, 1e20, 1e30]
+    c = make(binding, page=16, n_pages=2, max_seqs=1, max_ctx=32, max_rows=4, heads=8, kv=8, hd=hd, dtype=dtype, rope_base=10000.0)
+    c.plan(ints([0]), ints([3]), ints([2]), rows=2)
+    g = torch.Generator(device="cuda").manual_seed(hd)
+    x = (torch.randn(2, 8, hd, generator=g, device="cuda") * torch.tensor(sizes, device="cuda")[:, None]).to(c.dtype)
+    gain, out = torch.randn(hd, generator=g, device="cuda"), torch.empty_like(x)
+    pools = [torch.zeros(c.pool_shape, device="cuda", dtype=c.dtype) for _ in range(2)]
+    c.append(x, x, x, out, *pools, q_gain=gain, k_gain=gain, eps=eps)
+    keys = pools[0].transpose(1, 2).reshape(-1, 8, hd)[c.row_slot[:2].long()]
+    for got in (out, keys):
+        check(host(got), host(x), host(gain), float(np.float32(eps)), [3, 4], angles(hd), "half", c.dtype)
