@@ -432,6 +432,13 @@ def _changed(*tensors):
     _increment_version(tensors)
 
 
+def _count(x, name):
+    """x as the library takes it: ctypes would drop what is past 32 bits."""
+    if not -1 << 31 <= x < 1 << 31:
+        raise ValueError(f"{name} {x} is past 32 bits")
+    return x
+
+
 class PagedCache:
     """A paged KV cache (cllm_paged_*): the books of a page pool that the requests of a server share,
     and the operators of a step on it, on PyTorch tensors of the cache's GPU:
@@ -594,7 +601,7 @@ class PagedCache:
             if scaling is not None or len(freqs) != (dim or self.head_dim) // 2:
                 raise ValueError(f"freqs: {(dim or self.head_dim) // 2} numbers, and no scaling")
             freqs = (_dbl * max(len(freqs), 1))(*[float(x) for x in freqs])
-        spec = cllm_paged_rotary_spec(("half", "interleaved").index(layout), dim, (None, "linear", "parts").index(scaling),
+        spec = cllm_paged_rotary_spec(("half", "interleaved").index(layout), _count(dim, "dim"), (None, "linear", "parts").index(scaling),
                                       self.rope_base if base is None else base, factor, orig_ctx, low, high, magnitude, freqs)
         self._check(self.L.cllm_paged_rotary(self.h, ctypes.byref(spec)))
         _changed(self._ws)
@@ -654,7 +661,7 @@ class PagedCache:
     def verify_workspace_bytes(rows, vocab, draft):
         """cllm_paged_verify_bytes: bytes of the workspace of verify on so many rows, with draft logits or without."""
         n = ctypes.c_size_t(0)
-        st = lib().cllm_paged_verify_bytes(rows, vocab, 1 if draft else 0, ctypes.byref(n))
+        st = lib().cllm_paged_verify_bytes(_count(rows, "rows"), _count(vocab, "vocab"), 1 if draft else 0, ctypes.byref(n))
         if st != CLLM_OK:
             raise CllmError(st, "cllm_paged_verify_bytes failed")
         return int(n.value)
@@ -685,7 +692,7 @@ class PagedCache:
         self._on_stream()
         if logits.dim() != 2 or logits.dtype not in self._logits:
             raise ValueError(f"logits: bfloat16 or float32 [rows, vocab], got {logits.dtype} {tuple(logits.shape)}")
-        shape, n = logits.shape, accepted.numel()
+        shape, n = logits.shape, _count(accepted.numel(), "accepted of size")
         rows, vocab = shape
         i32, f64 = self._int32, self._float64
         lg = self._logit_rows(logits, shape, logits.dtype, "logits")
