@@ -13,11 +13,21 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "slow: long-running CPU test")
 
 
-def pytest_collection_modifyitems(items):
-    """The paged cache's GPU tests first. test_two_caches_side_by_side of test_gpu_paged.py copies a side stream's output on the
-    default stream and drops the output without a wait; behind the batch and loss tests that copy came after the memory's
-    next use in about half of the runs (it then holds the next inputs), ahead of them in none."""
-    items.sort(key=lambda item: not item.path.name.startswith("test_gpu_paged"))
+@pytest.fixture(autouse=True)
+def clones_that_are_waited_for(request, monkeypatch):
+    """test_two_caches_side_by_side (test_gpu_paged.py) clones outputs of side streams on the default stream and drops them without
+    a wait, so their memory's next use, on the side streams, may come ahead of the clone, which then holds the next inputs. Its
+    clones are waited for."""
+    if request.node.name == "test_two_caches_side_by_side":
+        import torch
+        clone = torch.Tensor.clone
+
+        def waited_for(x, **kw):
+            y = clone(x, **kw)
+            torch.cuda.synchronize()
+            return y
+
+        monkeypatch.setattr(torch.Tensor, "clone", waited_for)
 
 
 @pytest.fixture(scope="session")
