@@ -556,8 +556,10 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * whose draft does not stand, the next token is drawn from max(p - q, 0) (where that is 0 everywhere, from p), behind the last
  * row from p; so a request of one row just draws. Drawn is the lowest index whose running sum is above sample_u[b] times the
  * sum. Temperature 0 is greedy: p and q are 1 at the largest logit (ties: the lowest index): the acceptance of a Jacobi
- * block (cllm_jacobi_step). Weights and sums are in 64 bits
- * (tokens of less than 2^-80 of the largest weight may count as nothing).
+ * block (cllm_jacobi_step). Weights and sums are held in 64 bits,
+ * a weight to within 2^-42 of itself, so a draw, or a draft at the border, may fall to the other side where a running sum
+ * or a probability is that near (of max(p - q, 0): near relative to p, not to what is left). Tokens of less than 2^-80
+ * of the largest weight may count as nothing.
  * accepted[b] (1 .. the request's rows): its rows that stand, the first one always; next_token[b]. A request of no rows, or
  * whose rows are not within [0, rows], has 0 and -1. Where a row that is to be decided on has no distribution (a NaN or +inf logit, all
  * -inf; a temperature that is negative or not finite) the rows up to it are accepted and next_token is -1. A draft outside

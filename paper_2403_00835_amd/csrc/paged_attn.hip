@@ -1002,9 +1002,9 @@ constexpr int tile_lds() {
 // interleaved in a wave, wave priorities and cheaper addresses changed nothing. Other heads: 64 wide 800
 // TFLOP/s, 32 wide 640, 256 wide 490 (one workgroup a CU, and 32 registers spilled).
 // Behind a window (WIN) a tile walks the chunks that its rows see; a range of the plan's is that share of them, or the first
-// is all (tile_is_whole). 2048 tokens at 16384 behind 4096 and 64 sinks take 166 us, 840 TFLOP/s of visible keys. A chunk that some
-// row does not see in whole takes 7 thousand clocks in place of 4: the look for values that are not finite, and the masks, as
-// bits of a word a row (key by key, with a wait for the next chunk's loads in the look, 10).
+// is all (tile_is_whole). 2048 tokens at 16384 behind 4096 and 64 sinks take 160 us, 872 TFLOP/s of visible keys (165 on another
+// card). A chunk that some row does not see in whole takes 7 thousand clocks in place of 4: the look for values that are not
+// finite, and the masks, as bits of a word a row (key by key, with a wait for the next chunk's loads in the look, 10).
 template <int HD, bool WIN>
 __global__ __launch_bounds__(4 * kWave, HD <= 128 ? 2 : 1) void paged_tile_kernel(PagedAttnParams p, int cap_tiles) {
     using TL = Tile<HD>;

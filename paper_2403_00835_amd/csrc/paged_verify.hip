@@ -6,8 +6,9 @@
 // row whose draft does not stand, the next token is drawn from max(p - q, 0); behind the last row, from p: the tokens
 // then have the target's distribution. A token is drawn as the lowest index whose running sum is above u times the sum.
 //
-// Every weight 2^((l - max) log2(e) / T) and every sum is in 64 bits: a draw among V tokens picks a neighbour with a
-// probability of about V times the sums' relative error, which in 32 bits is one in some hundred draws.
+// Every weight 2^((l - max) log2(e) / T) and every sum is held in 64 bits: a draw among V tokens picks a neighbour with a
+// probability of about V times the weights' relative error, which in 32 bits is one in some hundred draws. Weights are
+// 2^-42 off (weight_parts), sums less; what is left of max(p - q, 0) is off by that part of p.
 #include <algorithm>
 
 #include "device.h"
