@@ -548,7 +548,8 @@ cllm_status cllm_paged_attn_window(cllm_paged *c, const void *q, int64_t q_strid
  * accepted counts are on the device, as the lengths of the next plan are.
  *
  * Request b of n has the rows [row_start[b], row_start[b + 1]) of tokens, logits and draft_logits (device, ascending;
- * row_start NULL: those of the last plan, none where it was refused; rows: the host's bound of row_start[n]). Row r's
+ * row_start NULL: those of the last plan, none for requests behind its own or where it was refused; rows: the host's
+ * bound of row_start[n]). Row r's
  * logits (vocab of them, of dtype, any row stride and element's alignment) are the target's behind tokens[r];
  * tokens[r + 1] is its draft. With p = softmax(logits /
  * temperature[b]) and q the softmax of the draft's logits at the same temperature (draft_logits NULL, or a row of them
